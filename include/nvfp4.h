@@ -76,7 +76,9 @@ enum { NVFP4_OP_QUANTIZE = 0, NVFP4_OP_KV_QUANT = 1, NVFP4_OP_GEMM_ACT_QUANT = 2
        NVFP4_OP_KV_DEQUANT_GATHER = 9, NVFP4_OP_QUANTIZE_2D = 10,
        NVFP4_OP_QUANTIZE_RHT = 11, NVFP4_OP_QUANTIZE_A2A = 12,
        NVFP4_OP_LORA_DOWN = 13, NVFP4_OP_GEMM_LORA = 14,
-       NVFP4_OP_PROBE = 15 /* timing only: nvfp4_probe */, NVFP4_OP_GEMM_SCALE_OUT = 16 };
+       NVFP4_OP_PROBE = 15 /* timing only: nvfp4_probe */, NVFP4_OP_GEMM_SCALE_OUT = 16,
+       NVFP4_OP_QK_NORM_ROPE = 17, NVFP4_OP_QK_NORM_ROPE_BACKWARD = 18, NVFP4_OP_KV_CACHE_WRITE = 19,
+       NVFP4_OP_KV_CACHE_READ = 20, NVFP4_OP_KV_ATTENTION = 21 };
 
 /*
  * Quantizer (Sec. 2.2, Eq. 2; Eq. 12 with target magnitude 6).
@@ -332,6 +334,130 @@ int nvfp4_quantize_for_all_to_all(const void *x_bf16, int64_t T, int64_t H, int6
  */
 int nvfp4_kv_dequant(const nvfp4_tensor *in, void *kv_bf16_out, int64_t T, int64_t H, int64_t d,
                      void *stream);
+
+/*
+ * Norm and rotation of queries and keys, in one pass in front of the cache and the attention below (and of the
+ * all-to-all packer).  For every token t and head h of a tensor, with its own weight w [d],
+ *   y = R_t( w x / sqrt( mean_u(x_u^2) + eps ) ),   x = x[t, h, :],
+ * evaluated in fp32 and rounded once to bf16.  R_t turns pair j (of P = sum of axis_pairs pairs) by the angle
+ *   positions[t, axis of j] * freqs[j]   (radians; the product and the reduction to one turn in fp64),
+ *   (a, b) -> (a cos - b sin, a sin + b cos);
+ * the first axis_pairs[0] pairs go by the first axis, the next by the second, and so on: one axis for text, three (time,
+ * height, width) for video.  interleaved != 0: pair j is the elements (2j, 2j + 1), P <= d / 2.  interleaved == 0: it is
+ * (j, j + P), P a multiple of 8.  Elements from 2P on are not turned.  rope NULL, or P = 0: no rotation.
+ * Magnitudes whose squares leave the fp32 range are outside the contract, as is eps below the normal fp32 numbers (NVFP4_ERR_SHAPE).
+ * A tensor of H heads: element [t, h, u] at t * ld + h * d + u, ld >= H * d a multiple of 8 (queries and keys inside one
+ * row of a fused projection), T tokens; weight NULL: rotated and not normalised.  out may be x itself (same ld).
+ * q or k may be NULL (not both).  d % 16 == 0, d <= 256.
+ */
+#define NVFP4_ROPE_MAX_AXES 4
+#define NVFP4_HEAD_DIM_MAX 256
+typedef struct nvfp4_rope {
+    const int32_t *positions;    /* device, [T, axes] */
+    const float   *freqs;        /* device, [P] */
+    int64_t axes;                /* 0 .. NVFP4_ROPE_MAX_AXES */
+    int64_t axis_pairs[NVFP4_ROPE_MAX_AXES];
+    int32_t interleaved;
+} nvfp4_rope;
+typedef struct nvfp4_heads {
+    const void *x;               /* device, bf16, 16-byte aligned */
+    int64_t     ld;              /* elements from token to token */
+    const void *weight;          /* device, bf16 [d], 16-byte aligned, or NULL */
+    void       *out;             /* device, bf16, 16-byte aligned */
+    int64_t     ld_out;
+    int64_t     H;
+} nvfp4_heads;
+int nvfp4_qk_norm_rope(const nvfp4_heads *q, const nvfp4_heads *k, int64_t T, int64_t d, float eps,
+                       const nvfp4_rope *rope, void *stream);
+
+/*
+ * Backward pass of nvfp4_qk_norm_rope: from the gradient dy of its output and its input x,
+ *   g = R_t^T dy,  r = 1 / sqrt( mean(x^2) + eps ),  xh = r x,
+ *   dx = r ( w g - xh mean(w g xh) ) (bf16, rounded once; g itself without a norm),  dweight = sum over t, h of g xh (fp32).
+ * dweight is deterministic: every workgroup's sum goes through the workspace and they are added in a fixed order.
+ * dweight NULL: not computed (it is not computed for a tensor without weight either).  dx may be dy or x itself.
+ * workspace: nvfp4_workspace_bytes(NVFP4_OP_QK_NORM_ROPE_BACKWARD, T, d, 0) bytes, 16-byte aligned; NULL if neither
+ * tensor wants a dweight.
+ */
+typedef struct nvfp4_heads_grad {
+    const void *dy;  int64_t ld_dy;
+    const void *x;   int64_t ld_x;
+    const void *weight;
+    void       *dx;  int64_t ld_dx;
+    float      *dweight;         /* device, fp32 [d], or NULL */
+    int64_t     H;
+} nvfp4_heads_grad;
+int nvfp4_qk_norm_rope_backward(const nvfp4_heads_grad *q, const nvfp4_heads_grad *k, int64_t T, int64_t d, float eps,
+                                const nvfp4_rope *rope, void *workspace, size_t workspace_bytes, void *stream);
+
+/*
+ * Paged NVFP4 KV cache.  A page holds page_tokens tokens of all H heads, keys and values, in the layout of a quantized
+ * chunk (nvfp4_kv_quant*: rows (token, head), blocks of 16 along d), with a tensor scale of its own, so a page, or a run of
+ * neighbouring pages, can be filled by the chunk quantizers above (a page that all of a latent frame fills, its scale from
+ * the frame's maximum) as well as token by token:
+ *   k_codes, v_codes    [n_pages, page_tokens, H, d/2]    k_scales, v_scales [n_pages, page_tokens, H, d/16]
+ *   k_global, v_global  [n_pages] fp32, positive and finite for every page in use
+ *   k_mean              bf16 [n_pages, page_tokens, H]: row means of smoothed keys (Eq. 6), or NULL: keys are not smoothed
+ * All device memory of the caller.  page_tokens % 16 == 0, d % 16 == 0, d <= 256.  Slot s is token s % page_tokens of page
+ * s / page_tokens.
+ */
+typedef struct nvfp4_kv_cache {
+    uint8_t *k_codes, *k_scales;
+    float   *k_global;
+    void    *k_mean;
+    uint8_t *v_codes, *v_scales;
+    float   *v_global;
+    int64_t  n_pages, page_tokens, H, d;
+} nvfp4_kv_cache;
+
+/*
+ * Quantizes T tokens into the cache: k[t], v[t] (bf16, [T, H, d], rows of ldk / ldv elements from token to token, multiples
+ * of 8) go to slot slots[t] (device, int64), quantized as nvfp4_quantize (scale_search == 0) or nvfp4_quantize_4over6
+ * (scale_search != 0) would with the page's scale as given scale; block scales saturate at 448 where a token exceeds 2688
+ * times the page's scale.  With k_mean keys lose their row mean first, exactly as in nvfp4_kv_quant_k (d / 16 a power of two).
+ * k or v may be NULL: the other alone is written.  Tokens whose slot is negative or not below n_pages * page_tokens are
+ * skipped.  The slots of one call differ from one another: of two tokens with the same slot some blocks of either would stay.
+ */
+int nvfp4_kv_cache_write(const nvfp4_kv_cache *cache, const void *k_bf16, int64_t ldk, const void *v_bf16, int64_t ldv,
+                         const int64_t *slots, int64_t T, int scale_search, void *stream);
+
+/*
+ * Reads T slots back: k_bf16_out, v_bf16_out [T, H, d] (contiguous; either may be NULL) receive
+ * RN_bf16(code * block_scale * global_scale [+ row mean]), rounded once.  Rows of slots outside the cache are left as they were.
+ */
+int nvfp4_kv_cache_read(const nvfp4_kv_cache *cache, const int64_t *slots, int64_t T, void *k_bf16_out, void *v_bf16_out,
+                        void *stream);
+
+/*
+ * Attention over the paged cache, which is read in 4 bits:
+ *   out[i, h, :] = sum_j softmax_j( softmax_scale * q[i, h, :] . K[j, h', :] ) V[j, h', :],   h' = h / (Hq / H),
+ * K and V the exact values that the cache holds (code * block_scale * global_scale [+ row mean]).
+ * B sequences: sequence b has queries q_starts[b] .. q_starts[b+1] - 1 (n_q of them) and kv_lens[b] cached tokens, token j in
+ * page page_table[b, j / page_tokens].  Its query i (from 0) stands at position p = kv_lens[b] - n_q + i when causal (the
+ * queries' own tokens are the last ones of the cache), and at kv_lens[b] - 1 when not (a chunk that sees itself whole); it sees
+ * the tokens j <= p with j > p - window (window 0: no limit) or j < sink.
+ *   q: bf16 [total_q, Hq, d], ldq elements from token to token (a multiple of 8, >= Hq * d); Hq a multiple of the cache's H
+ *   page_table: int32 [B, max_pages], kv_lens: int32 [B], q_starts: int32 [B + 1], all on the device, so that a captured call
+ *     follows them.  Lengths beyond the table and queries beyond total_q are cut off; tokens on a page outside 0 .. n_pages - 1
+ *     are not seen.
+ *   max_q: no sequence has more queries (those of one that has are not computed)
+ *   out: fp32 (NVFP4_OUT_F32) or bf16 (NVFP4_OUT_BF16) [total_q, Hq, d], ldo elements from token to token, rows 16-byte aligned
+ *   lse: fp32 [total_q, Hq], log of the sum of the exponentials (natural), or NULL; what joins this result with attention
+ *     over other tokens
+ * A query that sees nothing gets zeros and lse = -inf.  Rows of out and lse that no sequence owns are left as they were.
+ * Scores, their maxima and sums and the accumulation are fp32; the probabilities enter the second product as f16, relative
+ * to the row's running maximum (2^-11 of each; below 2^-24 of the largest they vanish).
+ * workspace: nvfp4_kv_attention_workspace_bytes() bytes, 16-byte aligned (0 bytes: may be NULL): partial results where the
+ * cache is split over workgroups.
+ */
+int nvfp4_kv_attention(const void *q_bf16, int64_t ldq, int64_t total_q, int64_t Hq, const nvfp4_kv_cache *cache,
+                       const int32_t *page_table, int64_t max_pages, const int32_t *kv_lens, const int32_t *q_starts,
+                       int64_t B, int64_t max_q, float softmax_scale, int causal, int64_t window, int64_t sink,
+                       void *out, int64_t ldo, int out_dtype, float *lse,
+                       void *workspace, size_t workspace_bytes, void *stream);
+/* max_kv = max_pages * page_tokens; 0 where no workspace is needed, and for sizes that the call refuses */
+size_t nvfp4_kv_attention_workspace_bytes(int64_t total_q, int64_t Hq, int64_t H, int64_t d, int64_t max_kv, int64_t B,
+                                          int64_t max_q, int64_t window, int64_t sink);
 
 /* Workspace size in bytes for `op` (NVFP4_OP_*) at the given sizes; 0 on a bad op. */
 size_t nvfp4_workspace_bytes(int op, int64_t a, int64_t b, int64_t c);

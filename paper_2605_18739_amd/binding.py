@@ -31,6 +31,8 @@ KV_MAX_CHUNKS = 64
 NOALLOC_MAX_ELEMENTS = 1 << 32
 OP_QUANTIZE_2D, OP_QUANTIZE_RHT, OP_QUANTIZE_A2A, OP_LORA_DOWN, OP_GEMM_LORA, OP_PROBE = 10, 11, 12, 13, 14, 15
 OP_GEMM_SCALE_OUT = 16
+OP_QK_NORM_ROPE, OP_QK_NORM_ROPE_BACKWARD, OP_KV_CACHE_WRITE, OP_KV_CACHE_READ, OP_KV_ATTENTION = 17, 18, 19, 20, 21
+ROPE_MAX_AXES, HEAD_DIM_MAX = 4, 256
 LORA_RANK = 128
 
 
@@ -41,6 +43,27 @@ class _CTensor(ctypes.Structure):
 
 class _CKvChunk(ctypes.Structure):
     _fields_ = [("q", _CTensor), ("row_mean_bf16", ctypes.c_void_p), ("T", ctypes.c_int64)]
+
+
+class _CRope(ctypes.Structure):
+    _fields_ = [("positions", ctypes.c_void_p), ("freqs", ctypes.c_void_p), ("axes", ctypes.c_int64),
+                ("axis_pairs", ctypes.c_int64 * ROPE_MAX_AXES), ("interleaved", ctypes.c_int32)]
+
+
+class _CHeads(ctypes.Structure):
+    _fields_ = [("x", ctypes.c_void_p), ("ld", ctypes.c_int64), ("weight", ctypes.c_void_p), ("out", ctypes.c_void_p),
+                ("ld_out", ctypes.c_int64), ("H", ctypes.c_int64)]
+
+
+class _CHeadsGrad(ctypes.Structure):
+    _fields_ = [("dy", ctypes.c_void_p), ("ld_dy", ctypes.c_int64), ("x", ctypes.c_void_p), ("ld_x", ctypes.c_int64),
+                ("weight", ctypes.c_void_p), ("dx", ctypes.c_void_p), ("ld_dx", ctypes.c_int64), ("dweight", ctypes.c_void_p), ("H", ctypes.c_int64)]
+
+
+class _CKvCache(ctypes.Structure):
+    _fields_ = [("k_codes", ctypes.c_void_p), ("k_scales", ctypes.c_void_p), ("k_global", ctypes.c_void_p), ("k_mean", ctypes.c_void_p),
+                ("v_codes", ctypes.c_void_p), ("v_scales", ctypes.c_void_p), ("v_global", ctypes.c_void_p),
+                ("n_pages", ctypes.c_int64), ("page_tokens", ctypes.c_int64), ("H", ctypes.c_int64), ("d", ctypes.c_int64)]
 
 
 class NVFP4Error(RuntimeError):
@@ -90,6 +113,19 @@ def lib():
         L.nvfp4_kv_quant_k.argtypes = [vp, i64, i64, i64, tp, vp, vp, sz, vp]
         L.nvfp4_kv_dequant_gather.restype = c.c_int
         L.nvfp4_kv_dequant_gather.argtypes = [c.POINTER(_CKvChunk), c.c_int, vp, i64, i64, vp]
+        L.nvfp4_qk_norm_rope.restype = c.c_int
+        L.nvfp4_qk_norm_rope.argtypes = [c.POINTER(_CHeads), c.POINTER(_CHeads), i64, i64, c.c_float, c.POINTER(_CRope), vp]
+        L.nvfp4_qk_norm_rope_backward.restype = c.c_int
+        L.nvfp4_qk_norm_rope_backward.argtypes = [c.POINTER(_CHeadsGrad), c.POINTER(_CHeadsGrad), i64, i64, c.c_float, c.POINTER(_CRope), vp, sz, vp]
+        L.nvfp4_kv_cache_write.restype = c.c_int
+        L.nvfp4_kv_cache_write.argtypes = [c.POINTER(_CKvCache), vp, i64, vp, i64, vp, i64, c.c_int, vp]
+        L.nvfp4_kv_cache_read.restype = c.c_int
+        L.nvfp4_kv_cache_read.argtypes = [c.POINTER(_CKvCache), vp, i64, vp, vp, vp]
+        L.nvfp4_kv_attention.restype = c.c_int
+        L.nvfp4_kv_attention.argtypes = [vp, i64, i64, i64, c.POINTER(_CKvCache), vp, i64, vp, vp, i64, i64, c.c_float, c.c_int, i64, i64,
+                                         vp, i64, c.c_int, vp, vp, sz, vp]
+        L.nvfp4_kv_attention_workspace_bytes.restype = sz
+        L.nvfp4_kv_attention_workspace_bytes.argtypes = [i64] * 9
         L.nvfp4_workspace_bytes.restype = sz
         L.nvfp4_workspace_bytes.argtypes = [c.c_int, i64, i64, i64]
         L.nvfp4_status_string.restype = c.c_char_p
@@ -162,7 +198,7 @@ def _on(stream, call, *args):
     here = torch.cuda.current_stream(stream.device)
     with torch.cuda.stream(stream):
         result = call(*args)
-    for new in result if isinstance(result, tuple) else (result,):
+    for new in result if isinstance(result, tuple) else () if isinstance(result, NVFP4KvCache) else (result,):
         if new is not None and not any(new is a for a in args):
             for t in (new.codes, new.scales, new.global_scale) if isinstance(new, NVFP4Tensor) else (new,):
                 t.record_stream(here)
@@ -396,6 +432,126 @@ def nvfp4_kv_dequant(q, T, H, d, out=None, stream=None):
         out = torch.empty((T, H, d), dtype=torch.bfloat16, device=q.codes.device)
     _check(_host().kv_dequant(q, T, H, d, out, _stream(stream)))
     return out
+
+
+class NVFP4Rope:
+    """Rotation of queries and keys: positions int32 [T, axes], freqs fp32 [pairs] (radians per position of each pair),
+    axis_pairs the number of pairs that go by each axis, in order (one axis for text; time, height, width for video).
+    interleaved: pairs of neighbours (2j, 2j + 1), else halves (j, j + pairs)."""
+
+    def __init__(self, positions, freqs, axis_pairs, interleaved=True):
+        self.positions, self.freqs = positions, freqs
+        self.axis_pairs, self.interleaved = tuple(int(n) for n in axis_pairs), bool(interleaved)
+
+    def _native(self):
+        return self.positions, self.freqs, self.axis_pairs, self.interleaved
+
+
+def nvfp4_qk_norm_rope(q, k, q_weight, k_weight, rope, eps=1e-6, q_out=None, k_out=None, stream=None):
+    """q [T, Hq, d], k [T, Hk, d] bf16 (contiguous heads, any token stride; either may be None): RMS norm of each head with
+    weights bf16 [d] (None: rotated only), then the rotation (an NVFP4Rope, or None).  q_out, k_out may be q and k.  Returns (q_out, k_out)."""
+    if stream is not None and _elsewhere(stream):
+        return _on(stream, nvfp4_qk_norm_rope, q, k, q_weight, k_weight, rope, eps, q_out, k_out)
+    if q is not None and q_out is None:
+        q_out = torch.empty(q.shape, dtype=torch.bfloat16, device=q.device)
+    if k is not None and k_out is None:
+        k_out = torch.empty(k.shape, dtype=torch.bfloat16, device=k.device)
+    _check(_host().qk_norm_rope(q, k, q_weight, k_weight, rope and rope._native(), eps, q_out, k_out, _stream(stream)))
+    return q_out, k_out
+
+
+def nvfp4_qk_norm_rope_backward(dq, dk, q, k, q_weight, k_weight, rope, eps=1e-6, dq_in=None, dk_in=None, dq_weight=None, dk_weight=None,
+                                weight_grads=True, workspace=None, stream=None):
+    """Gradients of nvfp4_qk_norm_rope from those of its outputs (dq, dk) and its inputs.  Returns (dq_in, dk_in, dq_weight,
+    dk_weight): bf16 like dq and dk, and fp32 [d] (None without a weight, or with weight_grads=False)."""
+    if stream is not None and _elsewhere(stream):
+        return _on(stream, nvfp4_qk_norm_rope_backward, dq, dk, q, k, q_weight, k_weight, rope, eps, dq_in, dk_in, dq_weight, dk_weight, weight_grads, workspace)
+    if dq is not None and dq_in is None:
+        dq_in = torch.empty(dq.shape, dtype=torch.bfloat16, device=dq.device)
+    if dk is not None and dk_in is None:
+        dk_in = torch.empty(dk.shape, dtype=torch.bfloat16, device=dk.device)
+    if weight_grads and dq is not None and q_weight is not None and dq_weight is None:
+        dq_weight = torch.empty(q_weight.shape, dtype=torch.float32, device=dq.device)
+    if weight_grads and dk is not None and k_weight is not None and dk_weight is None:
+        dk_weight = torch.empty(k_weight.shape, dtype=torch.float32, device=dk.device)
+    _check(_host().qk_norm_rope_backward(dq, dk, q, k, q_weight, k_weight, rope and rope._native(), eps, dq_in, dk_in, dq_weight, dk_weight,
+                                         workspace, _stream(stream)))
+    return dq_in, dk_in, dq_weight, dk_weight
+
+
+class NVFP4KvCache:
+    """Paged NVFP4 cache (see include/nvfp4.h): codes u8 [n_pages, page_tokens, H, d/2], scales u8 [n_pages, page_tokens, H, d/16],
+    tensor scales fp32 [n_pages], and for smoothed keys the row means bf16 [n_pages, page_tokens, H]."""
+
+    def __init__(self, k_codes, k_scales, k_global, v_codes, v_scales, v_global, k_mean=None):
+        if k_codes.dim() != 4:
+            raise _wrong_rank(k_codes, 4)
+        n, p, H, half = k_codes.shape
+        for name, t, shape, dtype in (("k_codes", k_codes, (n, p, H, half), torch.uint8), ("k_scales", k_scales, (n, p, H, half // 8), torch.uint8),
+                                      ("k_global", k_global, (n,), torch.float32), ("v_codes", v_codes, (n, p, H, half), torch.uint8),
+                                      ("v_scales", v_scales, (n, p, H, half // 8), torch.uint8), ("v_global", v_global, (n,), torch.float32),
+                                      ("k_mean", k_mean, (n, p, H), torch.bfloat16)):
+            if t is None and name == "k_mean":
+                continue
+            assert t.dtype == dtype and tuple(t.shape) == shape and t.is_contiguous(), f"{name}: expected a contiguous {dtype} tensor {shape}"
+        self.k_codes, self.k_scales, self.k_global, self.k_mean = k_codes, k_scales, k_global, k_mean
+        self.v_codes, self.v_scales, self.v_global = v_codes, v_scales, v_global
+        self.n_pages, self.page_tokens, self.H, self.d = n, p, H, 2 * half
+        self._native = (k_codes, k_scales, k_global, k_mean, v_codes, v_scales, v_global)
+
+    @staticmethod
+    def empty(n_pages, page_tokens, H, d, smooth=False, device="cuda"):
+        """A cache without contents: codes and scales of zero, tensor scales of one."""
+        planes = [torch.zeros((n_pages, page_tokens, H, w), dtype=torch.uint8, device=device) for w in (d // 2, d // 16) * 2]
+        k_global, v_global = (torch.ones(n_pages, dtype=torch.float32, device=device) for _ in range(2))
+        mean = torch.zeros((n_pages, page_tokens, H), dtype=torch.bfloat16, device=device) if smooth else None
+        return NVFP4KvCache(planes[0], planes[1], k_global, planes[2], planes[3], v_global, mean)
+
+    def page(self, i):
+        """(keys, row means or None, values) of page i as NVFP4Tensors on the cache's memory: what the chunk quantizers take as `out`."""
+        rows = self.page_tokens * self.H
+        k = NVFP4Tensor(rows, self.d, None, self.k_codes[i].view(rows, -1), self.k_scales[i].view(rows, -1), self.k_global[i:i + 1])
+        v = NVFP4Tensor(rows, self.d, None, self.v_codes[i].view(rows, -1), self.v_scales[i].view(rows, -1), self.v_global[i:i + 1])
+        return k, None if self.k_mean is None else self.k_mean[i].view(rows), v
+
+
+def nvfp4_kv_cache_write(cache, k, v, slots, scale_search=False, stream=None):
+    """Quantizes k, v (bf16 [T, H, d], contiguous heads, any token stride; either may be None) into the slots (int64 [T]) of the cache."""
+    if stream is not None and _elsewhere(stream):
+        return _on(stream, nvfp4_kv_cache_write, cache, k, v, slots, scale_search)
+    _check(_host().kv_cache_write(cache._native, k, v, slots, 1 if scale_search else 0, _stream(stream)))
+    return cache
+
+
+def nvfp4_kv_cache_read(cache, slots, k_out=None, v_out=None, stream=None):
+    """Slots (int64 [T]) back to bf16 [T, H, d].  Returns (k_out, v_out); with one of the two given, the other is not read (None)."""
+    if stream is not None and _elsewhere(stream):
+        return _on(stream, nvfp4_kv_cache_read, cache, slots, k_out, v_out)
+    if k_out is None and v_out is None:
+        k_out, v_out = (torch.empty((slots.shape[0], cache.H, cache.d), dtype=torch.bfloat16, device=slots.device) for _ in range(2))
+    _check(_host().kv_cache_read(cache._native, slots, k_out, v_out, _stream(stream)))
+    return k_out, v_out
+
+
+def nvfp4_kv_attention_workspace_bytes(total_q, Hq, H, d, max_kv, B, max_q, window=0, sink=0):
+    return int(lib().nvfp4_kv_attention_workspace_bytes(total_q, Hq, H, d, max_kv, B, max_q, window, sink))
+
+
+def nvfp4_kv_attention(q, cache, page_table, kv_lens, q_starts, max_q, softmax_scale=None, causal=False, window=0, sink=0, out_dtype=OUT_BF16,
+                       out=None, lse=None, workspace=None, stream=None):
+    """Attention of q (bf16 [total_q, Hq, d], contiguous heads, any token stride) over the cache: page_table int32 [B, max_pages],
+    kv_lens int32 [B], q_starts int32 [B + 1]; softmax_scale d ** -0.5 by default.  Returns (out [total_q, Hq, d], lse fp32 [total_q, Hq])."""
+    if stream is not None and _elsewhere(stream):
+        return _on(stream, nvfp4_kv_attention, q, cache, page_table, kv_lens, q_starts, max_q, softmax_scale, causal, window, sink, out_dtype, out, lse, workspace)
+    if q.dim() != 3:
+        raise _wrong_rank(q, 3)
+    if out is None:
+        out = torch.empty(q.shape, dtype=torch.float32 if out_dtype == OUT_F32 else torch.bfloat16, device=q.device)
+    if lse is None:
+        lse = torch.empty(q.shape[:2], dtype=torch.float32, device=q.device)
+    _check(_host().kv_attention(q, cache._native, page_table, kv_lens, q_starts, max_q, cache.d ** -0.5 if softmax_scale is None else softmax_scale,
+                                1 if causal else 0, window, sink, out_dtype, out, lse, workspace, _stream(stream)))
+    return out, lse
 
 
 def nvfp4_gemm_plan(M, N, K):

@@ -2,9 +2,11 @@
 // carving, kernel launches on the caller's stream.  See include/nvfp4.h for the
 // contract of every entry point.
 #include "../../include/nvfp4.h"
+#include "nvfp4_attention_plan.h"
 #include "nvfp4_kernels.h"
 
 #include <algorithm>
+#include <cmath>
 #include <mutex>
 #include <vector>
 
@@ -130,6 +132,110 @@ int check_gemm(const nvfp4_tensor *A, const nvfp4_tensor *W)
     if (int rc = check_tensor(W)) return rc;
     if (A->K != W->K) return NVFP4_ERR_SHAPE;
     return NVFP4_OK;
+}
+
+// ---- norm and rotation, paged cache, attention ---------------------------------------------------------------
+static_assert(kRopeMaxAxes == NVFP4_ROPE_MAX_AXES);
+inline bool aligned(const void *p, size_t bytes) { return (reinterpret_cast<uintptr_t>(p) & (bytes - 1)) == 0; }
+constexpr int64_t kMaxIndex = 1ll << 30;                       // tokens, rows and units that kernels count in 32 bits
+constexpr int64_t kMaxRow = 1ll << 24;                         // elements of a token (all heads)
+
+bool head_size_ok(int64_t H, int64_t d)
+{
+    return H > 0 && d > 0 && (d & 15) == 0 && d <= NVFP4_HEAD_DIM_MAX && H <= kMaxRow / d;
+}
+// rows of H heads of d elements, ld elements apart
+bool row_stride_ok(int64_t ld, int64_t H, int64_t d) { return ld >= H * d && ld <= (1ll << 32); }
+
+int fill_rope(const nvfp4_rope *rope, int64_t d, NormRopeArgs *a)
+{
+    for (int &s : a->axis_start) s = 0x7FFFFFFF;
+    if (!rope) return NVFP4_OK;
+    if (rope->axes < 0 || rope->axes > NVFP4_ROPE_MAX_AXES) return NVFP4_ERR_SHAPE;
+    int64_t P = 0;
+    for (int x = 0; x < (int)rope->axes; ++x) {
+        if (rope->axis_pairs[x] < 0 || rope->axis_pairs[x] > d) return NVFP4_ERR_SHAPE;
+        a->axis_start[x] = (int)P;
+        P += rope->axis_pairs[x];
+    }
+    if (2 * P > d || (!rope->interleaved && (P & 7) != 0)) return NVFP4_ERR_SHAPE;
+    if (P == 0) return NVFP4_OK;
+    if (!rope->positions || !rope->freqs) return NVFP4_ERR_NULL;
+    if (!aligned(rope->positions, 4) || !aligned(rope->freqs, 4)) return NVFP4_ERR_ALIGN;
+    a->positions = rope->positions;
+    a->freqs = rope->freqs;
+    a->axes = (int)rope->axes;
+    a->pairs = (int)P;
+    a->interleaved = rope->interleaved != 0;
+    return NVFP4_OK;
+}
+int fill_norm(int64_t T, int64_t d, float eps, bool normed, NormRopeArgs *a)
+{
+    if (T <= 0 || T > kMaxIndex) return NVFP4_ERR_SHAPE;
+    if (normed && !(std::isnormal(eps) && eps > 0.0f)) return NVFP4_ERR_SHAPE;
+    a->d = (int)d;
+    a->eps = eps;
+    return NVFP4_OK;
+}
+int fill_heads(const nvfp4_heads *h, int64_t d, NormRopeTensor *t)
+{
+    if (!h) return NVFP4_OK;
+    if (!h->x || !h->out) return NVFP4_ERR_NULL;
+    if (!head_size_ok(h->H, d) || !row_stride_ok(h->ld, h->H, d) || !row_stride_ok(h->ld_out, h->H, d)) return NVFP4_ERR_SHAPE;
+    if (!aligned16(h->x) || !aligned16(h->out) || !aligned16(h->weight) || (h->ld & 7) != 0 || (h->ld_out & 7) != 0) return NVFP4_ERR_ALIGN;
+    t->x = static_cast<const uint16_t *>(h->x);
+    t->weight = static_cast<const uint16_t *>(h->weight);
+    t->out = static_cast<uint16_t *>(h->out);
+    t->ld = h->ld;
+    t->ld_out = h->ld_out;
+    t->H = (int)h->H;
+    return NVFP4_OK;
+}
+int fill_heads_grad(const nvfp4_heads_grad *h, int64_t d, NormRopeTensor *t, float **dweight)
+{
+    *dweight = nullptr;
+    if (!h) return NVFP4_OK;
+    if (!h->dy || !h->dx || (h->weight && !h->x)) return NVFP4_ERR_NULL;
+    if (!head_size_ok(h->H, d) || !row_stride_ok(h->ld_dy, h->H, d) || !row_stride_ok(h->ld_dx, h->H, d)) return NVFP4_ERR_SHAPE;
+    if (h->weight && !row_stride_ok(h->ld_x, h->H, d)) return NVFP4_ERR_SHAPE;
+    if (!aligned16(h->dy) || !aligned16(h->dx) || (h->ld_dy & 7) != 0 || (h->ld_dx & 7) != 0) return NVFP4_ERR_ALIGN;
+    if (h->weight && (!aligned16(h->x) || !aligned16(h->weight) || (h->ld_x & 7) != 0 || !aligned(h->dweight, 4))) return NVFP4_ERR_ALIGN;
+    t->x = static_cast<const uint16_t *>(h->x);
+    t->dy = static_cast<const uint16_t *>(h->dy);
+    t->weight = static_cast<const uint16_t *>(h->weight);
+    t->out = static_cast<uint16_t *>(h->dx);
+    t->ld = h->ld_x;
+    t->ld_dy = h->ld_dy;
+    t->ld_out = h->ld_dx;
+    t->H = (int)h->H;
+    if (h->weight) *dweight = h->dweight;
+    return NVFP4_OK;
+}
+
+int fill_pages(const nvfp4_kv_cache *c, KvPages *p)
+{
+    if (!c || !c->k_codes || !c->k_scales || !c->k_global || !c->v_codes || !c->v_scales || !c->v_global) return NVFP4_ERR_NULL;
+    if (!head_size_ok(c->H, c->d) || c->n_pages <= 0 || c->n_pages > 0x7FFFFFFF || c->page_tokens <= 0 ||
+        c->page_tokens > kMaxIndex || (c->page_tokens & 15) != 0 || c->n_pages > (1ll << 36) / c->page_tokens)
+        return NVFP4_ERR_SHAPE;
+    if (!aligned16(c->k_codes) || !aligned16(c->k_scales) || !aligned16(c->v_codes) || !aligned16(c->v_scales) ||
+        !aligned(c->k_global, 4) || !aligned(c->v_global, 4) || !aligned(c->k_mean, 2))
+        return NVFP4_ERR_ALIGN;
+    *p = KvPages{c->k_codes, c->k_scales, c->v_codes, c->v_scales, c->k_global, c->v_global, static_cast<uint16_t *>(c->k_mean),
+                 c->n_pages, c->page_tokens, (int)c->H, (int)c->d};
+    return NVFP4_OK;
+}
+
+// sizes of an attention call that its kernels and its workspace go by
+bool attention_sizes_ok(int64_t total_q, int64_t Hq, int64_t H, int64_t d, int64_t max_kv, int64_t B, int64_t max_q)
+{
+    return head_size_ok(H, d) && head_size_ok(Hq, d) && Hq % H == 0 && total_q > 0 && total_q <= kMaxIndex && total_q <= kMaxIndex / Hq &&
+           max_kv > 0 && max_kv <= kMaxIndex && B > 0 && B <= kMaxIndex && max_q > 0 && max_q <= total_q && max_q <= kMaxIndex / Hq &&
+           B <= kMaxIndex / (max_q * Hq);
+}
+bool attention_grid_ok(const AttentionPlan &p, int64_t H, int64_t B)
+{
+    return B * H <= 0x7FFFFFFF / p.pieces && B * H * p.pieces <= 0x7FFFFFFF / p.groups;
 }
 
 }  // namespace
@@ -510,6 +616,132 @@ int nvfp4_gemm_act_quant(const nvfp4_tensor *A, const nvfp4_tensor *W, int act,
     return e == hipSuccess ? NVFP4_OK : NVFP4_ERR_LAUNCH;
 }
 
+int nvfp4_qk_norm_rope(const nvfp4_heads *q, const nvfp4_heads *k, int64_t T, int64_t d, float eps, const nvfp4_rope *rope,
+                       void *stream)
+{
+    if (!q && !k) return NVFP4_ERR_NULL;
+    NormRopeArgs a;
+    if (int rc = fill_heads(q, d, &a.q)) return rc;
+    if (int rc = fill_heads(k, d, &a.k)) return rc;
+    if (int rc = fill_norm(T, d, eps, a.q.weight || a.k.weight, &a)) return rc;
+    if (int rc = fill_rope(rope, d, &a)) return rc;
+    std::lock_guard<std::mutex> lk(g_mu);
+    hipStream_t s = static_cast<hipStream_t>(stream);
+    Timed t(s, NVFP4_OP_QK_NORM_ROPE);
+    return launch_norm_rope(a, T, s) == hipSuccess ? NVFP4_OK : NVFP4_ERR_LAUNCH;
+}
+
+int nvfp4_qk_norm_rope_backward(const nvfp4_heads_grad *q, const nvfp4_heads_grad *k, int64_t T, int64_t d, float eps,
+                                const nvfp4_rope *rope, void *workspace, size_t workspace_bytes, void *stream)
+{
+    if (!q && !k) return NVFP4_ERR_NULL;
+    NormRopeArgs a;
+    float *dwq, *dwk;
+    if (int rc = fill_heads_grad(q, d, &a.q, &dwq)) return rc;
+    if (int rc = fill_heads_grad(k, d, &a.k, &dwk)) return rc;
+    if (int rc = fill_norm(T, d, eps, a.q.weight || a.k.weight, &a)) return rc;
+    if (int rc = fill_rope(rope, d, &a)) return rc;
+    if (dwq || dwk) {
+        if (!workspace || workspace_bytes < norm_rope_workspace_bytes(T, d)) return NVFP4_ERR_WORKSPACE;
+        if (!aligned16(workspace)) return NVFP4_ERR_ALIGN;
+    }
+    std::lock_guard<std::mutex> lk(g_mu);
+    hipStream_t s = static_cast<hipStream_t>(stream);
+    Timed t(s, NVFP4_OP_QK_NORM_ROPE_BACKWARD);
+    return launch_norm_rope_backward(a, T, dwq, dwk, static_cast<float *>(workspace), s) == hipSuccess ? NVFP4_OK : NVFP4_ERR_LAUNCH;
+}
+
+int nvfp4_kv_cache_write(const nvfp4_kv_cache *cache, const void *k_bf16, int64_t ldk, const void *v_bf16, int64_t ldv,
+                         const int64_t *slots, int64_t T, int scale_search, void *stream)
+{
+    if ((!k_bf16 && !v_bf16) || !slots) return NVFP4_ERR_NULL;
+    KvPages c;
+    if (int rc = fill_pages(cache, &c)) return rc;
+    const int64_t nb = c.d >> 4, parts = (c.H * nb + 63) / 64;
+    if (T <= 0 || T > kMaxIndex / (2 * parts)) return NVFP4_ERR_SHAPE;
+    if ((k_bf16 && !row_stride_ok(ldk, c.H, c.d)) || (v_bf16 && !row_stride_ok(ldv, c.H, c.d))) return NVFP4_ERR_SHAPE;
+    if (k_bf16 && c.k_mean && (nb & (nb - 1)) != 0) return NVFP4_ERR_SHAPE;       // the lanes of a row reduce by shuffles
+    if (!aligned16(k_bf16) || !aligned16(v_bf16) || (k_bf16 && (ldk & 7) != 0) || (v_bf16 && (ldv & 7) != 0) || !aligned(slots, 8))
+        return NVFP4_ERR_ALIGN;
+    std::lock_guard<std::mutex> lk(g_mu);
+    hipStream_t s = static_cast<hipStream_t>(stream);
+    Timed t(s, NVFP4_OP_KV_CACHE_WRITE);
+    hipError_t e = launch_kv_cache_write(c, static_cast<const uint16_t *>(k_bf16), ldk, static_cast<const uint16_t *>(v_bf16), ldv, slots, T,
+                                         scale_search != 0, s);
+    return e == hipSuccess ? NVFP4_OK : NVFP4_ERR_LAUNCH;
+}
+
+int nvfp4_kv_cache_read(const nvfp4_kv_cache *cache, const int64_t *slots, int64_t T, void *k_bf16_out, void *v_bf16_out,
+                        void *stream)
+{
+    if ((!k_bf16_out && !v_bf16_out) || !slots) return NVFP4_ERR_NULL;
+    KvPages c;
+    if (int rc = fill_pages(cache, &c)) return rc;
+    if (T <= 0 || T > kMaxIndex / (2 * ((c.H * (c.d >> 3) + 63) / 64))) return NVFP4_ERR_SHAPE;
+    if (!aligned16(k_bf16_out) || !aligned16(v_bf16_out) || !aligned(slots, 8)) return NVFP4_ERR_ALIGN;
+    std::lock_guard<std::mutex> lk(g_mu);
+    hipStream_t s = static_cast<hipStream_t>(stream);
+    Timed t(s, NVFP4_OP_KV_CACHE_READ);
+    hipError_t e = launch_kv_cache_read(c, slots, T, static_cast<uint16_t *>(k_bf16_out), static_cast<uint16_t *>(v_bf16_out), s);
+    return e == hipSuccess ? NVFP4_OK : NVFP4_ERR_LAUNCH;
+}
+
+int nvfp4_kv_attention(const void *q_bf16, int64_t ldq, int64_t total_q, int64_t Hq, const nvfp4_kv_cache *cache,
+                       const int32_t *page_table, int64_t max_pages, const int32_t *kv_lens, const int32_t *q_starts, int64_t B,
+                       int64_t max_q, float softmax_scale, int causal, int64_t window, int64_t sink, void *out, int64_t ldo,
+                       int out_dtype, float *lse, void *workspace, size_t workspace_bytes, void *stream)
+{
+    if (!q_bf16 || !page_table || !kv_lens || !q_starts || !out) return NVFP4_ERR_NULL;
+    KvAttention a{};
+    if (int rc = fill_pages(cache, &a.cache)) return rc;
+    const int64_t H = a.cache.H, d = a.cache.d;
+    if (max_pages <= 0 || max_pages > kMaxIndex / a.cache.page_tokens) return NVFP4_ERR_SHAPE;
+    const int64_t max_kv = max_pages * a.cache.page_tokens;
+    max_q = std::min(max_q, total_q);
+    if (!attention_sizes_ok(total_q, Hq, H, d, max_kv, B, max_q)) return NVFP4_ERR_SHAPE;
+    if (!row_stride_ok(ldq, Hq, d) || !row_stride_ok(ldo, Hq, d) || window < 0 || sink < 0) return NVFP4_ERR_SHAPE;
+    if (!(softmax_scale > 0.0f) || !std::isfinite(softmax_scale)) return NVFP4_ERR_SHAPE;
+    if (out_dtype != NVFP4_OUT_F32 && out_dtype != NVFP4_OUT_BF16) return NVFP4_ERR_SHAPE;
+    if (!aligned16(q_bf16) || !aligned16(out) || (ldq & 7) != 0 || (ldo & (out_dtype == NVFP4_OUT_BF16 ? 7 : 3)) != 0 ||
+        !aligned(page_table, 4) || !aligned(kv_lens, 4) || !aligned(q_starts, 4) || !aligned(lse, 4))
+        return NVFP4_ERR_ALIGN;
+    const AttentionPlan plan = attention_plan(Hq, H, d, max_kv, B, max_q, window, sink);
+    if (!attention_grid_ok(plan, H, B)) return NVFP4_ERR_SHAPE;
+    const size_t need = attention_workspace_bytes(plan, total_q, Hq, d);
+    if (need > 0 && (!workspace || workspace_bytes < need)) return NVFP4_ERR_WORKSPACE;
+    if (need > 0 && !aligned16(workspace)) return NVFP4_ERR_ALIGN;
+    a.q = static_cast<const uint16_t *>(q_bf16);
+    a.ldq = ldq;
+    a.total_q = total_q;
+    a.Hq = Hq;
+    a.page_table = page_table;
+    a.kv_lens = kv_lens;
+    a.q_starts = q_starts;
+    a.max_pages = max_pages;
+    a.B = B;
+    a.max_q = max_q;
+    a.softmax_scale = softmax_scale;
+    a.causal = causal != 0;
+    a.window = window;
+    a.sink = sink;
+    a.out = out;
+    a.ldo = ldo;
+    a.out_f32 = out_dtype == NVFP4_OUT_F32;
+    a.lse = lse;
+    std::lock_guard<std::mutex> lk(g_mu);
+    hipStream_t s = static_cast<hipStream_t>(stream);
+    Timed t(s, NVFP4_OP_KV_ATTENTION);
+    return launch_kv_attention(a, workspace, s) == hipSuccess ? NVFP4_OK : NVFP4_ERR_LAUNCH;
+}
+
+size_t nvfp4_kv_attention_workspace_bytes(int64_t total_q, int64_t Hq, int64_t H, int64_t d, int64_t max_kv, int64_t B, int64_t max_q,
+                                          int64_t window, int64_t sink)
+{
+    max_q = std::min(max_q, total_q);
+    if (!attention_sizes_ok(total_q, Hq, H, d, max_kv, B, max_q) || window < 0 || sink < 0) return 0;
+    return attention_workspace_bytes(attention_plan(Hq, H, d, max_kv, B, max_q, window, sink), total_q, Hq, d);
+}
+
 size_t nvfp4_workspace_bytes(int op, int64_t a, int64_t b, int64_t c)
 {
     switch (op) {
@@ -524,6 +756,8 @@ size_t nvfp4_workspace_bytes(int op, int64_t a, int64_t b, int64_t c)
         return kPartialBytes;
     case NVFP4_OP_QUANTIZE_RHT:       // a = R, b = C
         return kPartialBytes + ((a > 0 && b > 0) ? rht_inexact_bytes(a, b) : 0);
+    case NVFP4_OP_QK_NORM_ROPE_BACKWARD:   // a = T, b = d
+        return a > 0 && b > 0 && b <= NVFP4_HEAD_DIM_MAX ? norm_rope_workspace_bytes(a, b) : 0;
     case NVFP4_OP_LORA_DOWN:          // a = M, b = K
         if (a <= 0 || b <= 0) return 0;
         return lora_down_workspace_bytes(a, b);

@@ -1,0 +1,121 @@
+// What the two attention kernels share: which tokens a sequence's queries see, the values of a tile's page, the running
+// maximum, and how partial results are laid out.
+#pragma once
+
+#include "nvfp4_attention_plan.h"
+#include "nvfp4_device.h"
+#include "nvfp4_kernels.h"
+
+namespace nvfp4 {
+
+struct AttentionArgs {
+    const uint16_t *q;
+    int64_t ldq, ldo;
+    int32_t total_q, Hq, H, G, d, n_pages, page_tokens, max_pages, B, max_q;      // G: query heads of a cached head
+    const uint8_t *k_codes, *k_scales, *v_codes, *v_scales;
+    const uint16_t *k_mean;
+    float scale;                          // softmax scale times log2(e): scores are exponents of two
+    int32_t causal, window, sink;
+    void *out;
+    float *lse;
+    AttentionPlan plan;
+    float *part_o;                        // [piece][total_q * Hq][d], partial sums relative to ...
+    float2 *part_ml;                      // [piece][total_q * Hq] their row's maximum (base 2) and sum
+    Divisor by_page;
+};
+
+// Queries and cached tokens of a sequence (clamped to what the call describes), and the steps of kStep tokens that some
+// query among i0 .. i1 sees: sink_steps steps from token 0, then those from lo_step on.
+struct Sequence {
+    int start, n_q, len, p0;              // p0: position of query 0; query i stands at p0 + i (causal) or p0
+    __device__ __forceinline__ Sequence(const AttentionArgs &a, const int32_t *__restrict__ q_starts, const int32_t *__restrict__ kv_lens, int b)
+    {
+        start = min(max(q_starts[b], 0), a.total_q);
+        n_q = min(max(q_starts[b + 1], start), a.total_q) - start;
+        len = min(max(kv_lens[b], 0), a.max_pages * a.page_tokens);
+        p0 = a.causal ? len - n_q : len - 1;
+    }
+    __device__ __forceinline__ int position(const AttentionArgs &a, int i) const { return a.causal ? p0 + i : p0; }
+};
+struct Steps {
+    int sink_steps, lo_step, total;
+    __device__ __forceinline__ Steps(const AttentionArgs &a, const Sequence &q, int i0, int i1, int step_tokens)
+    {
+        const int hi = q.position(a, i1) + 1;                                    // (at most q.len)
+        const int lo = a.window > 0 ? max(q.position(a, i0) - a.window + 1, 0) : 0;
+        lo_step = lo / step_tokens;
+        const int hi_step = hi > 0 ? (hi + step_tokens - 1) / step_tokens : 0;
+        sink_steps = a.window > 0 && hi > 0 ? min((min(a.sink, hi) + step_tokens - 1) / step_tokens, lo_step) : 0;
+        total = sink_steps + max(hi_step - lo_step, 0);
+    }
+    __device__ __forceinline__ int first_token(int n, int step_tokens) const { return (n < sink_steps ? n : n - sink_steps + lo_step) * step_tokens; }
+};
+
+// The page of a group of 16 tokens (pages hold whole groups): slot of the group's first token, or none.
+__device__ __forceinline__ int page_of(const AttentionArgs &a, const int32_t *__restrict__ page_table, int b, int token, int &offset)
+{
+    const int at = (int)(a.by_page.m ? a.by_page.small((uint32_t)token) : (uint32_t)token / (uint32_t)a.page_tokens);
+    offset = token - at * a.page_tokens;
+    const int page = page_table[(int64_t)b * a.max_pages + at];
+    return (uint32_t)page < (uint32_t)a.n_pages ? page : -1;
+}
+
+__device__ __forceinline__ bool seen(const AttentionArgs &a, int j, int p)
+{
+    return (j <= p) & ((a.window == 0) | (j > p - a.window) | (j < a.sink));
+}
+
+// A token's weight is 2^(s + log2 g_v - m): with its page's value scale g_v in the exponent the values enter the product
+// as code * block scale, exact in f16, and the sum of the weights takes the factor out again (weight / g_v).
+// m is the row's running maximum of s + log2 g_v, raised only when a score exceeds it by kSlack binades: weights of up to
+// 2^kSlack are as good in f16 as those up to one, and most steps then need no reduction between lanes and no rescaling.
+constexpr float kSlack = 8.0f, kLowest = -3.0e38f;      // (kLowest: below every score, and 2^(-inf - kLowest) is still 0)
+
+// E4M3 bytes in the low halves of two 16-bit lanes -> f16 values times 2^-8, exact (subnormal f16 where the byte is
+// below 2^-6), for every byte: sign bit dropped, no NaN, so slots that were never written cannot reach a sum.
+__device__ __forceinline__ half2v scale_pair(uint32_t b) { return __builtin_bit_cast(half2v, (b & 0x007F007Fu) << 7); }
+// two codes -> f16 times 2^8; times a scale from scale_pair: code * block scale
+template <int BYTE>
+__device__ __forceinline__ half2v code_pair(uint32_t w) { return __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(w, 256.0f, BYTE); }
+
+__device__ __forceinline__ half8v join8(half2v a, half2v b, half2v c, half2v d)
+{
+    return half8v{a.x, a.y, b.x, b.y, c.x, c.y, d.x, d.y};
+}
+// eight codes along a row (one word) times one scale
+__device__ __forceinline__ half8v eight_codes(uint32_t w, half2v s)
+{
+    return join8(code_pair<0>(w) * s, code_pair<1>(w) * s, code_pair<2>(w) * s, code_pair<3>(w) * s);
+}
+
+// bf16 queries -> f16 times a power of two that puts the row's largest magnitude into [2^14, 2^15): exact but for elements
+// 2^-29 of it and less.  Returns the factor's inverse for the scores.
+__device__ __forceinline__ int row_exponent(float amax) { return amax > 0.0f ? min(max(15 - __builtin_amdgcn_frexp_expf(amax), -110), 110) : 0; }
+__device__ __forceinline__ half8v query_pairs(uint4v w, int e)
+{
+    half8v r;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        r[2 * i] = (_Float16)__builtin_amdgcn_ldexpf(bf16lo_to_f32(w[i]), e);
+        r[2 * i + 1] = (_Float16)__builtin_amdgcn_ldexpf(bf16hi_to_f32(w[i]), e);
+    }
+    return r;
+}
+__device__ __forceinline__ float absmax8(uint4v w, float m)
+{
+#pragma unroll
+    for (int i = 0; i < 4; ++i) m = fmaxf(fmaxf(m, fabsf(bf16lo_to_f32(w[i]))), fabsf(bf16hi_to_f32(w[i])));
+    return m;
+}
+__device__ __forceinline__ float sum8(uint4v w, float s)
+{
+#pragma unroll
+    for (int i = 0; i < 4; ++i) s += bf16lo_to_f32(w[i]) + bf16hi_to_f32(w[i]);
+    return s;
+}
+
+hipError_t launch_attention_rows16(const AttentionArgs &a, const KvAttention &k, hipStream_t s);
+hipError_t launch_attention_tiles(const AttentionArgs &a, const KvAttention &k, hipStream_t s);
+hipError_t launch_attention_join(const AttentionArgs &a, const KvAttention &k, hipStream_t s);
+
+}  // namespace nvfp4

@@ -386,6 +386,42 @@ __device__ __forceinline__ uint32_t bf16_rne_signed_from_f64(double v)
     return sign | bf16_rne_from_f64(fabs(v));
 }
 
+// Eight codes (one dword) with their block's scale -> eight bf16 (four dwords) RN_bf16(code s_b s_g + mean), the exact sum
+// rounded once.  code s_b is exact in fp32 (2 + 4 bits), and the fused multiply-add rounds (code s_b) s_g + mean once, to
+// fp32: the result lies within half an fp32 ulp of the exact sum, and rounding to bf16 is constant between consecutive bf16
+// midpoints, which are fp32 numbers -- so the two round alike unless the fp32 result is itself a midpoint (low sixteen
+// bits 0x8000: one element in 65 536).  With the tensor scale and the mean in [2^-60, 2^60] (or a mean of zero; `mid` says
+// that both are) every non-zero sum is a multiple of 2^-93 below 2^73: nothing overflows or goes subnormal.  The rest takes
+// the sum in fp64.
+__device__ __forceinline__ bool scale_is_mid(float sg) { return sg >= 0x1p-60f && sg <= 0x1p60f; }
+__device__ __forceinline__ bool mean_is_mid(float abs_mean) { return (abs_mean == 0.0f) | ((abs_mean >= 0x1p-60f) & (abs_mean <= 0x1p60f)); }
+__device__ __forceinline__ void dequant_half_mean(uint32_t cw, float sb, float sg, bool mid, float mean, uint32_t (&o)[4])
+{
+    typedef float float2v __attribute__((ext_vector_type(2)));
+    uint32_t hit = 0xFFFFFFFFu;
+#define NVFP4_PAIR(I)                                                                                                \
+    {                                                                                                                \
+        const float2v q = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(cw, 1.0f, I);                                     \
+        const float y0 = __builtin_fmaf(q.x * sb, sg, mean), y1 = __builtin_fmaf(q.y * sb, sg, mean);                \
+        const uint32_t low = __builtin_amdgcn_perm(__float_as_uint(y1), __float_as_uint(y0), 0x05040100u) ^ 0x80008000u; \
+        hit = __builtin_bit_cast(uint32_t, __builtin_elementwise_min(__builtin_bit_cast(ushort2v, hit), __builtin_bit_cast(ushort2v, low))); \
+        o[I] = pack_bf16x2(y0, y1);                                                                                  \
+    }
+    NVFP4_PAIR(0) NVFP4_PAIR(1) NVFP4_PAIR(2) NVFP4_PAIR(3)
+#undef NVFP4_PAIR
+    const bool sure = mid & ((hit & 0xFFFFu) != 0u) & ((hit >> 16) != 0u);
+    if (__builtin_expect(!sure, 0)) {
+        const double mu = (double)mean, den = (double)sb * (double)sg;      // exact
+#define NVFP4_PAIR(I)                                                                                                \
+    {                                                                                                                \
+        const float2v q = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(cw, 1.0f, I);                                     \
+        o[I] = bf16_rne_signed_from_f64((double)q.x * den + mu) | (bf16_rne_signed_from_f64((double)q.y * den + mu) << 16); \
+    }
+        NVFP4_PAIR(0) NVFP4_PAIR(1) NVFP4_PAIR(2) NVFP4_PAIR(3)
+#undef NVFP4_PAIR
+    }
+}
+
 // K-smoothing (Sec. 3.2, Eq. 6) of one 16-element block given its row mean (a bf16 value):
 // x_j -> RN_bf16(x_j - mean), one rounding of the exact difference.  An fp32 subtraction
 // followed by the rounding to bf16 gives exactly that for every pair of finite bf16 numbers:

@@ -9,6 +9,7 @@
 
 #include <ATen/core/Tensor.h>
 #include <ATen/ops/empty.h>
+#include <c10/core/impl/DeviceGuardImplInterface.h>
 #include <torch/csrc/Device.h>
 #include <torch/csrc/Exceptions.h>
 #include <torch/csrc/autograd/python_variable.h>
@@ -337,6 +338,224 @@ PyObject *gemm_act_quant(PyObject *const *a)                        // A, W, act
     return status([&] { return nvfp4_gemm_act_quant(A.c(), W.c(), act, scale, out.c(), h, ws.data(), ws.size(), s); });
 }
 
+// ---- norm and rotation, paged cache, attention ----------------------------------------------------------
+// Everything these calls take lies on the current GPU: a tensor elsewhere would be an address that the kernels cannot read.
+struct OnDevice {
+    at::Device device = c10::impl::getDeviceGuardImpl(at::kCUDA)->getDevice();
+    const at::Tensor &operator()(const at::Tensor &t) const
+    {
+        require(t.device() == device, "expected tensors on the current GPU");
+        return t;
+    }
+};
+// [T, H, d] with whole rows: heads one behind the other, any distance from token to token
+const at::Tensor &rows(const OnDevice &on, PyObject *o)
+{
+    const at::Tensor &x = on(tensor(o));
+    require(x.scalar_type() == at::kBFloat16 && x.dim() == 3 && x.stride(2) == 1 && x.stride(1) == x.size(2), "expected a bf16 tensor [T, H, d] with contiguous [H, d]");
+    return x;
+}
+int64_t token_stride(const at::Tensor &x) { return x.size(0) > 1 ? x.stride(0) : x.size(1) * x.size(2); }
+const at::Tensor &vector_of(const OnDevice &on, PyObject *o, at::ScalarType type, int dims, const char *text)
+{
+    const at::Tensor &x = on(tensor(o));
+    require(x.scalar_type() == type && x.dim() == dims && x.is_contiguous(), text);
+    return x;
+}
+double real(PyObject *o)
+{
+    const double v = PyFloat_AsDouble(o);
+    if (v == -1.0 && PyErr_Occurred()) throw Fail();
+    return v;
+}
+// (positions, freqs, axis_pairs, interleaved) or None
+struct Rope {
+    nvfp4_rope r{};
+    at::Tensor positions, freqs;
+    nvfp4_rope *c = nullptr;
+    Rope(const OnDevice &on, PyObject *o, int64_t T)
+    {
+        if (o == Py_None) return;
+        if (!PyTuple_Check(o) || PyTuple_GET_SIZE(o) != 4 || !PyTuple_Check(PyTuple_GET_ITEM(o, 2))) fail(PyExc_TypeError, "expected an NVFP4Rope");
+        PyObject *pairs = PyTuple_GET_ITEM(o, 2);
+        r.axes = PyTuple_GET_SIZE(pairs);
+        require(r.axes <= NVFP4_ROPE_MAX_AXES, "at most 4 position axes");
+        int64_t P = 0;
+        for (int64_t i = 0; i < r.axes; ++i) P += r.axis_pairs[i] = number(PyTuple_GET_ITEM(pairs, i));
+        r.interleaved = PyTuple_GET_ITEM(o, 3) == Py_True;
+        positions = vector_of(on, PyTuple_GET_ITEM(o, 0), at::kInt, 2, "expected contiguous int32 positions [T, axes]");
+        freqs = vector_of(on, PyTuple_GET_ITEM(o, 1), at::kFloat, 1, "expected contiguous fp32 frequencies [pairs]");
+        require(positions.size(0) == T && positions.size(1) == r.axes, "expected positions of T tokens and as many axes as axis_pairs");
+        require(freqs.size(0) == P, "expected a frequency for each pair");
+        r.positions = static_cast<const int32_t *>(positions.data_ptr());
+        r.freqs = static_cast<const float *>(freqs.data_ptr());
+        c = &r;
+    }
+};
+const at::Tensor &weight_of(const OnDevice &on, PyObject *o, int64_t d)
+{
+    const at::Tensor &w = vector_of(on, o, at::kBFloat16, 1, "expected a contiguous bf16 weight [d]");
+    require(w.size(0) == d, "expected a weight of d elements");
+    return w;
+}
+PyObject *qk_norm_rope(PyObject *const *a)                          // q, k, q_weight, k_weight, rope, eps, q_out, k_out, stream
+{
+    const OnDevice on;
+    nvfp4_heads h[2]{}, *given[2] = {nullptr, nullptr};
+    int64_t T = -1, d = -1;
+    for (int i = 0; i < 2; ++i) {
+        if (a[i] == Py_None) continue;
+        const at::Tensor &x = rows(on, a[i]), &y = rows(on, a[6 + i]);
+        require((T < 0 || T == x.size(0)) && (d < 0 || d == x.size(2)), "queries and keys of the same tokens and head size");
+        require(y.sizes() == x.sizes(), "an output has its input's shape");
+        T = x.size(0);
+        d = x.size(2);
+        h[i] = {x.data_ptr(), token_stride(x), a[2 + i] == Py_None ? nullptr : weight_of(on, a[2 + i], d).data_ptr(), y.data_ptr(), token_stride(y), x.size(1)};
+        given[i] = &h[i];
+    }
+    const Rope rope(on, a[4], T);
+    const float eps = (float)real(a[5]);
+    void *s = stream_of(a[8]);
+    return status([&] { return nvfp4_qk_norm_rope(given[0], given[1], T, d, eps, rope.c, s); });
+}
+// dq, dk, q, k, q_weight, k_weight, rope, eps, dq_in, dk_in, dq_weight, dk_weight, workspace, stream
+PyObject *qk_norm_rope_backward(PyObject *const *a)
+{
+    const OnDevice on;
+    nvfp4_heads_grad h[2]{}, *given[2] = {nullptr, nullptr};
+    int64_t T = -1, d = -1;
+    bool weights = false;
+    for (int i = 0; i < 2; ++i) {
+        if (a[i] == Py_None) continue;
+        const at::Tensor &dy = rows(on, a[i]), &dx = rows(on, a[8 + i]);
+        require((T < 0 || T == dy.size(0)) && (d < 0 || d == dy.size(2)), "queries and keys of the same tokens and head size");
+        require(dx.sizes() == dy.sizes(), "a gradient has its input's shape");
+        T = dy.size(0);
+        d = dy.size(2);
+        h[i].dy = dy.data_ptr();
+        h[i].ld_dy = token_stride(dy);
+        h[i].dx = dx.data_ptr();
+        h[i].ld_dx = token_stride(dx);
+        h[i].H = dy.size(1);
+        if (a[4 + i] != Py_None) {
+            const at::Tensor &x = rows(on, a[2 + i]);
+            require(x.sizes() == dy.sizes(), "a gradient has its input's shape");
+            h[i].x = x.data_ptr();
+            h[i].ld_x = token_stride(x);
+            h[i].weight = weight_of(on, a[4 + i], d).data_ptr();
+            if (a[10 + i] != Py_None) {
+                const at::Tensor &dw = vector_of(on, a[10 + i], at::kFloat, 1, "expected a contiguous fp32 weight gradient [d]");
+                require(dw.size(0) == d, "expected a weight gradient of d elements");
+                h[i].dweight = static_cast<float *>(dw.data_ptr());
+                weights = true;
+            }
+        }
+        given[i] = &h[i];
+    }
+    const Rope rope(on, a[6], T);
+    const float eps = (float)real(a[7]);
+    at::Tensor ws;
+    if (a[12] != Py_None) ws = on(tensor(a[12]));
+    else if (weights) ws = bytes_on(on.device, std::max<int64_t>(16, (int64_t)nvfp4_workspace_bytes(NVFP4_OP_QK_NORM_ROPE_BACKWARD, T, d, 0)));
+    void *s = stream_of(a[13]), *w = ws.defined() ? ws.data_ptr() : nullptr;
+    const size_t n = ws.defined() ? (size_t)ws.nbytes() : 0;
+    return status([&] { return nvfp4_qk_norm_rope_backward(given[0], given[1], T, d, eps, rope.c, w, n, s); });
+}
+
+// the tuple that an NVFP4KvCache keeps: k_codes, k_scales, k_global, k_mean or None, v_codes, v_scales, v_global
+struct Pages {
+    nvfp4_kv_cache c{};
+    at::Tensor keep[7];
+    Pages(const OnDevice &on, PyObject *o)
+    {
+        if (!PyTuple_Check(o) || PyTuple_GET_SIZE(o) != 7) fail(PyExc_TypeError, "expected an NVFP4KvCache");
+        void *p[7] = {};
+        for (int i = 0; i < 7; ++i) {
+            if (i == 3 && PyTuple_GET_ITEM(o, i) == Py_None) continue;
+            keep[i] = on(tensor(PyTuple_GET_ITEM(o, i)));
+            p[i] = keep[i].data_ptr();
+        }
+        c.k_codes = static_cast<uint8_t *>(p[0]);
+        c.k_scales = static_cast<uint8_t *>(p[1]);
+        c.k_global = static_cast<float *>(p[2]);
+        c.k_mean = p[3];
+        c.v_codes = static_cast<uint8_t *>(p[4]);
+        c.v_scales = static_cast<uint8_t *>(p[5]);
+        c.v_global = static_cast<float *>(p[6]);
+        c.n_pages = keep[0].size(0);                                 // (shapes and strides: checked once, by the NVFP4KvCache)
+        c.page_tokens = keep[0].size(1);
+        c.H = keep[0].size(2);
+        c.d = 2 * keep[0].size(3);
+    }
+};
+PyObject *kv_cache_write(PyObject *const *a)                        // cache, k, v, slots, scale_search, stream
+{
+    const OnDevice on;
+    const Pages pages(on, a[0]);
+    const at::Tensor &slots = vector_of(on, a[3], at::kLong, 1, "expected contiguous int64 slots [T]");
+    void *p[2] = {};
+    int64_t ld[2] = {};
+    for (int i = 0; i < 2; ++i) {
+        if (a[1 + i] == Py_None) continue;
+        const at::Tensor &x = rows(on, a[1 + i]);
+        require(x.size(0) == slots.size(0) && x.size(1) == pages.c.H && x.size(2) == pages.c.d, "expected a token of the cache's heads for each slot");
+        p[i] = x.data_ptr();
+        ld[i] = token_stride(x);
+    }
+    const int search = (int)number(a[4]);
+    void *s = stream_of(a[5]);
+    return status([&] { return nvfp4_kv_cache_write(&pages.c, p[0], ld[0], p[1], ld[1], static_cast<const int64_t *>(slots.data_ptr()), slots.size(0), search, s); });
+}
+PyObject *kv_cache_read(PyObject *const *a)                         // cache, slots, k_out, v_out, stream
+{
+    const OnDevice on;
+    const Pages pages(on, a[0]);
+    const at::Tensor &slots = vector_of(on, a[1], at::kLong, 1, "expected contiguous int64 slots [T]");
+    void *p[2] = {};
+    for (int i = 0; i < 2; ++i) {
+        if (a[2 + i] == Py_None) continue;
+        const at::Tensor &x = on(heads(a[2 + i]));
+        require(x.size(0) == slots.size(0) && x.size(1) == pages.c.H && x.size(2) == pages.c.d, "expected room for a token of the cache's heads for each slot");
+        p[i] = x.data_ptr();
+    }
+    void *s = stream_of(a[4]);
+    return status([&] { return nvfp4_kv_cache_read(&pages.c, static_cast<const int64_t *>(slots.data_ptr()), slots.size(0), p[0], p[1], s); });
+}
+// q, cache, page_table, kv_lens, q_starts, max_q, softmax_scale, causal, window, sink, out_dtype, out, lse, workspace, stream
+PyObject *kv_attention(PyObject *const *a)
+{
+    const OnDevice on;
+    const at::Tensor &q = rows(on, a[0]);
+    const Pages pages(on, a[1]);
+    const nvfp4_kv_cache &c = pages.c;
+    const at::Tensor &table = vector_of(on, a[2], at::kInt, 2, "expected a contiguous int32 page table [B, max_pages]");
+    const at::Tensor &lens = vector_of(on, a[3], at::kInt, 1, "expected contiguous int32 lengths [B]");
+    const at::Tensor &starts = vector_of(on, a[4], at::kInt, 1, "expected contiguous int32 query offsets [B + 1]");
+    const int64_t B = table.size(0), total_q = q.size(0), Hq = q.size(1), max_q = number(a[5]), window = number(a[8]), sink = number(a[9]);
+    require(lens.size(0) == B && starts.size(0) == B + 1, "expected B lengths and B + 1 query offsets");
+    require(q.size(2) == c.d, "expected queries of the cache's head size");
+    const float scale = (float)real(a[6]);
+    const int causal = (int)number(a[7]), dtype = (int)number(a[10]);
+    const at::Tensor &out = on(tensor(a[11]));
+    require(out.scalar_type() == (dtype == NVFP4_OUT_F32 ? at::kFloat : at::kBFloat16) && out.sizes() == q.sizes() && out.stride(2) == 1 && out.stride(1) == c.d,
+            "expected an output of the queries' shape and the chosen type with contiguous [H, d]");
+    float *lse = nullptr;
+    if (a[12] != Py_None) {
+        const at::Tensor &l = vector_of(on, a[12], at::kFloat, 2, "expected a contiguous fp32 lse [total_q, H]");
+        require(l.size(0) == total_q && l.size(1) == Hq, "expected an lse for each query and head");
+        lse = static_cast<float *>(l.data_ptr());
+    }
+    at::Tensor ws;
+    if (a[13] != Py_None) ws = on(tensor(a[13]));
+    else if (const size_t n = nvfp4_kv_attention_workspace_bytes(total_q, Hq, c.H, c.d, table.size(1) * c.page_tokens, B, max_q, window, sink)) ws = bytes_on(on.device, (int64_t)n);
+    void *s = stream_of(a[14]), *w = ws.defined() ? ws.data_ptr() : nullptr, *pq = q.data_ptr(), *po = out.data_ptr();
+    const size_t n = ws.defined() ? (size_t)ws.nbytes() : 0;
+    const int32_t *pt = static_cast<const int32_t *>(table.data_ptr()), *pl = static_cast<const int32_t *>(lens.data_ptr()), *ps = static_cast<const int32_t *>(starts.data_ptr());
+    return status([&] {
+        return nvfp4_kv_attention(pq, token_stride(q), total_q, Hq, &c, pt, table.size(1), pl, ps, B, max_q, scale, causal, window, sink, po, token_stride(out), dtype, lse, w, n, s);
+    });
+}
+
 // one Python function: fixed number of positional arguments, C++ and torch exceptions turned into Python's
 template <PyObject *(*F)(PyObject *const *), int N>
 PyObject *entry(PyObject *, PyObject *const *args, Py_ssize_t n)
@@ -370,7 +589,9 @@ extern "C" PyObject *PyInit__host(void)
         method<kv_quant_4over6, 4>("kv_quant_4over6"), method<kv_quant_noalloc, 3>("kv_quant_noalloc"), method<kv_quant_k, 5>("kv_quant_k"),
         method<kv_dequant, 6>("kv_dequant"), method<kv_dequant_gather, 5>("kv_dequant_gather"), method<gemm, 5>("gemm"),
         method<gemm_scale_out, 6>("gemm_scale_out"), method<lora_down, 5>("lora_down"), method<gemm_lora, 8>("gemm_lora"),
-        method<gemm_act_quant, 8>("gemm_act_quant"), {nullptr, nullptr, 0, nullptr}};
+        method<gemm_act_quant, 8>("gemm_act_quant"), method<qk_norm_rope, 9>("qk_norm_rope"),
+        method<qk_norm_rope_backward, 14>("qk_norm_rope_backward"), method<kv_cache_write, 6>("kv_cache_write"),
+        method<kv_cache_read, 5>("kv_cache_read"), method<kv_attention, 15>("kv_attention"), {nullptr, nullptr, 0, nullptr}};
     static PyModuleDef module = {PyModuleDef_HEAD_INIT, "_host", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
     s_codes = PyUnicode_InternFromString("codes");
     s_scales = PyUnicode_InternFromString("scales");

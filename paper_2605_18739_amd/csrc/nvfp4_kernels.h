@@ -74,6 +74,59 @@ struct KvChunkDesc { const uint8_t *codes, *scales; const float *global_scale; c
 hipError_t launch_dequant_gather(const KvChunkDesc *chunks, int n_chunks, int64_t H, int64_t d, uint16_t *out,
                                  hipStream_t s);
 
+// Norm and rotation of queries and keys, and its gradient.
+constexpr int kRopeMaxAxes = 4;
+struct NormRopeTensor {
+    const uint16_t *x = nullptr, *dy = nullptr;       // dy: backward only
+    const uint16_t *weight = nullptr;                 // nullptr: not normalised
+    uint16_t *out = nullptr;                          // (may be x or dy)
+    int64_t ld = 0, ld_dy = 0, ld_out = 0;
+    int H = 0;                                        // 0: no such tensor
+};
+struct NormRopeArgs {
+    NormRopeTensor q, k;
+    const int32_t *positions = nullptr;
+    const float *freqs = nullptr;
+    int axes = 0, pairs = 0, axis_start[kRopeMaxAxes] = {};       // first pair of each axis (unused axes: never reached)
+    int interleaved = 0, d = 0;
+    float eps = 0.0f;
+    int groups_q = 0, groups_k = 0, groups_per_part = 0;          // filled in by the launchers
+    int64_t parts = 0, units = 0;
+    Divisor by_parts;
+};
+hipError_t launch_norm_rope(NormRopeArgs a, int64_t T, hipStream_t s);
+size_t norm_rope_workspace_bytes(int64_t T, int64_t d);
+hipError_t launch_norm_rope_backward(NormRopeArgs a, int64_t T, float *dwq, float *dwk, float *partial, hipStream_t s);
+
+// Paged KV cache
+struct KvPages {
+    uint8_t *k_codes, *k_scales, *v_codes, *v_scales;
+    const float *k_global, *v_global;
+    uint16_t *k_mean;                                  // nullptr: keys are not smoothed
+    int64_t n_pages, page_tokens;
+    int H, d;
+};
+hipError_t launch_kv_cache_write(const KvPages &c, const uint16_t *k, int64_t ldk, const uint16_t *v, int64_t ldv, const int64_t *slots,
+                                 int64_t T, bool scale_search, hipStream_t s);
+hipError_t launch_kv_cache_read(const KvPages &c, const int64_t *slots, int64_t T, uint16_t *k_out, uint16_t *v_out, hipStream_t s);
+
+// Attention over the paged cache (sizes below 2^31, checked by the caller)
+struct KvAttention {
+    const uint16_t *q;
+    int64_t ldq, total_q, Hq;
+    KvPages cache;
+    const int32_t *page_table, *kv_lens, *q_starts;
+    int64_t max_pages, B, max_q;
+    float softmax_scale;
+    bool causal;
+    int64_t window, sink;
+    void *out;
+    int64_t ldo;
+    bool out_f32;
+    float *lse;
+};
+hipError_t launch_kv_attention(const KvAttention &k, void *workspace, hipStream_t s);
+
 // Ceiling probes (benchmark utilities): kind 0 read `bytes` of a (b: a sink of at least 8 KB), 1 write `bytes` to b,
 // 2 copy a -> b, 3 `iters` x 64 register-resident MFMAs per wave on 256 x 4 waves (b: a sink of at least 256 KB)
 hipError_t launch_probe(int kind, const void *a, void *b, int64_t bytes, int iters, hipStream_t s);

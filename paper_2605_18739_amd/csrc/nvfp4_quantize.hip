@@ -711,7 +711,7 @@ __device__ __forceinline__ void gather_unit(const uint4v *table, const uint8_t *
         if constexpr (SMOOTH) mus[u] = mean[row[u]];
     }
     const float sgf = (float)sg;                           // (the chunk's tensor scale is an fp32 number)
-    const bool sg_mid = sgf >= 0x1p-60f && sgf <= 0x1p60f;
+    const bool sg_mid = scale_is_mid(sgf);
 #pragma unroll
     for (int u = 0; u < U; ++u) {
         const int64_t h = h0 + u * 256;
@@ -721,41 +721,8 @@ __device__ __forceinline__ void gather_unit(const uint4v *table, const uint8_t *
         if constexpr (!SMOOTH) {
             dequant_half_lookup(cw, table[sbs[u]], o);
         } else {
-            // RN_bf16(code s_b s_g + mean), the exact sum rounded once.  code s_b is exact in fp32 (2 + 4 bits), and
-            // the fused multiply-add rounds (code s_b) s_g + mean once, to fp32: the result lies within half an
-            // fp32 ulp of the exact sum, and rounding to bf16 is constant between consecutive bf16 midpoints, which
-            // are fp32 numbers -- so the two round alike unless the fp32 result is itself a midpoint (low sixteen
-            // bits 0x8000: one element in 65 536).  With the tensor scale and the mean in [2^-60, 2^60] (or a mean
-            // of zero) every non-zero sum is a multiple of 2^-93 below 2^73: nothing overflows or goes subnormal.
-            // The rest takes the sum in fp64.
-            typedef float float2v __attribute__((ext_vector_type(2)));
-            const float muf = __uint_as_float(mus[u] << 16), amu = fabsf(muf);
-            const float sbf = e4m3_to_f32(sbs[u]);
-            uint32_t hit = 0xFFFFFFFFu;
-#define NVFP4_GATHER_PAIR(I, SEL)                                                                 \
-    {                                                                                             \
-        const float2v q = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(cw, 1.0f, SEL);                \
-        const float y0 = __builtin_fmaf(q.x * sbf, sgf, muf), y1 = __builtin_fmaf(q.y * sbf, sgf, muf); \
-        const uint32_t low = __builtin_amdgcn_perm(__float_as_uint(y1), __float_as_uint(y0), 0x05040100u) ^ 0x80008000u; \
-        hit = __builtin_bit_cast(uint32_t, __builtin_elementwise_min(__builtin_bit_cast(ushort2v, hit), __builtin_bit_cast(ushort2v, low))); \
-        o[I] = pack_bf16x2(y0, y1);                                                               \
-    }
-            NVFP4_GATHER_PAIR(0, 0) NVFP4_GATHER_PAIR(1, 1) NVFP4_GATHER_PAIR(2, 2) NVFP4_GATHER_PAIR(3, 3)
-#undef NVFP4_GATHER_PAIR
-            const bool sure = sg_mid & ((hit & 0xFFFFu) != 0u) & ((hit >> 16) != 0u) &
-                              ((amu == 0.0f) | ((amu >= 0x1p-60f) & (amu <= 0x1p60f)));
-            if (__builtin_expect(!sure, 0)) {
-                const double mu = (double)muf;
-                const double den = (double)sbf * sg;                // exact
-#define NVFP4_GATHER_PAIR(I, SEL)                                                                 \
-    {                                                                                             \
-        const float2v q = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(cw, 1.0f, SEL);                \
-        o[I] = bf16_rne_signed_from_f64((double)q.x * den + mu) |                                 \
-               (bf16_rne_signed_from_f64((double)q.y * den + mu) << 16);                          \
-    }
-                NVFP4_GATHER_PAIR(0, 0) NVFP4_GATHER_PAIR(1, 1) NVFP4_GATHER_PAIR(2, 2) NVFP4_GATHER_PAIR(3, 3)
-#undef NVFP4_GATHER_PAIR
-            }
+            const float muf = __uint_as_float(mus[u] << 16);
+            dequant_half_mean(cw, e4m3_to_f32(sbs[u]), sgf, sg_mid & mean_is_mid(fabsf(muf)), muf, o);
         }
         __builtin_nontemporal_store(uint4v{o[0], o[1], o[2], o[3]}, (uint4v *)(dst + (h << 3)));
     }
