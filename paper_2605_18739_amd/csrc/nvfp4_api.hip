@@ -219,7 +219,7 @@ int fill_pages(const nvfp4_kv_cache *c, KvPages *p)
         c->page_tokens > kMaxIndex || (c->page_tokens & 15) != 0 || c->n_pages > (1ll << 36) / c->page_tokens)
         return NVFP4_ERR_SHAPE;
     if (!aligned16(c->k_codes) || !aligned16(c->k_scales) || !aligned16(c->v_codes) || !aligned16(c->v_scales) ||
-        !aligned(c->k_global, 4) || !aligned(c->v_global, 4) || !aligned(c->k_mean, 2))
+        !aligned16(c->k_mean) || !aligned(c->k_global, 4) || !aligned(c->v_global, 4))
         return NVFP4_ERR_ALIGN;
     *p = KvPages{c->k_codes, c->k_scales, c->v_codes, c->v_scales, c->k_global, c->v_global, static_cast<uint16_t *>(c->k_mean),
                  c->n_pages, c->page_tokens, (int)c->H, (int)c->d};
@@ -235,7 +235,7 @@ bool attention_sizes_ok(int64_t total_q, int64_t Hq, int64_t H, int64_t d, int64
 }
 bool attention_grid_ok(const AttentionPlan &p, int64_t H, int64_t B)
 {
-    return B * H <= 0x7FFFFFFF / p.pieces && B * H * p.pieces <= 0x7FFFFFFF / p.groups;
+    return B * H <= (kMaxIndex - 8) / p.pieces && B * H * p.pieces + 8 <= kMaxIndex / p.groups;
 }
 
 }  // namespace

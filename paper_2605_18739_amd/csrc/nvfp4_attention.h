@@ -51,13 +51,12 @@ struct Steps {
     __device__ __forceinline__ int first_token(int n, int step_tokens) const { return (n < sink_steps ? n : n - sink_steps + lo_step) * step_tokens; }
 };
 
-// The page of a group of 16 tokens (pages hold whole groups): slot of the group's first token, or none.
-__device__ __forceinline__ int page_of(const AttentionArgs &a, const int32_t *__restrict__ page_table, int b, int token, int &offset)
+// The page of a group of 16 tokens (pages hold whole groups), as the table gives it, and the group's first token in it.
+__device__ __forceinline__ int raw_page(const AttentionArgs &a, const int32_t *__restrict__ page_table, int b, int token, int &offset)
 {
-    const int at = (int)(a.by_page.m ? a.by_page.small((uint32_t)token) : (uint32_t)token / (uint32_t)a.page_tokens);
+    const int at = (int)a.by_page.small((uint32_t)token);
     offset = token - at * a.page_tokens;
-    const int page = page_table[(int64_t)b * a.max_pages + at];
-    return (uint32_t)page < (uint32_t)a.n_pages ? page : -1;
+    return page_table[(int64_t)b * a.max_pages + at];
 }
 
 __device__ __forceinline__ bool seen(const AttentionArgs &a, int j, int p)

@@ -108,9 +108,9 @@ __global__ __launch_bounds__(64 * WAVES, D == 256 ? 1 : 2) void attention_tiles_
     auto group_slot = [&](int first, int group, bool &valid) {
         const int token = first + 16 * group < seq.len ? first + 16 * group : first;
         int offset;
-        const int page = page_of(a, page_table, b, token, offset);
-        valid = page >= 0;
-        return (int64_t)max(page, 0) * a.page_tokens + offset;
+        const int page = raw_page(a, page_table, b, token, offset);
+        valid = (uint32_t)page < (uint32_t)a.n_pages;
+        return (int64_t)(valid ? page : 0) * a.page_tokens + offset;
     };
     auto fetch = [&](int n, Share &s) {
         const int first = steps.first_token(n, kTileStep);

@@ -87,7 +87,7 @@ BAD_CACHES = [(dict([(n, None)]), NULL) for n in ("k_codes", "k_scales", "k_glob
     (dict(n_pages=0), SHAPE), (dict(n_pages=-1), SHAPE), (dict(n_pages=1 << 31), SHAPE), (dict(page_tokens=0), SHAPE), (dict(page_tokens=24), SHAPE),
     (dict(page_tokens=1 << 31), SHAPE), (dict(n_pages=1 << 30, page_tokens=1 << 20), SHAPE), (dict(H=0), SHAPE), (dict(H=1 << 22), SHAPE),
     (dict(d=0), SHAPE), (dict(d=72), SHAPE), (dict(d=288), SHAPE)] + [
-    (dict([(n, P + 4)]), ALIGN) for n in ("k_codes", "k_scales", "v_codes", "v_scales")] + [(dict(k_global=P + 2), ALIGN), (dict(v_global=P + 1), ALIGN), (dict(k_mean=P + 1), ALIGN)]
+    (dict([(n, P + 4)]), ALIGN) for n in ("k_codes", "k_scales", "v_codes", "v_scales")] + [(dict(k_global=P + 2), ALIGN), (dict(v_global=P + 1), ALIGN), (dict(k_mean=P + 2), ALIGN)]
 
 
 def write(c, k=P, ldk=512, v=P, ldv=512, slots=P, T=3, search=0):
