@@ -235,7 +235,8 @@ bool attention_sizes_ok(int64_t total_q, int64_t Hq, int64_t H, int64_t d, int64
 }
 bool attention_grid_ok(const AttentionPlan &p, int64_t H, int64_t B)
 {
-    return B * H <= (kMaxIndex - 8) / p.pieces && B * H * p.pieces + 8 <= kMaxIndex / p.groups;
+    if (p.rows16) return p.pieces + B + 8 <= kMaxIndex / p.groups;
+    return B * H <= kMaxIndex / p.pieces && B * H * p.pieces <= kMaxIndex / p.groups;
 }
 
 }  // namespace
@@ -705,9 +706,9 @@ int nvfp4_kv_attention(const void *q_bf16, int64_t ldq, int64_t total_q, int64_t
     if (!aligned16(q_bf16) || !aligned16(out) || (ldq & 7) != 0 || (ldo & (out_dtype == NVFP4_OUT_BF16 ? 7 : 3)) != 0 ||
         !aligned(page_table, 4) || !aligned(kv_lens, 4) || !aligned(q_starts, 4) || !aligned(lse, 4))
         return NVFP4_ERR_ALIGN;
-    const AttentionPlan plan = attention_plan(Hq, H, d, max_kv, B, max_q, window, sink);
+    const AttentionPlan plan = attention_plan(total_q, Hq, H, d, max_kv, B, max_q, window, sink);
     if (!attention_grid_ok(plan, H, B)) return NVFP4_ERR_SHAPE;
-    const size_t need = attention_workspace_bytes(plan, total_q, Hq, d);
+    const size_t need = attention_workspace_bytes(plan, d);
     if (need > 0 && (!workspace || workspace_bytes < need)) return NVFP4_ERR_WORKSPACE;
     if (need > 0 && !aligned16(workspace)) return NVFP4_ERR_ALIGN;
     a.q = static_cast<const uint16_t *>(q_bf16);
@@ -739,7 +740,7 @@ size_t nvfp4_kv_attention_workspace_bytes(int64_t total_q, int64_t Hq, int64_t H
 {
     max_q = std::min(max_q, total_q);
     if (!attention_sizes_ok(total_q, Hq, H, d, max_kv, B, max_q) || window < 0 || sink < 0) return 0;
-    return attention_workspace_bytes(attention_plan(Hq, H, d, max_kv, B, max_q, window, sink), total_q, Hq, d);
+    return attention_workspace_bytes(attention_plan(total_q, Hq, H, d, max_kv, B, max_q, window, sink), d);
 }
 
 size_t nvfp4_workspace_bytes(int op, int64_t a, int64_t b, int64_t c)

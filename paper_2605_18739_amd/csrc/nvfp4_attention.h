@@ -19,8 +19,8 @@ struct AttentionArgs {
     void *out;
     float *lse;
     AttentionPlan plan;
-    float *part_o;                        // [piece][total_q * Hq][d], partial sums relative to ...
-    float2 *part_ml;                      // [piece][total_q * Hq] their row's maximum (base 2) and sum
+    float *part_o;                        // [partial row][d], partial sums relative to ...
+    float2 *part_ml;                      // [partial row] their row's maximum (base 2) and sum
     Divisor by_page;
 };
 
@@ -58,6 +58,60 @@ __device__ __forceinline__ int raw_page(const AttentionArgs &a, const int32_t *_
     offset = token - at * a.page_tokens;
     return page_table[(int64_t)b * a.max_pages + at];
 }
+
+// rows16: the pieces of all sequences, one behind the other, in the order of the sequences.  A piece is as many steps as
+// make about plan.pieces of them out of what the lengths on the device ask for, so that the work is spread evenly whatever
+// the lengths are (pieces laid out for the longest sequence left a third of the chip's shader engines with twice the others'
+// work: workgroups go round them by number, the empty ones too).  Every wave finds its place by a scan over the sequences,
+// 64 at a time, in registers.
+struct Pieces {
+    int steps;                            // of a piece
+    int first, count;                     // pieces in front of sequence b, and its own
+    int b;                                // sequence of piece number `at`, B: behind the last one
+    __device__ __forceinline__ static int sequence_steps(const AttentionArgs &a, const int32_t *__restrict__ q_starts, const int32_t *__restrict__ kv_lens, int b)
+    {
+        if (b >= a.B) return -1;
+        const Sequence seq(a, q_starts, kv_lens, b);
+        const int n_q = min(seq.n_q, a.max_q);
+        return n_q > 0 ? Steps(a, seq, 0, n_q - 1, kRows16Step).total : -1;
+    }
+    // by_sequence: `at` is a sequence, its pieces are what is asked for
+    __device__ __forceinline__ Pieces(const AttentionArgs &a, const int32_t *__restrict__ q_starts, const int32_t *__restrict__ kv_lens, int at, bool by_sequence)
+    {
+        const int lane = threadIdx.x & 63;
+        int total = 0, mine = sequence_steps(a, q_starts, kv_lens, lane);
+        for (int b0 = 0; b0 < a.B; b0 += 64) {
+            int n = max(b0 == 0 ? mine : sequence_steps(a, q_starts, kv_lens, b0 + lane), 0);
+#pragma unroll
+            for (int x = 32; x > 0; x >>= 1) n += __shfl_xor(n, x, 64);
+            total = total > 0x3FFFFFFF - n ? 0x3FFFFFFF : total + n;
+        }
+        steps = max(__builtin_amdgcn_readfirstlane((total + a.plan.pieces - 1) / a.plan.pieces), a.plan.piece_steps);
+        if (a.plan.pieces <= 1) steps = 0x3FFFFFFF;
+        int before = 0;
+        for (int b0 = 0; b0 < a.B; b0 += 64) {
+            const int s = b0 == 0 ? mine : sequence_steps(a, q_starts, kv_lens, b0 + lane);
+            const int n = s < 0 ? 0 : max((s + steps - 1) / steps, 1);       // (a sequence without tokens has one, which writes its zeros)
+            int upto = n;                                                    // inclusive sum over the lanes
+#pragma unroll
+            for (int x = 1; x < 64; x <<= 1) {
+                const int o = __shfl_up(upto, x, 64);
+                upto += lane >= x ? o : 0;
+            }
+            const bool here = by_sequence ? b0 + lane == at : (at >= before + upto - n) & (at < before + upto);
+            if (const uint64_t found = __ballot(here)) {
+                const int l = (int)__builtin_ctzll(found);
+                b = b0 + l;
+                count = __builtin_amdgcn_readlane(n, l);
+                first = before + __builtin_amdgcn_readlane(upto, l) - count;
+                return;
+            }
+            before += __builtin_amdgcn_readlane(upto, 63);
+        }
+        b = a.B;
+        first = count = 0;
+    }
+};
 
 __device__ __forceinline__ bool seen(const AttentionArgs &a, int j, int p)
 {

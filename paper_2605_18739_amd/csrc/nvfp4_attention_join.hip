@@ -3,64 +3,76 @@
 
 namespace nvfp4 {
 
-// A wave takes a row (query, head): the pieces' maxima and sums first, a lane each, then their partial sums, D / 64 elements
-// a lane.  Pieces are added in order: the result does not depend on when they finished.
-__global__ __launch_bounds__(256) void attention_join_kernel(const AttentionArgs a, const int32_t *__restrict__ kv_lens, const int32_t *__restrict__ q_starts,
-                                                             const float *__restrict__ part_o, const float2 *__restrict__ part_ml, int out_f32)
+// A workgroup takes a row (query, head): the pieces' maxima and sums first (every wave for itself, a lane a piece), then
+// their partial sums, d / 4 lanes to a piece, as many pieces side by side as there are lanes for.  Pieces are added in an
+// order that does not depend on when they finished.
+constexpr int kJoinThreads = 256;
+__global__ __launch_bounds__(kJoinThreads) void attention_join_kernel(const AttentionArgs a, const int32_t *__restrict__ kv_lens, const int32_t *__restrict__ q_starts,
+                                                                      const float *__restrict__ part_o, const float2 *__restrict__ part_ml, int out_f32)
 {
+    __shared__ float4v sums[kJoinThreads];
     const int lane = threadIdx.x & 63;
-    int64_t id = (int64_t)__builtin_amdgcn_readfirstlane((int)(blockIdx.x * 4 + (threadIdx.x >> 6)));
+    int64_t id = blockIdx.x;
     const int head = (int)(id % a.Hq);
     id /= a.Hq;
     const int i = (int)(id % a.max_q), b = (int)(id / a.max_q);
-    if (b >= a.B) return;
     const Sequence seq(a, q_starts, kv_lens, b);
     const int n_q = min(seq.n_q, a.max_q);
     if (i >= n_q) return;
-    // the steps of the workgroup that had this row
-    int i0 = 0, i1 = n_q - 1;
-    if (!a.plan.rows16) {
+    int pieces;
+    int64_t first, stride;                                    // partial rows of this row: first + s * stride
+    const int64_t query = (int64_t)seq.start + i, out_row = query * a.Hq + head;
+    if (a.plan.rows16) {
+        const Pieces p(a, q_starts, kv_lens, b, true);
+        pieces = p.count;
+        first = ((int64_t)p.first * a.max_q + i) * a.Hq + head;
+        stride = (int64_t)a.max_q * a.Hq;
+    } else {
+        // the steps of the workgroup that had this row
         const int rows = 32 * a.plan.waves, row0 = (i * a.G + head % a.G) / rows * rows;
-        i0 = row0 / a.G;
-        i1 = min((row0 + rows - 1) / a.G, n_q - 1);
+        const Steps steps(a, seq, row0 / a.G, min((row0 + rows - 1) / a.G, n_q - 1), kTileStep);
+        pieces = (steps.total + a.plan.piece_steps - 1) / a.plan.piece_steps;
+        first = out_row;
+        stride = (int64_t)a.total_q * a.Hq;
     }
-    const Steps steps(a, seq, i0, i1, a.plan.rows16 ? kRows16Step : kTileStep);
-    if (steps.total <= a.plan.piece_steps) return;            // (one piece: written by its workgroup)
-    const int pieces = (steps.total + a.plan.piece_steps - 1) / a.plan.piece_steps;
-    const int64_t query = (int64_t)seq.start + i, out_row = query * a.Hq + head, rows = (int64_t)a.total_q * a.Hq;
+    if (pieces <= 1) return;                                  // (written by its workgroup)
 
     float m = kLowest;
-    for (int s = lane; s < pieces; s += 64) m = fmaxf(m, part_ml[s * rows + out_row].x);
+    for (int s = lane; s < pieces; s += 64) m = fmaxf(m, part_ml[first + s * stride].x);
 #pragma unroll
     for (int x = 32; x > 0; x >>= 1) m = fmaxf(m, __shfl_xor(m, x, 64));
     float l = 0.0f;
     for (int s = lane; s < pieces; s += 64) {
-        const float2 v = part_ml[s * rows + out_row];
+        const float2 v = part_ml[first + s * stride];
         l = __builtin_fmaf(v.y, __builtin_amdgcn_exp2f(v.x - m), l);
     }
 #pragma unroll
     for (int x = 32; x > 0; x >>= 1) l += __shfl_xor(l, x, 64);
-    const int e = 4 * lane;
+    const int lanes = a.d >> 2, side = kJoinThreads / lanes, sub = (int)threadIdx.x / lanes, e = 4 * ((int)threadIdx.x - sub * lanes);
     float4v o = {0.0f, 0.0f, 0.0f, 0.0f};
-    if (e < a.d) {
+    if (sub < side) {
 #pragma unroll 4
-        for (int s = 0; s < pieces; ++s) {
-            const float w = __builtin_amdgcn_exp2f(part_ml[s * rows + out_row].x - m);
-            const float4v v = *(const float4v *)(part_o + (s * rows + out_row) * a.d + e);
-            o += v * w;
+        for (int s = sub; s < pieces; s += side) {
+            const int64_t row = first + s * stride;
+            const float w = __builtin_amdgcn_exp2f(part_ml[row].x - m);
+            o += *(const float4v *)(part_o + row * a.d + e) * w;
         }
+    }
+    sums[threadIdx.x] = o;
+    __syncthreads();
+    if (sub == 0) {
+        for (int s = 1; s < side; ++s) o += sums[s * lanes + (int)threadIdx.x];
         o *= l > 0.0f ? 1.0f / l : 0.0f;
         const int64_t at = query * a.ldo + (int64_t)head * a.d + e;
         if (out_f32) *(float4v *)((float *)a.out + at) = o;
         else *(uint2v *)((uint16_t *)a.out + at) = uint2v{pack_bf16x2(o.x, o.y), pack_bf16x2(o.z, o.w)};
     }
-    if (a.lse && lane == 0) a.lse[out_row] = l > 0.0f ? (m + __builtin_amdgcn_logf(l)) * 0.6931471805599453f : -__builtin_inff();
+    if (a.lse && threadIdx.x == 0) a.lse[out_row] = l > 0.0f ? (m + __builtin_amdgcn_logf(l)) * 0.6931471805599453f : -__builtin_inff();
 }
 
 hipError_t launch_attention_join(const AttentionArgs &a, const KvAttention &k, hipStream_t s)
 {
-    const int64_t rows = (int64_t)a.B * a.max_q * a.Hq;
-    attention_join_kernel<<<(unsigned)((rows + 3) / 4), 256, 0, s>>>(a, k.kv_lens, k.q_starts, a.part_o, a.part_ml, k.out_f32);
+    attention_join_kernel<<<(unsigned)((int64_t)a.B * a.max_q * a.Hq), kJoinThreads, 0, s>>>(a, k.kv_lens, k.q_starts, a.part_o, a.part_ml, k.out_f32);
     return hipGetLastError();
 }
 
@@ -93,9 +105,9 @@ hipError_t launch_kv_attention(const KvAttention &k, void *workspace, hipStream_
     a.sink = (int)std::min(k.sink, far);
     a.out = k.out;
     a.lse = k.lse;
-    a.plan = attention_plan(k.Hq, c.H, c.d, k.max_pages * c.page_tokens, k.B, k.max_q, k.window, k.sink);
+    a.plan = attention_plan(k.total_q, k.Hq, c.H, c.d, k.max_pages * c.page_tokens, k.B, k.max_q, k.window, k.sink);
     a.part_o = static_cast<float *>(workspace);
-    a.part_ml = reinterpret_cast<float2 *>(a.part_o + (int64_t)a.plan.pieces * k.total_q * k.Hq * c.d);
+    a.part_ml = reinterpret_cast<float2 *>(a.part_o + a.plan.part_rows * c.d);
     a.by_page = Divisor(c.page_tokens, k.max_pages * c.page_tokens);
     const hipError_t e = a.plan.rows16 ? launch_attention_rows16(a, k, s) : launch_attention_tiles(a, k, s);
     if (e != hipSuccess || a.plan.pieces <= 1) return e;

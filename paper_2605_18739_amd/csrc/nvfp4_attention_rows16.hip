@@ -35,28 +35,26 @@ struct Step {
 };
 
 template <int D, bool FULL, bool SMOOTH, bool F32>
-__global__ __launch_bounds__(512) void attention_rows16_kernel(const AttentionArgs a, const int32_t *__restrict__ page_table,
+__global__ __launch_bounds__(64 * kRows16Heads) void attention_rows16_kernel(const AttentionArgs a, const int32_t *__restrict__ page_table,
                                                                const int32_t *__restrict__ kv_lens, const int32_t *__restrict__ q_starts,
                                                                const float *__restrict__ k_global, const float *__restrict__ v_global)
 {
     constexpr int KD = D / 4, NT = D / 16;                 // elements of a lane's key part; column tiles of the values
     const int lane = threadIdx.x & 63, r = lane & 15, g = lane >> 4;
     const int d = FULL ? D : a.d;
-    // pieces go round the eight chiplets (workgroup id modulo 8), whatever the sequences' lengths: with a chiplet a sequence the
-    // longest of eight took twice as long as all of them spread out; the head groups of a piece, whose scales share cache
-    // lines, follow each other on one chiplet
-    const int set = (int)(blockIdx.x >> 3) / a.plan.groups * 8 + (int)(blockIdx.x & 7u), hg = (int)(blockIdx.x >> 3) % a.plan.groups;
-    const int b = set / a.plan.pieces, piece = set - b * a.plan.pieces;
+    // pieces go round the eight chiplets (workgroup id modulo 8); the head groups of a piece, whose scales share cache lines,
+    // follow each other on one chiplet
+    const int at = (int)(blockIdx.x >> 3) / a.plan.groups * 8 + (int)(blockIdx.x & 7u), hg = (int)(blockIdx.x >> 3) % a.plan.groups;
+    const Pieces pieces(a, q_starts, kv_lens, at, false);
+    const int b = pieces.b;
     if (b >= a.B) return;
     const int h = hg * a.plan.waves + __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
     if (h >= a.H) return;
     const Sequence seq(a, q_starts, kv_lens, b);
     const int n_q = min(seq.n_q, a.max_q);
-    if (n_q <= 0) return;
     const Steps steps(a, seq, 0, n_q - 1, kRows16Step);
-    const int n0 = piece * a.plan.piece_steps, n1 = min(n0 + a.plan.piece_steps, steps.total);
-    const bool alone = steps.total <= a.plan.piece_steps;  // this sequence has one piece: no partial results
-    if (n0 >= n1 && piece > 0) return;
+    const bool alone = pieces.count == 1;                  // no partial results
+    const int n0 = alone ? 0 : (at - pieces.first) * pieces.steps, n1 = alone ? steps.total : min(n0 + pieces.steps, steps.total);
 
     // ---- pages of a step, and what a lane loads of it, as offsets from the group's first slot.
     // Pages and their scales are the same for the whole wave, but they come through vector loads like the rest: those return
@@ -346,7 +344,7 @@ __global__ __launch_bounds__(512) void attention_rows16_kernel(const AttentionAr
         }
         return;
     }
-    const int64_t part = (int64_t)piece * a.total_q * a.Hq + out_row;
+    const int64_t part = ((int64_t)at * a.max_q + i) * a.Hq + head;
     if (g == 0) a.part_ml[part] = float2{m, l};
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
@@ -361,7 +359,8 @@ __global__ __launch_bounds__(512) void attention_rows16_kernel(const AttentionAr
 template <int D>
 static void launch_rows16(const AttentionArgs &a, const KvAttention &k, hipStream_t s)
 {
-    const dim3 grid((unsigned)((((int64_t)a.B * a.plan.pieces + 7) >> 3 << 3) * a.plan.groups)), block((unsigned)(64 * a.plan.waves));
+    const int64_t pieces = a.plan.pieces > 1 ? a.plan.pieces + a.B : a.B;
+    const dim3 grid((unsigned)(((pieces + 7) >> 3 << 3) * a.plan.groups)), block((unsigned)(64 * a.plan.waves));
     auto go = [&](auto kernel) { kernel<<<grid, block, 0, s>>>(a, k.page_table, k.kv_lens, k.q_starts, k.cache.k_global, k.cache.v_global); };
     auto smooth = [&](auto full) {
         constexpr bool FULL = decltype(full)::value;
