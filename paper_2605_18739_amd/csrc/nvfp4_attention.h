@@ -51,14 +51,6 @@ struct Steps {
     __device__ __forceinline__ int first_token(int n, int step_tokens) const { return (n < sink_steps ? n : n - sink_steps + lo_step) * step_tokens; }
 };
 
-// The page of a group of 16 tokens (pages hold whole groups), as the table gives it, and the group's first token in it.
-__device__ __forceinline__ int raw_page(const AttentionArgs &a, const int32_t *__restrict__ page_table, int b, int token, int &offset)
-{
-    const int at = (int)a.by_page.small((uint32_t)token);
-    offset = token - at * a.page_tokens;
-    return page_table[(int64_t)b * a.max_pages + at];
-}
-
 // rows16: the pieces of all sequences, one behind the other, in the order of the sequences.  A piece is as many steps as
 // make about plan.pieces of them out of what the lengths on the device ask for, so that the work is spread evenly whatever
 // the lengths are (pieces laid out for the longest sequence left a third of the chip's shader engines with twice the others'
@@ -113,10 +105,12 @@ struct Pieces {
     }
 };
 
-__device__ __forceinline__ bool seen(const AttentionArgs &a, int j, int p)
-{
-    return (j <= p) & ((a.window == 0) | (j > p - a.window) | (j < a.sink));
-}
+// What a query at position p sees: token j <= p, behind `after` or in front of the sink's end.
+struct Sight {
+    int p, after, sink;
+    __device__ __forceinline__ Sight(const AttentionArgs &a, int position) : p(position), after(a.window > 0 ? position - a.window : -0x40000000), sink(a.sink) {}
+    __device__ __forceinline__ bool of(int j) const { return (j <= p) & ((j > after) | (j < sink)); }
+};
 
 // A token's weight is 2^(s + log2 g_v - m): with its page's value scale g_v in the exponent the values enter the product
 // as code * block scale, exact in f16, and the sum of the weights takes the factor out again (weight / g_v).

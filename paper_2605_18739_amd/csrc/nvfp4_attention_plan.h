@@ -40,7 +40,7 @@ inline AttentionPlan attention_plan(int64_t total_q, int64_t Hq, int64_t H, int6
         if (steps <= kRows16MinSteps) p.pieces = 1;
         p.part_rows = p.pieces <= 1 ? 0 : (p.pieces + B) * max_q * Hq;
     } else {
-        p.waves = d <= 128 && rows > 128 ? 8 : 4;
+        p.waves = d > 64 && d <= 128 && rows > 128 ? 8 : 4;
         p.groups = (int)((rows + 32 * p.waves - 1) / (32 * p.waves));
         const int64_t steps = std::max<int64_t>(1, (max_kv + kTileStep - 1) / kTileStep);
         const int64_t items = B * H * p.groups, slots = p.waves == 8 || d > 128 ? 256 : 512;

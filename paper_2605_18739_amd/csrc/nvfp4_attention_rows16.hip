@@ -172,7 +172,7 @@ __global__ __launch_bounds__(64 * kRows16Heads) void attention_rows16_kernel(con
     // ---- queries
     const int i = r / a.G, head = h * a.G + (r - i * a.G);
     const bool row = i < n_q;
-    const int p = seq.position(a, i);
+    const Sight sight(a, seq.position(a, i));
     const int64_t query = (int64_t)seq.start + i;
     half8v q[KD / 8];
     float factor, sum_q;                                   // score = (S + (mean / g_k) sum_q) factor g_k, base 2
@@ -244,7 +244,7 @@ __global__ __launch_bounds__(64 * kRows16Heads) void attention_rows16_kernel(con
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
                 const int j = s.first + 16 * (e >> 2) + 4 * g + (e & 3);
-                x[e] = (s.valid[e >> 2] & seen(a, j, p)) ? x[e] : -__builtin_inff();
+                x[e] = (s.valid[e >> 2] & sight.of(j)) ? x[e] : -__builtin_inff();
             }
         }
         const float top = fmaxf(fmaxf(fmaxf(x[0], x[1]), fmaxf(x[2], x[3])), fmaxf(fmaxf(x[4], x[5]), fmaxf(x[6], x[7])));

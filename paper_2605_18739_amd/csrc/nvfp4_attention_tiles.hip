@@ -2,6 +2,8 @@
 // video, prompts.  Bound by the matrix pipes and the vector pipes' exponentials together.
 #include "nvfp4_attention.h"
 
+#include <type_traits>
+
 namespace nvfp4 {
 
 // A workgroup takes 32 WAVES rows of one cached head and walks over the cached tokens, 64 at a time:
@@ -17,19 +19,36 @@ namespace nvfp4 {
 template <int D, int WAVES>
 struct Tiles {
     static constexpr int kThreads = 64 * WAVES;
-    static constexpr int kTasks = 4 * D / kThreads > 0 ? 4 * D / kThreads : 1;    // blocks of keys, and pieces of values, of a lane
+    static constexpr int kTasks = 4 * D / kThreads;       // blocks of keys, and pieces of values, of a lane
     uint8_t k[2][kTileStep * D * 2];      // [token][D] f16
     uint8_t v[2][D * kTileStep * 2];      // [element][token] f16
-    float mean[2][kTileStep];
+    float mean[2][kTileStep];             // row mean / g_k
     float kg[2][4], log_v[2][4], inv_v[2][4];       // of the four groups of sixteen tokens
     uint32_t valid[2][4];
 };
 
-template <int D>
-__device__ __forceinline__ uint32_t k_place(int token, int chunk) { return (uint32_t)(token * (2 * D) + ((chunk ^ (token & (D / 8 - 1) & 15)) << 4)); }
-__device__ __forceinline__ uint32_t v_place(int element, int chunk) { return (uint32_t)(element * (2 * kTileStep) + (((chunk ^ element ^ (element >> 3)) & 7) << 4)); }
+// (integral constants 0 .. N - 1, for code that has to be laid out by hand)
+template <int N, class F>
+__device__ __forceinline__ void each(F &&f)
+{
+    if constexpr (N > 0) {
+        each<N - 1>(f);
+        f(std::integral_constant<int, N - 1>());
+    }
+}
 
-template <int D, int WAVES, bool F32>
+// What a wave does in a turn is laid out by hand, because the compiler reads a fragment right in front of the instruction
+// that multiplies it and waits for LDS every time (18480 tokens, 3520 x 24 queries: 1120 us):
+//   Q K^T   the next fragments are read while the present ones are multiplied, and the next step's codes are turned into f16
+//           in between (their loads were issued a turn before);
+//   loads of the step behind that one;
+//   the maximum; then the weights of sixteen tokens while the sixteen before are multiplied with their values.
+// The fences keep what stands between them in place.
+#define NVFP4_FENCE __builtin_amdgcn_sched_barrier(0)
+
+// SMOOTH: the keys' row means enter as an outer product, (mean / g_k) x (sum of the query's elements), by one
+// v_mfma_f32_32x32x2_f32 into the accumulator that the codes are then added to: the vector pipe has no time for them.
+template <int D, int WAVES, bool SMOOTH, bool F32>
 __global__ __launch_bounds__(64 * WAVES, D == 256 ? 1 : 2) void attention_tiles_kernel(const AttentionArgs a, const int32_t *__restrict__ page_table,
                                                                           const int32_t *__restrict__ kv_lens, const int32_t *__restrict__ q_starts,
                                                                           const float *__restrict__ k_global, const float *__restrict__ v_global)
@@ -66,15 +85,140 @@ __global__ __launch_bounds__(64 * WAVES, D == 256 ? 1 : 2) void attention_tiles_
     const int n0 = piece * a.plan.piece_steps, n1 = min(n0 + a.plan.piece_steps, steps.total);
     const bool alone = steps.total <= a.plan.piece_steps;
     if (n0 >= n1 && piece > 0) return;
-    const bool smooth = a.k_mean != nullptr;
+
+    // ---- this lane's share of a step: blocks of keys (token, block) and pieces of values (pair of tokens, eight elements).
+    // The tasks of a wave lie in one group of sixteen tokens, so its page is the wave's; like everything else it comes
+    // through vector loads, which return in order, and it is looked up a step ahead of its use.
+    constexpr int NB = D / 16, NE = D / 8;
+    static_assert(4 * D >= kThreads, "every lane has a task");
+    const uint32_t token_codes = (uint32_t)a.H * (uint32_t)(a.d >> 1), token_scales = (uint32_t)a.H * (uint32_t)(a.d >> 4);
+    constexpr uint32_t kOutside = 0x7FFFFF00u;             // (loads behind the sixteen tokens give zeros: elements from d on)
+    constexpr uint32_t kZero = 0x0Cu;                      // (of a byte permutation: zero)
+    uint32_t zero;                                         // (an offset that the compiler takes for a lane's own)
+    asm("v_mov_b32 %0, 0" : "=v"(zero));
+    // offsets within a group: a lane's task has the same place in each of its groups
+    const int token16 = (tid / NB) & 15, blk = tid % NB, pair8 = (tid / NE) & 7, part = tid % NE;
+    const bool k_in = 16 * blk < a.d, v_in = 8 * part < a.d;
+    const uint32_t k_at = k_in ? token16 * token_codes + (uint32_t)h * (uint32_t)(a.d >> 1) + 8u * blk : kOutside;
+    const uint32_t ks_byte = token16 * token_scales + (uint32_t)h * (uint32_t)(a.d >> 4) + blk;
+    const uint32_t ks_at = k_in ? ks_byte & ~3u : kOutside, ks_pick = (ks_byte & 3u) * 0x10001u | kZero << 8 | kZero << 24;
+    const uint32_t v_at = v_in ? 2 * pair8 * token_codes + (uint32_t)h * (uint32_t)(a.d >> 1) + 4u * part : kOutside;
+    const uint32_t vs_byte0 = 2 * pair8 * token_scales + (uint32_t)h * (uint32_t)(a.d >> 4) + (part >> 1), vs_byte1 = vs_byte0 + token_scales;
+    const uint32_t vs_at0 = v_in ? vs_byte0 & ~3u : kOutside, vs_at1 = v_in ? vs_byte1 & ~3u : kOutside;
+    const uint32_t vs_pick = (vs_byte0 & 3u) | ((vs_byte1 & 3u) + 4u) << 16 | kZero << 8 | kZero << 24;
+    const uint32_t mean_at = ((uint32_t)(token16 * a.H + h) * 2u) & ~3u, mean_shift = ((uint32_t)(token16 * a.H + h) & 1u) * 16u;
+    struct Share {
+        uint2v k[kTasks];
+        uint32_t ks[kTasks], v[kTasks][2], vs[kTasks][2], mean[kTasks], kg[kTasks], vg[kTasks];
+        bool valid[kTasks];
+    };
+    struct Ahead {
+        int offset[kTasks];
+        uint32_t page[kTasks];
+    };
+    auto group_of = [&](int t) { return (64 * wave + t * kThreads) / (16 * NB); };
+    auto as_loaded = [](uint32_t &v) { asm volatile("" : "+v"(v)); };
+    auto group = [](const void *base, int64_t at, uint32_t bytes) {
+        return __builtin_amdgcn_make_buffer_rsrc((void *)((const uint8_t *)base + at), 0, (int)bytes, 0x00020000);
+    };
+    auto look_up = [&](int n) {
+        Ahead p;
+        const int first = steps.first_token(min(n, n1 - 1), kTileStep);
+#pragma unroll
+        for (int t = 0; t < kTasks; ++t) {  // (a group past the length is masked; it may be past the table: the step's first group stands in)
+            const int token = first + 16 * group_of(t) < seq.len ? first + 16 * group_of(t) : first;
+            const int at = (int)a.by_page.small((uint32_t)token);
+            p.offset[t] = token - at * a.page_tokens;
+            p.page[t] = ((const uint32_t *)page_table)[(int64_t)b * a.max_pages + at + zero];
+        }
+        return p;
+    };
+    // fetches the step whose pages were looked up, and looks up those of step n
+    auto fetch = [&](Ahead &p, Share &s, int n) {
+        uint32_t pages[kTasks];
+#pragma unroll
+        for (int t = 0; t < kTasks; ++t) {
+            as_loaded(p.page[t]);
+            pages[t] = (uint32_t)__builtin_amdgcn_readfirstlane((int)p.page[t]);
+        }
+        const Ahead now = p;
+        p = look_up(n);
+#pragma unroll
+        for (int t = 0; t < kTasks; ++t) {
+            s.valid[t] = pages[t] < (uint32_t)a.n_pages;
+            const uint32_t page = s.valid[t] ? pages[t] : 0u;
+            s.kg[t] = ((const uint32_t *)k_global)[page + zero];
+            s.vg[t] = ((const uint32_t *)v_global)[page + zero];
+            const int64_t row = ((int64_t)page * a.page_tokens + now.offset[t]) * a.H;
+            const __amdgpu_buffer_rsrc_t vc = group(a.v_codes, row * (a.d >> 1), 16u * token_codes), vsc = group(a.v_scales, row * (a.d >> 4), 16u * token_scales);
+            s.k[t] = __builtin_amdgcn_raw_buffer_load_b64(group(a.k_codes, row * (a.d >> 1), 16u * token_codes), k_at, 0, 0);
+            s.ks[t] = __builtin_amdgcn_raw_buffer_load_b32(group(a.k_scales, row * (a.d >> 4), 16u * token_scales), ks_at, 0, 0);
+            s.v[t][0] = __builtin_amdgcn_raw_buffer_load_b32(vc, v_at, 0, 0);
+            s.v[t][1] = __builtin_amdgcn_raw_buffer_load_b32(vc, v_at, (int)token_codes, 0);
+            s.vs[t][0] = __builtin_amdgcn_raw_buffer_load_b32(vsc, vs_at0, 0, 0);
+            s.vs[t][1] = __builtin_amdgcn_raw_buffer_load_b32(vsc, vs_at1, 0, 0);
+            if constexpr (SMOOTH) s.mean[t] = __builtin_amdgcn_raw_buffer_load_b32(group(a.k_mean, 2 * row, 32u * (uint32_t)a.H), mean_at, 0, 0);
+        }
+        __builtin_amdgcn_sched_barrier(0);                 // (the loads stay in front of what follows)
+    };
+    // ---- places in LDS: 16-byte chunk c of row r at r * (row size) + (c ^ key(r)) * 16.  Keys: token rows of D / 8 chunks, key
+    // r % 16 (r % 8 where there are eight chunks); values: element rows of eight chunks, key (r ^ r / 8) % 8.
+    constexpr uint32_t kKRow = 2 * D, kVRow = 2 * kTileStep, kKStage = kTileStep * kKRow, kVStage = D * kVRow, kVBase = 2 * kKStage;
+    constexpr int kKeyMask = (D / 8 - 1) & 15;
+    const int token0 = tid / NB, pair0 = tid / NE, quarter = (pair0 >> 1) & 3;
+    const uint32_t k_to = (uint32_t)token0 * kKRow + (uint32_t)(((2 * blk) ^ (token0 & kKeyMask)) << 4);     // (the block's second chunk: ^ 16)
+    // tokens 2 pair and 2 pair + 1 of their sixteen lie in quarter (pair / 2) % 4; quarter 2 x + y goes to chunk y (of the sixteen's two), half x
+    const uint32_t v_to = kVBase + 8u * part * kVRow + (uint32_t)(((2 * group_of(0) + (quarter & 1)) ^ part) & 7) * 16u + 8u * (quarter >> 1) + 4u * (pair0 & 1);
+    constexpr int kPieces = 7;                             // of a task
+    uint32_t even[kTasks], odd[kTasks];
+    half2v sv[kTasks];
+    auto store_piece = [&](Share &s, auto stage_constant, auto piece_constant) {
+        constexpr int stage = decltype(stage_constant)::value, t = decltype(piece_constant)::value / kPieces, i = decltype(piece_constant)::value % kPieces;
+        constexpr uint32_t k_off = stage * kKStage + t * (kThreads / NB) * kKRow;
+        uint8_t *const lds_v = lds_bytes + stage * kVStage;
+        if constexpr (i == 0) {
+            const half2v sk = scale_pair(__builtin_amdgcn_perm(0u, s.ks[t], ks_pick));
+            *(half8v *)(lds_bytes + k_to + k_off) = eight_codes(s.k[t].x, sk);
+        } else if constexpr (i == 1) {
+            const half2v sk = scale_pair(__builtin_amdgcn_perm(0u, s.ks[t], ks_pick));
+            *(half8v *)(lds_bytes + (k_to ^ 16u) + k_off) = eight_codes(s.k[t].y, sk);
+        } else if constexpr (i == 2) {
+            // nibbles of the two tokens side by side: byte j of `even` is element 2 j of both, of `odd` element 2 j + 1
+            even[t] = (s.v[t][0] & 0x0F0F0F0Fu) | ((s.v[t][1] << 4) & 0xF0F0F0F0u);
+            odd[t] = ((s.v[t][0] >> 4) & 0x0F0F0F0Fu) | (s.v[t][1] & 0xF0F0F0F0u);
+            sv[t] = scale_pair(__builtin_amdgcn_perm(s.vs[t][1], s.vs[t][0], vs_pick));
+            const float kg = __uint_as_float(s.kg[t]), vg = __uint_as_float(s.vg[t]);
+            if constexpr (SMOOTH)
+                if (blk == 0) lds.mean[stage][token0 + t * (kThreads / NB)] = __uint_as_float((s.mean[t] >> mean_shift) << 16) * __builtin_amdgcn_rcpf(kg);
+            if (token16 == 0 && blk == 0) {
+                lds.kg[stage][group_of(t)] = kg;
+                lds.log_v[stage][group_of(t)] = __builtin_amdgcn_logf(vg);
+                lds.inv_v[stage][group_of(t)] = __builtin_amdgcn_rcpf(vg);
+                lds.valid[stage][group_of(t)] = s.valid[t] ? 1u : 0u;
+            }
+        } else {
+            constexpr int b = i - 3;                       // elements 2 b and 2 b + 1 of the eight
+            const uint32_t to = v_to ^ (uint32_t)((2 * (group_of(t) ^ group_of(0))) << 4);
+            *(half2v *)(lds_v + (to ^ (2 * b) << 4) + 2 * b * kVRow) = code_pair<b>(even[t]) * sv[t];
+            *(half2v *)(lds_v + (to ^ (2 * b + 1) << 4) + (2 * b + 1) * kVRow) = code_pair<b>(odd[t]) * sv[t];
+        }
+    };
+
+    // the first step's loads go out before the queries are read
+    Share share;
+    Ahead ahead = {};
+    if (n0 < n1) {
+        ahead = look_up(n0);
+        fetch(ahead, share, n0 + 1);
+    }
 
     // ---- queries of this wave's rows: lane holds row c32, elements 16 step + 8 hi .. + 7 of every k step
     const int my_row = row0 + 32 * wave + c32, i = my_row / a.G, head = h * a.G + (my_row - i * a.G);
     const bool row = i < n_q;
-    const int p = seq.position(a, i);
+    const Sight sight(a, seq.position(a, i));
     const int64_t query = (int64_t)seq.start + i;
     half8v q[D / 16];
-    float factor, sum_q;
+    float factor, sum_q;                                   // score = (S + (mean / g_k) sum_q) factor g_k, base 2
     {
         uint4v w[D / 16];
         float amax = 0.0f, sum = 0.0f;
@@ -83,8 +227,11 @@ __global__ __launch_bounds__(64 * WAVES, D == 256 ? 1 : 2) void attention_tiles_
             const int e = 16 * c + 8 * hi;
             w[c] = uint4v{0u, 0u, 0u, 0u};
             if (row && e < a.d) w[c] = *(const uint4v *)(a.q + query * a.ldq + (int64_t)head * a.d + e);
+        }
+#pragma unroll
+        for (int c = 0; c < D / 16; ++c) {
             amax = absmax8(w[c], amax);
-            sum = sum8(w[c], sum);
+            if constexpr (SMOOTH) sum = sum8(w[c], sum);
         }
         amax = fmaxf(amax, __shfl_xor(amax, 32, 64));
         sum += __shfl_xor(sum, 32, 64);
@@ -92,102 +239,8 @@ __global__ __launch_bounds__(64 * WAVES, D == 256 ? 1 : 2) void attention_tiles_
 #pragma unroll
         for (int c = 0; c < D / 16; ++c) q[c] = query_pairs(w[c], e);
         factor = __builtin_amdgcn_ldexpf(a.scale, -e);
-        sum_q = sum * a.scale;
+        sum_q = hi == 0 ? __builtin_amdgcn_ldexpf(sum, e) : 0.0f;        // (the outer product has two terms, one of them zero)
     }
-
-    // ---- this lane's share of a step: blocks of keys (token, block) and pieces of values (pair of tokens, eight elements)
-    struct Share {
-        uint2v k[kTasks];
-        uint32_t ks[kTasks], v[kTasks][2], vs[kTasks];
-        uint32_t mean;
-        float kg, vg;
-        uint32_t valid;
-    };
-    constexpr int NB = D / 16, NE = D / 8;
-    // first slot of a token's group, times H: the row of its codes (a group past the length: the step's first one)
-    auto group_slot = [&](int first, int group, bool &valid) {
-        const int token = first + 16 * group < seq.len ? first + 16 * group : first;
-        int offset;
-        const int page = raw_page(a, page_table, b, token, offset);
-        valid = (uint32_t)page < (uint32_t)a.n_pages;
-        return (int64_t)(valid ? page : 0) * a.page_tokens + offset;
-    };
-    auto fetch = [&](int n, Share &s) {
-        const int first = steps.first_token(n, kTileStep);
-#pragma unroll
-        for (int t = 0; t < kTasks; ++t) {
-            const int task = tid + t * kThreads;
-            s.k[t] = uint2v{0u, 0u};
-            s.ks[t] = s.v[t][0] = s.v[t][1] = s.vs[t] = 0u;
-            if (task < 4 * D) {
-                bool valid;
-                const int token = task / NB, blk = task % NB;
-                if (16 * blk < a.d) {
-                    const int64_t at = (group_slot(first, token >> 4, valid) + (token & 15)) * a.H + h;
-                    const uint32_t *c = (const uint32_t *)(a.k_codes + at * (a.d >> 1)) + 2 * blk;
-                    s.k[t] = *(const uint2v *)c;
-                    s.ks[t] = a.k_scales[at * (a.d >> 4) + blk];
-                }
-                const int pair = task / NE, part = task % NE;
-                if (8 * part < a.d) {
-                    const int64_t at = (group_slot(first, pair >> 3, valid) + ((2 * pair) & 15)) * a.H + h;
-                    const uint8_t *c = a.v_codes + at * (a.d >> 1) + 4 * part;
-                    s.v[t][0] = *(const uint32_t *)c;
-                    s.v[t][1] = *(const uint32_t *)(c + (int64_t)a.H * (a.d >> 1));
-                    const uint8_t *sc = a.v_scales + at * (a.d >> 4) + (part >> 1);
-                    s.vs[t] = (uint32_t)sc[0] | ((uint32_t)sc[(int64_t)a.H * (a.d >> 4)] << 16);
-                }
-            }
-        }
-        if (tid < kTileStep) {
-            bool valid;
-            const int64_t slot = group_slot(first, tid >> 4, valid);
-            s.valid = valid;
-            s.mean = smooth ? (uint32_t)a.k_mean[(slot + (tid & 15)) * a.H + h] : 0u;
-            const int64_t page = slot / a.page_tokens;
-            s.kg = k_global[page];
-            s.vg = v_global[page];
-        }
-    };
-    auto store = [&](const Share &s, int stage) {
-#pragma unroll
-        for (int t = 0; t < kTasks; ++t) {
-            const int task = tid + t * kThreads;
-            if (task < 4 * D) {
-                const int token = task / NB, blk = task % NB;
-                const half2v sk = scale_pair(s.ks[t] * 0x10001u);
-                *(half8v *)(lds.k[stage] + k_place<D>(token, 2 * blk)) = eight_codes(s.k[t].x, sk);
-                *(half8v *)(lds.k[stage] + k_place<D>(token, 2 * blk + 1)) = eight_codes(s.k[t].y, sk);
-                const int pair = task / NE, part = task % NE;
-                // nibbles of the two tokens side by side: byte j of `even` is element 2 j of both, of `odd` element 2 j + 1
-                const uint32_t even = (s.v[t][0] & 0x0F0F0F0Fu) | ((s.v[t][1] << 4) & 0xF0F0F0F0u);
-                const uint32_t odd = ((s.v[t][0] >> 4) & 0x0F0F0F0Fu) | (s.v[t][1] & 0xF0F0F0F0u);
-                const half2v sv = scale_pair(s.vs[t]);
-                // token 2 pair: of its sixteen in quarter (pair / 2) % 4; quarter 2 x + y goes to chunk y (of the sixteen's two), half x
-                const int quarter = (pair >> 1) & 3, chunk = 2 * (pair >> 3) + (quarter & 1);
-                const uint32_t in_chunk = (uint32_t)(8 * (quarter >> 1) + 4 * (pair & 1));
-                uint8_t *to = lds.v[stage] + in_chunk;
-                const int e = 8 * part;
-                *(half2v *)(to + v_place(e, chunk)) = code_pair<0>(even) * sv;
-                *(half2v *)(to + v_place(e + 1, chunk)) = code_pair<0>(odd) * sv;
-                *(half2v *)(to + v_place(e + 2, chunk)) = code_pair<1>(even) * sv;
-                *(half2v *)(to + v_place(e + 3, chunk)) = code_pair<1>(odd) * sv;
-                *(half2v *)(to + v_place(e + 4, chunk)) = code_pair<2>(even) * sv;
-                *(half2v *)(to + v_place(e + 5, chunk)) = code_pair<2>(odd) * sv;
-                *(half2v *)(to + v_place(e + 6, chunk)) = code_pair<3>(even) * sv;
-                *(half2v *)(to + v_place(e + 7, chunk)) = code_pair<3>(odd) * sv;
-            }
-        }
-        if (tid < kTileStep) {
-            lds.mean[stage][tid] = __uint_as_float(s.mean << 16);
-            if ((tid & 15) == 0) {
-                lds.kg[stage][tid >> 4] = s.kg;
-                lds.log_v[stage][tid >> 4] = __builtin_amdgcn_logf(s.vg);
-                lds.inv_v[stage][tid >> 4] = __builtin_amdgcn_rcpf(s.vg);
-                lds.valid[stage][tid >> 4] = s.valid;
-            }
-        }
-    };
 
     float m = kLowest, l = 0.0f;
     float16v o[D / 32];
@@ -196,94 +249,151 @@ __global__ __launch_bounds__(64 * WAVES, D == 256 ? 1 : 2) void attention_tiles_
 #pragma unroll
         for (int e = 0; e < 16; ++e) o[t][e] = 0.0f;
 
-    auto take = [&](int n, int stage) {
+    const bool busy = row0 + 32 * wave < n_q * a.G;        // (a wave behind the last row only loads)
+    // this lane's chunks: keys 2 c + hi of row c32 (+ 32), values 2 g + hi of row c32 (+ 32 c, whose key has bit 2 the other way where c is odd)
+    constexpr int KA = D / 16 < 8 ? D / 16 : 8;
+    uint32_t k_from[KA], v_from[4];
+#pragma unroll
+    for (int c = 0; c < KA; ++c) k_from[c] = (uint32_t)c32 * kKRow + (uint32_t)(((2 * c + hi) ^ (c32 & kKeyMask)) << 4);
+#pragma unroll
+    for (int g = 0; g < 4; ++g) v_from[g] = kVBase + (uint32_t)c32 * kVRow + (uint32_t)(((2 * g + hi) ^ c32 ^ (c32 >> 3)) & 7) * 16u;
+
+    constexpr int KF = D / 16, VF = D / 32, kDepth = KF < 8 ? KF : 8;      // fragments of a tile of keys, of sixteen tokens' values; keys read ahead
+    auto turn = [&](int n, auto stage_constant) {
+        using Stage = decltype(stage_constant);
+        using Other = std::integral_constant<int, 1 - Stage::value>;
+        constexpr int stage = Stage::value;
+        constexpr int kStore = kTasks * kPieces;
         const int first = steps.first_token(n, kTileStep);
-        float x[2][16];
-        const uint32_t all_valid = lds.valid[stage][0] & lds.valid[stage][1] & lds.valid[stage][2] & lds.valid[stage][3];
-#pragma unroll
-        for (int t = 0; t < 2; ++t) {
-            float16v acc;
-#pragma unroll
-            for (int e = 0; e < 16; ++e) acc[e] = 0.0f;
-#pragma unroll
-            for (int c = 0; c < D / 16; ++c) {
-                const half8v kf = *(const half8v *)(lds.k[stage] + k_place<D>(32 * t + c32, 2 * c + hi));
-                acc = __builtin_amdgcn_mfma_f32_32x32x16_f16(kf, q[c], acc, 0, 0, 0);
-            }
-            // acc[e]: token 32 t + 8 (e / 4) + 4 hi + e % 4
-#pragma unroll
-            for (int e4 = 0; e4 < 4; ++e4) {
-                const int group = 2 * t + (e4 >> 1);
-                const float f = factor * lds.kg[stage][group];
-                float4v add = {lds.log_v[stage][group], lds.log_v[stage][group], lds.log_v[stage][group], lds.log_v[stage][group]};
-                if (smooth) {
-                    const float4v mean = *(const float4v *)&lds.mean[stage][32 * t + 8 * e4 + 4 * hi];
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) add[e] = __builtin_fmaf(mean[e], sum_q, add[e]);
-                }
-#pragma unroll
-                for (int e = 0; e < 4; ++e) x[t][4 * e4 + e] = __builtin_fmaf(acc[4 * e4 + e], f, add[e]);
-            }
+        auto k_fragment = [&](auto f) {                        // fragment f: tile f / KF, chunk pair f % KF
+            constexpr int F = decltype(f)::value, t = F / KF, c = F % KF;
+            return *(const half8v *)(lds_bytes + k_from[c % KA] + (stage * kKStage + t * 32 * kKRow + c / KA * 256));
+        };
+        auto v_fragment = [&](auto f) {                        // fragment f: group f / VF, rows 32 (f % VF) on
+            constexpr int F = decltype(f)::value, g = F / VF, c = F % VF;
+            return *(const half8v *)(lds_bytes + v_from[g ^ ((c & 1) << 1)] + (stage * kVStage + c * 32 * kVRow));
+        };
+        if (!busy) {
+            each<kStore>([&](auto i) { store_piece(share, Other(), i); });
+            fetch(ahead, share, n + 3);
+            __syncthreads();
+            return;
         }
-        const bool masked = all_valid == 0u || first + kTileStep - 1 > seq.position(a, i0) ||
-                            (a.window > 0 && first <= seq.position(a, i1) - a.window);
+
+        // ---- S^T = K Q^T
+        half8v kf[kDepth];
+        float16v x[2];
+        each<kDepth>([&](auto f) { kf[decltype(f)::value] = k_fragment(f); });
+        float mean[2] = {0.0f, 0.0f};
+        if constexpr (SMOOTH) {
+            mean[0] = lds.mean[stage][c32];
+            mean[1] = lds.mean[stage][32 + c32];
+        }
+        const uint4v valid = *(const uint4v *)lds.valid[stage];
+        const float4v kg = *(const float4v *)lds.kg[stage], log_v = *(const float4v *)lds.log_v[stage], inv_v = *(const float4v *)lds.inv_v[stage];
+        NVFP4_FENCE;
+#pragma unroll
+        for (int t = 0; t < 2; ++t)
+#pragma unroll
+            for (int e = 0; e < 16; ++e) x[t][e] = 0.0f;
+        each<2 * KF>([&](auto f) {
+            constexpr int F = decltype(f)::value, t = F / KF;
+            x[t] = __builtin_amdgcn_mfma_f32_32x32x16_f16(kf[F % kDepth], q[F % KF], x[t], 0, 0, 0);
+            if constexpr (F + kDepth < 2 * KF) kf[F % kDepth] = k_fragment(std::integral_constant<int, F + kDepth>());
+            if constexpr (F == KF / 2 && SMOOTH) {
+                x[0] = __builtin_amdgcn_mfma_f32_32x32x2f32(mean[0], sum_q, x[0], 0, 0, 0);
+                x[1] = __builtin_amdgcn_mfma_f32_32x32x2f32(mean[1], sum_q, x[1], 0, 0, 0);
+            }
+            constexpr int p0 = F * kStore / (2 * KF), p1 = (F + 1) * kStore / (2 * KF);
+            each<p1 - p0>([&](auto i) { store_piece(share, Other(), std::integral_constant<int, p0 + decltype(i)::value>()); });
+            NVFP4_FENCE;
+        });
+        half8v vf[2][VF];
+        each<VF>([&](auto f) { vf[0][decltype(f)::value] = v_fragment(f); });
+        fetch(ahead, share, n + 3);
+
+        // ---- the row's maximum.  x[t][e]: token 32 t + 8 (e / 4) + 4 hi + e % 4, group 2 t + e / 8
+        const uint32_t all = __builtin_amdgcn_readfirstlane((int)(valid.x | valid.y << 1 | valid.z << 2 | valid.w << 3));
+        const bool masked = all != 15u || first + kTileStep - 1 > seq.position(a, i0) || (a.window > 0 && first <= seq.position(a, i1) - a.window);
         if (masked) {
 #pragma unroll
             for (int t = 0; t < 2; ++t)
 #pragma unroll
                 for (int e = 0; e < 16; ++e) {
                     const int at = 32 * t + 8 * (e >> 2) + 4 * hi + (e & 3);
-                    x[t][e] = (lds.valid[stage][2 * t + (e >> 3)] != 0u && seen(a, first + at, p)) ? x[t][e] : -__builtin_inff();
+                    const bool there = (all >> (2 * t + (e >> 3)) & 1u) != 0u;
+                    x[t][e] = (there & sight.of(first + at)) ? x[t][e] : -__builtin_inff();
                 }
         }
-        float top = kLowest;
+        float f[4], top = kLowest;
 #pragma unroll
-        for (int t = 0; t < 2; ++t)
-#pragma unroll
-            for (int e = 0; e < 16; e += 2) top = fmaxf(fmaxf(top, x[t][e]), x[t][e + 1]);
+        for (int g = 0; g < 4; ++g) {
+            f[g] = factor * kg[g];                               // (positive: the largest score is the largest product)
+            const float16v &v = x[g >> 1];
+            const int e = 8 * (g & 1);
+            const float t0 = fmaxf(fmaxf(v[e], v[e + 1]), v[e + 2]), t1 = fmaxf(fmaxf(v[e + 3], v[e + 4]), v[e + 5]);
+            top = fmaxf(top, __builtin_fmaf(fmaxf(fmaxf(t0, t1), fmaxf(v[e + 6], v[e + 7])), f[g], log_v[g]));
+        }
         if (__ballot(top > m + kSlack) != 0ull) {
             const float raised = fmaxf(fmaxf(top, __shfl_xor(top, 32, 64)), m);
-            const float f = __builtin_amdgcn_exp2f(m - raised);
+            const float r = __builtin_amdgcn_exp2f(m - raised);
             m = raised;
-            l *= f;
+            l *= r;
 #pragma unroll
-            for (int t = 0; t < D / 32; ++t) o[t] *= f;
+            for (int t = 0; t < VF; ++t) o[t] *= r;
         }
-#pragma unroll
-        for (int t = 0; t < 2; ++t)
-#pragma unroll
-            for (int s = 0; s < 2; ++s) {                        // sixteen tokens
-                half8v w, w_low;
-                float sum = 0.0f;
-#pragma unroll
-                for (int e = 0; e < 8; ++e) {
-                    const float v = __builtin_amdgcn_exp2f(x[t][8 * s + e] - m);
-                    sum += v;
-                    w[e] = (_Float16)v;
-                    if constexpr (F32) w_low[e] = (_Float16)(v - (float)w[e]);
-                }
-                l = __builtin_fmaf(sum, lds.inv_v[stage][2 * t + s], l);
-#pragma unroll
-                for (int c = 0; c < D / 32; ++c) {
-                    const half8v vf = *(const half8v *)(lds.v[stage] + v_place(32 * c + c32, 2 * (2 * t + s) + hi));
-                    o[c] = __builtin_amdgcn_mfma_f32_32x32x16_f16(vf, w, o[c], 0, 0, 0);
-                    if constexpr (F32) o[c] = __builtin_amdgcn_mfma_f32_32x32x16_f16(vf, w_low, o[c], 0, 0, 0);
-                }
+
+        // ---- weights, O^T = V^T P^T
+        half8v w[2], w_low[2];
+        float sum[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+        auto weights = [&](auto group, auto pair_constant) {   // two of a group's eight
+            constexpr int g = decltype(group)::value, e = 2 * decltype(pair_constant)::value;
+            const float add = log_v[g] - m;
+            const float v0 = __builtin_amdgcn_exp2f(__builtin_fmaf(x[g >> 1][8 * (g & 1) + e], f[g], add));
+            const float v1 = __builtin_amdgcn_exp2f(__builtin_fmaf(x[g >> 1][8 * (g & 1) + e + 1], f[g], add));
+            sum[g] += v0;
+            sum[g] += v1;
+            const half2v both = {(_Float16)v0, (_Float16)v1};
+            w[g & 1][e] = both.x;
+            w[g & 1][e + 1] = both.y;
+            if constexpr (F32) {
+                w_low[g & 1][e] = (_Float16)(v0 - (float)both.x);
+                w_low[g & 1][e + 1] = (_Float16)(v1 - (float)both.y);
             }
+        };
+        each<4>([&](auto i) { weights(std::integral_constant<int, 0>(), i); });
+        NVFP4_FENCE;
+        each<4>([&](auto group) {
+            constexpr int g = decltype(group)::value;
+            each<VF>([&](auto column) {
+                constexpr int c = decltype(column)::value;
+                if constexpr (g < 3) vf[(g + 1) & 1][c] = v_fragment(std::integral_constant<int, (g + 1) * VF + c>());
+                o[c] = __builtin_amdgcn_mfma_f32_32x32x16_f16(vf[g & 1][c], w[g & 1], o[c], 0, 0, 0);
+                if constexpr (F32) o[c] = __builtin_amdgcn_mfma_f32_32x32x16_f16(vf[g & 1][c], w_low[g & 1], o[c], 0, 0, 0);
+                if constexpr (g < 3) {
+                    constexpr int p0 = c * 4 / VF, p1 = (c + 1) * 4 / VF;
+                    each<p1 - p0>([&](auto i) { weights(std::integral_constant<int, g + 1>(), std::integral_constant<int, p0 + decltype(i)::value>()); });
+                }
+                NVFP4_FENCE;
+            });
+        });
+#pragma unroll
+        for (int g = 0; g < 4; ++g) l = __builtin_fmaf(sum[g], inv_v[g], l);
+        __syncthreads();
     };
 
+    // A turn reads one stage and writes the other; the barrier behind it says that both are done.  (What is fetched past the
+    // last step is the last step again.)
     if (n0 < n1) {
-        Share s;
-        fetch(n0, s);
-        store(s, 0);
+        using S0 = std::integral_constant<int, 0>;
+        using S1 = std::integral_constant<int, 1>;
+        each<kTasks * kPieces>([&](auto i) { store_piece(share, S0(), i); });
+        fetch(ahead, share, n0 + 2);
         __syncthreads();
-        for (int n = n0; n < n1; ++n) {
-            const int stage = (n - n0) & 1;
-            if (n + 1 < n1) fetch(n + 1, s);
-            take(n, stage);
-            // (the other stage was read in the turn before, which every wave has left behind the barrier)
-            if (n + 1 < n1) store(s, stage ^ 1);
-            __syncthreads();
+        for (int n = n0; n < n1; n += 2) {
+            turn(n, S0());
+            if (n + 1 >= n1) break;
+            turn(n + 1, S1());
         }
     }
 
@@ -306,21 +416,21 @@ __global__ __launch_bounds__(64 * WAVES, D == 256 ? 1 : 2) void attention_tiles_
             }
         return;
     }
-    const int64_t part = (int64_t)piece * a.total_q * a.Hq + out_row;
-    if (hi == 0) a.part_ml[part] = float2{m, l};
+    const int64_t part_row = (int64_t)piece * a.total_q * a.Hq + out_row;
+    if (hi == 0) a.part_ml[part_row] = float2{m, l};
 #pragma unroll
     for (int c = 0; c < D / 32; ++c)
 #pragma unroll
         for (int e = 0; e < 16; e += 4) {
             const int first = 32 * c + 2 * e + 4 * hi;
-            if (first < a.d) *(float4v *)(a.part_o + part * a.d + first) = float4v{o[c][e], o[c][e + 1], o[c][e + 2], o[c][e + 3]};
+            if (first < a.d) *(float4v *)(a.part_o + part_row * a.d + first) = float4v{o[c][e], o[c][e + 1], o[c][e + 2], o[c][e + 3]};
         }
 }
 
-template <int D, int WAVES, bool F32>
-static hipError_t launch_tiles(const AttentionArgs &a, const KvAttention &k, hipStream_t s)
+template <int D, int WAVES, bool SMOOTH, bool F32>
+static hipError_t launch_variant(const AttentionArgs &a, const KvAttention &k, hipStream_t s)
 {
-    auto kernel = attention_tiles_kernel<D, WAVES, F32>;
+    auto kernel = attention_tiles_kernel<D, WAVES, SMOOTH, F32>;
     constexpr int bytes = (int)sizeof(Tiles<D, WAVES>);
     static bool raised[64] = {};                                       // the dynamic LDS limit, once per device
     int dev = -1;
@@ -334,17 +444,18 @@ static hipError_t launch_tiles(const AttentionArgs &a, const KvAttention &k, hip
     kernel<<<grid, 64 * WAVES, bytes, s>>>(a, k.page_table, k.kv_lens, k.q_starts, k.cache.k_global, k.cache.v_global);
     return hipGetLastError();
 }
+template <int D, int WAVES>
+static hipError_t launch_tiles(const AttentionArgs &a, const KvAttention &k, hipStream_t s)
+{
+    if (a.k_mean) return k.out_f32 ? launch_variant<D, WAVES, true, true>(a, k, s) : launch_variant<D, WAVES, true, false>(a, k, s);
+    return k.out_f32 ? launch_variant<D, WAVES, false, true>(a, k, s) : launch_variant<D, WAVES, false, false>(a, k, s);
+}
 
 hipError_t launch_attention_tiles(const AttentionArgs &a, const KvAttention &k, hipStream_t s)
 {
-    const bool f = k.out_f32;
-    if (a.d > 128) return f ? launch_tiles<256, 4, true>(a, k, s) : launch_tiles<256, 4, false>(a, k, s);
-    if (a.plan.waves == 8) {
-        if (a.d <= 64) return f ? launch_tiles<64, 8, true>(a, k, s) : launch_tiles<64, 8, false>(a, k, s);
-        return f ? launch_tiles<128, 8, true>(a, k, s) : launch_tiles<128, 8, false>(a, k, s);
-    }
-    if (a.d <= 64) return f ? launch_tiles<64, 4, true>(a, k, s) : launch_tiles<64, 4, false>(a, k, s);
-    return f ? launch_tiles<128, 4, true>(a, k, s) : launch_tiles<128, 4, false>(a, k, s);
+    if (a.d > 128) return launch_tiles<256, 4>(a, k, s);
+    if (a.d <= 64) return launch_tiles<64, 4>(a, k, s);
+    return a.plan.waves == 8 ? launch_tiles<128, 8>(a, k, s) : launch_tiles<128, 4>(a, k, s);
 }
 
 }  // namespace nvfp4
