@@ -236,7 +236,7 @@ bool attention_sizes_ok(int64_t total_q, int64_t Hq, int64_t H, int64_t d, int64
 bool attention_grid_ok(const AttentionPlan &p, int64_t H, int64_t B)
 {
     if (p.rows16) return p.pieces + B + 8 <= kMaxIndex / p.groups;
-    return B * H <= kMaxIndex / p.pieces && B * H * p.pieces <= kMaxIndex / p.groups;
+    return B * H <= kMaxIndex / p.groups && p.whole + (p.rest + 8) * p.pieces <= kMaxIndex && p.rest * 32 * p.waves <= kMaxIndex;
 }
 
 }  // namespace

@@ -105,6 +105,28 @@ struct Pieces {
     }
 };
 
+// Blocks of rows (tiles): number `at` of all blocks <-> sequence, cached head and block.  Blocks that read the same tokens of
+// the same head are eight numbers apart, and so on one of the eight chiplets, each of which has an L2.
+struct Block {
+    int b, h, block;
+    __device__ __forceinline__ Block(const AttentionArgs &a, int64_t at)
+    {
+        const int64_t same = a.plan.groups, full = (int64_t)a.B * a.H & ~(int64_t)7;
+        int64_t set;
+        if (at < full * same) {
+            set = at / (8 * same) * 8 + (at & 7);
+            block = (int)((at >> 3) % same);
+        } else {
+            set = full + (at - full * same) / same;
+            block = (int)((at - full * same) % same);
+        }
+        h = (int)(set % a.H);
+        b = (int)(set / a.H);
+    }
+};
+// steps of a piece of a block that is cut
+__device__ __forceinline__ int tile_piece_steps(const AttentionArgs &a, int total) { return max((total + a.plan.pieces - 1) / a.plan.pieces, a.plan.piece_steps); }
+
 // What a query at position p sees: token j <= p, behind `after` or in front of the sink's end.
 struct Sight {
     int p, after, sink;

@@ -3,24 +3,41 @@
 
 namespace nvfp4 {
 
-// A workgroup takes a row (query, head): the pieces' maxima and sums first (every wave for itself, a lane a piece), then
+// Threads threads take a row (query, head): the pieces' maxima and sums first (every wave for itself, a lane a piece), then
 // their partial sums, d / 4 lanes to a piece, as many pieces side by side as there are lanes for.  Pieces are added in an
-// order that does not depend on when they finished.
-constexpr int kJoinThreads = 256;
+// order that does not depend on when they finished.  A wave a row where there are few pieces and many rows (chunks: 84480
+// rows in three pieces took 53 us, a workgroup to each 182), a workgroup where there are many pieces (single tokens: 256
+// rows in 50 pieces 9 us and 7).
+constexpr int kJoinThreads = 256, kJoinFew = 8;
+template <int THREADS>
 __global__ __launch_bounds__(kJoinThreads) void attention_join_kernel(const AttentionArgs a, const int32_t *__restrict__ kv_lens, const int32_t *__restrict__ q_starts,
                                                                       const float *__restrict__ part_o, const float2 *__restrict__ part_ml, int out_f32)
 {
-    __shared__ float4v sums[kJoinThreads];
-    const int lane = threadIdx.x & 63;
-    int64_t id = blockIdx.x;
-    const int head = (int)(id % a.Hq);
-    id /= a.Hq;
-    const int i = (int)(id % a.max_q), b = (int)(id / a.max_q);
+    __shared__ float4v sums[THREADS > 64 ? THREADS : 1];
+    const int lane = threadIdx.x & 63, tid = (int)threadIdx.x & (THREADS - 1);
+    const int64_t id = (int64_t)blockIdx.x * (kJoinThreads / THREADS) + __builtin_amdgcn_readfirstlane((int)threadIdx.x / THREADS);
+    int i, b, head, pieces;
+    int64_t first, stride;                                    // partial rows of this row: first + s * stride
+    if (a.plan.rows16) {
+        head = (int)(id % a.Hq);
+        i = (int)(id / a.Hq % a.max_q);
+        b = (int)(id / a.Hq / a.max_q);
+        if (b >= a.B) return;
+    } else {
+        const int rows = 32 * a.plan.waves;
+        const int64_t j = id / rows;
+        if (j >= a.plan.rest) return;
+        const Block place(a, a.plan.whole + j);
+        const int row = place.block * rows + (int)(id - j * rows);
+        i = row / a.G;
+        head = place.h * a.G + (row - i * a.G);
+        b = place.b;
+        first = j * a.plan.pieces * rows + (id - j * rows);
+        stride = rows;
+    }
     const Sequence seq(a, q_starts, kv_lens, b);
     const int n_q = min(seq.n_q, a.max_q);
     if (i >= n_q) return;
-    int pieces;
-    int64_t first, stride;                                    // partial rows of this row: first + s * stride
     const int64_t query = (int64_t)seq.start + i, out_row = query * a.Hq + head;
     if (a.plan.rows16) {
         const Pieces p(a, q_starts, kv_lens, b, true);
@@ -28,12 +45,10 @@ __global__ __launch_bounds__(kJoinThreads) void attention_join_kernel(const Atte
         first = ((int64_t)p.first * a.max_q + i) * a.Hq + head;
         stride = (int64_t)a.max_q * a.Hq;
     } else {
-        // the steps of the workgroup that had this row
         const int rows = 32 * a.plan.waves, row0 = (i * a.G + head % a.G) / rows * rows;
         const Steps steps(a, seq, row0 / a.G, min((row0 + rows - 1) / a.G, n_q - 1), kTileStep);
-        pieces = (steps.total + a.plan.piece_steps - 1) / a.plan.piece_steps;
-        first = out_row;
-        stride = (int64_t)a.total_q * a.Hq;
+        const int piece_steps = tile_piece_steps(a, steps.total);
+        pieces = (steps.total + piece_steps - 1) / piece_steps;
     }
     if (pieces <= 1) return;                                  // (written by its workgroup)
 
@@ -48,9 +63,9 @@ __global__ __launch_bounds__(kJoinThreads) void attention_join_kernel(const Atte
     }
 #pragma unroll
     for (int x = 32; x > 0; x >>= 1) l += __shfl_xor(l, x, 64);
-    const int lanes = a.d >> 2, side = kJoinThreads / lanes, sub = (int)threadIdx.x / lanes, e = 4 * ((int)threadIdx.x - sub * lanes);
+    const int lanes = THREADS > 64 ? a.d >> 2 : 64, side = THREADS / lanes, sub = tid / lanes, e = 4 * (tid - sub * lanes);
     float4v o = {0.0f, 0.0f, 0.0f, 0.0f};
-    if (sub < side) {
+    if (sub < side && e < a.d) {
 #pragma unroll 4
         for (int s = sub; s < pieces; s += side) {
             const int64_t row = first + s * stride;
@@ -58,21 +73,28 @@ __global__ __launch_bounds__(kJoinThreads) void attention_join_kernel(const Atte
             o += *(const float4v *)(part_o + row * a.d + e) * w;
         }
     }
-    sums[threadIdx.x] = o;
-    __syncthreads();
-    if (sub == 0) {
-        for (int s = 1; s < side; ++s) o += sums[s * lanes + (int)threadIdx.x];
+    if constexpr (THREADS > 64) {
+        sums[tid] = o;
+        __syncthreads();
+        if (sub == 0)
+            for (int s = 1; s < side; ++s) o += sums[s * lanes + tid];
+    }
+    if (sub == 0 && e < a.d) {
         o *= l > 0.0f ? 1.0f / l : 0.0f;
         const int64_t at = query * a.ldo + (int64_t)head * a.d + e;
         if (out_f32) *(float4v *)((float *)a.out + at) = o;
         else *(uint2v *)((uint16_t *)a.out + at) = uint2v{pack_bf16x2(o.x, o.y), pack_bf16x2(o.z, o.w)};
     }
-    if (a.lse && threadIdx.x == 0) a.lse[out_row] = l > 0.0f ? (m + __builtin_amdgcn_logf(l)) * 0.6931471805599453f : -__builtin_inff();
+    if (a.lse && tid == 0) a.lse[out_row] = l > 0.0f ? (m + __builtin_amdgcn_logf(l)) * 0.6931471805599453f : -__builtin_inff();
 }
 
 hipError_t launch_attention_join(const AttentionArgs &a, const KvAttention &k, hipStream_t s)
 {
-    attention_join_kernel<<<(unsigned)((int64_t)a.B * a.max_q * a.Hq), kJoinThreads, 0, s>>>(a, k.kv_lens, k.q_starts, a.part_o, a.part_ml, k.out_f32);
+    const int64_t rows = a.plan.rows16 ? (int64_t)a.B * a.max_q * a.Hq : a.plan.rest * 32 * a.plan.waves;
+    const bool few = !a.plan.rows16 && a.plan.pieces <= kJoinFew;
+    const unsigned grid = (unsigned)(few ? (rows + 3) / 4 : rows);
+    if (few) attention_join_kernel<64><<<grid, kJoinThreads, 0, s>>>(a, k.kv_lens, k.q_starts, a.part_o, a.part_ml, k.out_f32);
+    else attention_join_kernel<kJoinThreads><<<grid, kJoinThreads, 0, s>>>(a, k.kv_lens, k.q_starts, a.part_o, a.part_ml, k.out_f32);
     return hipGetLastError();
 }
 

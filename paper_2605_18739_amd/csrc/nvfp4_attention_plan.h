@@ -10,13 +10,15 @@ namespace nvfp4 {
 constexpr int kRows16Step = 32, kTileStep = 64;       // cached tokens of a step of either kernel
 // rows16: heads of a workgroup at most, workgroups that the chip holds at once, steps of a piece at least
 constexpr int kRows16Heads = 4, kRows16Slots = 512, kRows16MinSteps = 4;
+constexpr int kTileMinSteps = 8;                       // steps of a piece of the other kernel, at least
 
 struct AttentionPlan {
     bool rows16;            // at most 16 (query, head) rows a cached head: a wave per cached head and piece
     int waves;              // waves of a workgroup
     int groups;             // rows16: workgroups that a token's heads take; otherwise: blocks of rows of a cached head
-    int pieces;             // rows16: of all sequences together, about; otherwise of each.  1: no partial results
-    int piece_steps;        // steps of a piece (rows16: at least so many; the lengths, which the device knows, decide)
+    int pieces;             // rows16: of all sequences together, about; otherwise of a block of rows that is cut.  1: no partial results
+    int piece_steps;        // steps of a piece, at least (the lengths, which the device knows, decide)
+    int64_t whole, rest;    // blocks of rows (all sequences, heads) that are not cut, and those that are
     int64_t part_rows;      // (query, head) rows of partial results
 };
 
@@ -43,18 +45,23 @@ inline AttentionPlan attention_plan(int64_t total_q, int64_t Hq, int64_t H, int6
         p.waves = d > 64 && d <= 128 && rows > 128 ? 8 : 4;
         p.groups = (int)((rows + 32 * p.waves - 1) / (32 * p.waves));
         const int64_t steps = std::max<int64_t>(1, (max_kv + kTileStep - 1) / kTileStep);
+        // Workgroups that the chip holds at once: as many blocks of rows as fill it a whole number of times walk over all their
+        // tokens; what is left over is cut into pieces, so that it takes a part of a round instead of one of its own.  (A
+        // piece more costs a pass over its partial results; 336 blocks: 256 whole and 80 in three pieces each take 1.34
+        // rounds, all of them in three pieces as long, with four times the partial results.)
         const int64_t items = B * H * p.groups, slots = p.waves == 8 || d > 128 ? 256 : 512;
-        // as many pieces as make whole waves of workgroups (a piece more costs a pass over the partial results), with at
-        // least 8 steps each
+        const int64_t whole = items / slots * slots, rest = items - whole;
         int best = 1;
         double best_cost = 1e30;
-        for (int n = 1; n <= 64 && (n == 1 || steps / n >= 8); ++n) {
-            const double rounds = (double)((items * n + slots - 1) / slots), cost = rounds / n * (1.0 + 0.02 * (n > 1 ? n : 0));
+        for (int n = 1; rest > 0 && n <= 64 && (n == 1 || steps / n >= kTileMinSteps); ++n) {
+            const double cost = (double)((rest * n + slots - 1) / slots) / n * (1.0 + (n > 1 ? 0.02 * n : 0.0));
             if (cost < best_cost * 0.999) best = n, best_cost = cost;
         }
-        p.piece_steps = (int)((steps + best - 1) / best);
-        p.pieces = (int)((steps + p.piece_steps - 1) / p.piece_steps);
-        p.part_rows = p.pieces <= 1 ? 0 : p.pieces * total_q * Hq;
+        p.pieces = best;
+        p.piece_steps = kTileMinSteps;
+        p.whole = best > 1 ? whole : items;
+        p.rest = items - p.whole;
+        p.part_rows = p.rest * best * 32 * p.waves;
     }
     return p;
 }

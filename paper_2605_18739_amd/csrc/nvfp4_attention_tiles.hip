@@ -59,31 +59,25 @@ __global__ __launch_bounds__(64 * WAVES, D == 256 ? 1 : 2) void attention_tiles_
     constexpr int kThreads = Lds::kThreads, kTasks = Lds::kTasks, kRows = 32 * WAVES;
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), c32 = lane & 31, hi = lane >> 5;
 
-    // workgroups that read the same tokens of the same head follow each other on one of the eight chiplets (each has an L2)
-    int id = blockIdx.x, block, b, h, piece;
-    {
-        const int same = a.plan.groups, sets = a.B * a.H * a.plan.pieces, full = sets & ~7;
-        int set;
-        if (id < full * same) {
-            set = id / (8 * same) * 8 + (id & 7);
-            block = (id >> 3) % same;
-        } else {
-            id -= full * same;
-            set = full + id / same;
-            block = id % same;
-        }
-        h = set % a.H;
-        set /= a.H;
-        b = set % a.B;
-        piece = set / a.B;
+    // whole blocks first, then the pieces of the others: all first pieces, all second ones, ...
+    int64_t at = blockIdx.x;
+    int piece = -1;
+    if (at >= a.plan.whole) {
+        const int64_t rest = (a.plan.rest + 7) & ~(int64_t)7, j = at - a.plan.whole;
+        piece = (int)(j / rest);
+        if (j - piece * rest >= a.plan.rest) return;
+        at = a.plan.whole + (j - piece * rest);
     }
+    const Block place(a, at);
+    const int b = place.b, h = place.h, block = place.block;
     const Sequence seq(a, q_starts, kv_lens, b);
     const int n_q = min(seq.n_q, a.max_q), row0 = block * kRows;
     if (row0 >= n_q * a.G) return;
     const int i0 = row0 / a.G, i1 = min((row0 + kRows - 1) / a.G, n_q - 1);
     const Steps steps(a, seq, i0, i1, kTileStep);
-    const int n0 = piece * a.plan.piece_steps, n1 = min(n0 + a.plan.piece_steps, steps.total);
-    const bool alone = steps.total <= a.plan.piece_steps;
+    const int piece_steps = piece < 0 ? steps.total : tile_piece_steps(a, steps.total);
+    const bool alone = steps.total <= piece_steps;         // no partial results
+    const int n0 = max(piece, 0) * piece_steps, n1 = min(n0 + piece_steps, steps.total);
     if (n0 >= n1 && piece > 0) return;
 
     // ---- this lane's share of a step: blocks of keys (token, block) and pieces of values (pair of tokens, eight elements).
@@ -416,7 +410,7 @@ __global__ __launch_bounds__(64 * WAVES, D == 256 ? 1 : 2) void attention_tiles_
             }
         return;
     }
-    const int64_t part_row = (int64_t)piece * a.total_q * a.Hq + out_row;
+    const int64_t part_row = ((at - a.plan.whole) * a.plan.pieces + piece) * kRows + (32 * wave + c32);
     if (hi == 0) a.part_ml[part_row] = float2{m, l};
 #pragma unroll
     for (int c = 0; c < D / 32; ++c)
@@ -440,7 +434,7 @@ static hipError_t launch_variant(const AttentionArgs &a, const KvAttention &k, h
         if (hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void *>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, bytes)) return e;
         raised[dev] = true;
     }
-    const unsigned grid = (unsigned)((int64_t)a.plan.groups * a.B * a.H * a.plan.pieces);
+    const unsigned grid = (unsigned)(a.plan.whole + ((a.plan.rest + 7) & ~(int64_t)7) * a.plan.pieces);
     kernel<<<grid, 64 * WAVES, bytes, s>>>(a, k.page_table, k.kv_lens, k.q_starts, k.cache.k_global, k.cache.v_global);
     return hipGetLastError();
 }
