@@ -259,21 +259,31 @@ __global__ __launch_bounds__(kNormThreads) void norm_rope_backward_kernel(const 
     }
 }
 
-// dweight = the sum of the workgroups' partial sums: sixteen columns a workgroup, each in sixteen strided parts that are
-// added in order.
-__global__ __launch_bounds__(256) void norm_rope_weights_kernel(const float *__restrict__ partial, int n, int d, float *__restrict__ dwq,
-                                                                float *__restrict__ dwk)
+// dweight = the sum of the workgroups' partial sums: sixteen columns a workgroup, each in 64 strided parts (eight loads of
+// one in flight) that are added in order.  Bound by latency: 1024 partial sums of d = 64 (0.5 MB) take 6 us, of d = 128 8 us;
+// sixteen parts with one load in flight each took 15 and 21 us.
+constexpr int kWeightParts = 64;
+
+__global__ __launch_bounds__(16 * kWeightParts) void norm_rope_weights_kernel(const float *__restrict__ partial, int n, int d, float *__restrict__ dwq,
+                                                                              float *__restrict__ dwk)
 {
-    __shared__ float part[16][17];
+    __shared__ float part[kWeightParts][17];
     const int c = blockIdx.x * 16 + (threadIdx.x & 15), row = threadIdx.x >> 4;
-    float v = 0.0f;
-    for (int i = row; i < n; i += 16) v += partial[(int64_t)i * (2 * d) + c];      // (2 d is a multiple of 16)
-    part[row][threadIdx.x & 15] = v;
+    float v[8];
+#pragma unroll
+    for (int k = 0; k < 8; ++k) v[k] = 0.0f;
+    for (int i = row; i < n; i += 8 * kWeightParts)
+#pragma unroll
+        for (int k = 0; k < 8; ++k) {
+            const int at = i + k * kWeightParts;
+            if (at < n) v[k] += partial[(int64_t)at * (2 * d) + c];      // (2 d is a multiple of 16)
+        }
+    part[row][threadIdx.x & 15] = ((v[0] + v[1]) + (v[2] + v[3])) + ((v[4] + v[5]) + (v[6] + v[7]));
     __syncthreads();
     if (threadIdx.x < 16) {
         float sum = 0.0f;
 #pragma unroll
-        for (int i = 0; i < 16; ++i) sum += part[i][threadIdx.x];
+        for (int i = 0; i < kWeightParts; ++i) sum += part[i][threadIdx.x];
         float *dw = c < d ? dwq : dwk;
         if (dw) dw[c < d ? c : c - d] = sum;
     }
@@ -327,7 +337,7 @@ hipError_t launch_norm_rope_backward(NormRopeArgs a, int64_t T, float *dwq, floa
     else a.interleaved ? go(norm_rope_backward_kernel<32, true>) : go(norm_rope_backward_kernel<32, false>);
     if (hipError_t e = hipGetLastError()) return e;
     if (!weights) return hipSuccess;
-    norm_rope_weights_kernel<<<2 * a.d / 16, 256, 0, s>>>(partial, grid, a.d, dwq, dwk);
+    norm_rope_weights_kernel<<<2 * a.d / 16, 16 * kWeightParts, 0, s>>>(partial, grid, a.d, dwq, dwk);
     return hipGetLastError();
 }
 
