@@ -22,9 +22,11 @@ struct Tiles {
     static constexpr int kTasks = 4 * D / kThreads;       // blocks of keys, and pieces of values, of a lane
     uint8_t k[2][kTileStep * D * 2];      // [token][D] f16
     uint8_t v[2][D * kTileStep * 2];      // [element][token] f16
-    float mean[2][kTileStep];             // row mean / g_k
-    float kg[2][4], log_v[2][4], inv_v[2][4];       // of the four groups of sixteen tokens
-    uint32_t valid[2][4];
+    struct {
+        float mean[kTileStep];            // row mean / g_k
+        float kg[4], log_v[4], inv_v[4];  // of the four groups of sixteen tokens
+        uint32_t valid[4];
+    } of[2];
 };
 
 // (integral constants 0 .. N - 1, for code that has to be laid out by hand)
@@ -143,15 +145,15 @@ __global__ __launch_bounds__(64 * WAVES, D == 256 ? 1 : 2) void attention_tiles_
             const uint32_t page = s.valid[t] ? pages[t] : 0u;
             s.kg[t] = ((const uint32_t *)k_global)[page + zero];
             s.vg[t] = ((const uint32_t *)v_global)[page + zero];
-            const int64_t row = ((int64_t)page * a.page_tokens + now.offset[t]) * a.H;
-            const __amdgpu_buffer_rsrc_t vc = group(a.v_codes, row * (a.d >> 1), 16u * token_codes), vsc = group(a.v_scales, row * (a.d >> 4), 16u * token_scales);
-            s.k[t] = __builtin_amdgcn_raw_buffer_load_b64(group(a.k_codes, row * (a.d >> 1), 16u * token_codes), k_at, 0, 0);
-            s.ks[t] = __builtin_amdgcn_raw_buffer_load_b32(group(a.k_scales, row * (a.d >> 4), 16u * token_scales), ks_at, 0, 0);
+            const int64_t slot = (int64_t)page * a.page_tokens + now.offset[t], at = slot * token_scales;
+            const __amdgpu_buffer_rsrc_t vc = group(a.v_codes, at << 3, 16u * token_codes), vsc = group(a.v_scales, at, 16u * token_scales);
+            s.k[t] = __builtin_amdgcn_raw_buffer_load_b64(group(a.k_codes, at << 3, 16u * token_codes), k_at, 0, 0);
+            s.ks[t] = __builtin_amdgcn_raw_buffer_load_b32(group(a.k_scales, at, 16u * token_scales), ks_at, 0, 0);
             s.v[t][0] = __builtin_amdgcn_raw_buffer_load_b32(vc, v_at, 0, 0);
             s.v[t][1] = __builtin_amdgcn_raw_buffer_load_b32(vc, v_at, (int)token_codes, 0);
             s.vs[t][0] = __builtin_amdgcn_raw_buffer_load_b32(vsc, vs_at0, 0, 0);
             s.vs[t][1] = __builtin_amdgcn_raw_buffer_load_b32(vsc, vs_at1, 0, 0);
-            if constexpr (SMOOTH) s.mean[t] = __builtin_amdgcn_raw_buffer_load_b32(group(a.k_mean, 2 * row, 32u * (uint32_t)a.H), mean_at, 0, 0);
+            if constexpr (SMOOTH) s.mean[t] = __builtin_amdgcn_raw_buffer_load_b32(group(a.k_mean, slot * a.H * 2, 32u * (uint32_t)a.H), mean_at, 0, 0);
         }
         __builtin_amdgcn_sched_barrier(0);                 // (the loads stay in front of what follows)
     };
@@ -160,41 +162,40 @@ __global__ __launch_bounds__(64 * WAVES, D == 256 ? 1 : 2) void attention_tiles_
     constexpr uint32_t kKRow = 2 * D, kVRow = 2 * kTileStep, kKStage = kTileStep * kKRow, kVStage = D * kVRow, kVBase = 2 * kKStage;
     constexpr int kKeyMask = (D / 8 - 1) & 15;
     const int token0 = tid / NB, pair0 = tid / NE, quarter = (pair0 >> 1) & 3;
-    const uint32_t k_to = (uint32_t)token0 * kKRow + (uint32_t)(((2 * blk) ^ (token0 & kKeyMask)) << 4);     // (the block's second chunk: ^ 16)
+    uint32_t k_to = (uint32_t)token0 * kKRow + (uint32_t)(((2 * blk) ^ (token0 & kKeyMask)) << 4);     // (the block's second chunk: ^ 16)
     // tokens 2 pair and 2 pair + 1 of their sixteen lie in quarter (pair / 2) % 4; quarter 2 x + y goes to chunk y (of the sixteen's two), half x
-    const uint32_t v_to = kVBase + 8u * part * kVRow + (uint32_t)(((2 * group_of(0) + (quarter & 1)) ^ part) & 7) * 16u + 8u * (quarter >> 1) + 4u * (pair0 & 1);
+    uint32_t v_to = kVBase + 8u * part * kVRow + (uint32_t)(((2 * group_of(0) + (quarter & 1)) ^ part) & 7) * 16u + 8u * (quarter >> 1) + 4u * (pair0 & 1);
     constexpr int kPieces = 7;                             // of a task
     uint32_t even[kTasks], odd[kTasks];
     half2v sv[kTasks];
-    auto store_piece = [&](Share &s, auto stage_constant, auto piece_constant) {
-        constexpr int stage = decltype(stage_constant)::value, t = decltype(piece_constant)::value / kPieces, i = decltype(piece_constant)::value % kPieces;
-        constexpr uint32_t k_off = stage * kKStage + t * (kThreads / NB) * kKRow;
-        uint8_t *const lds_v = lds_bytes + stage * kVStage;
-        if constexpr (i == 0) {
+    // a stage is chosen by one bit of an address, so it is flipped by ^ kKStage, ^ kVStage; k_to, v_to point at the stage that
+    // is written, k_from, v_from at the one that is read
+    auto store_piece = [&](Share &s, int stage, auto piece_constant) {
+        constexpr int t = decltype(piece_constant)::value / kPieces, i = decltype(piece_constant)::value % kPieces;
+        constexpr uint32_t k_off = t * (kThreads / NB) * kKRow;
+        if constexpr (i < 2) {
             const half2v sk = scale_pair(__builtin_amdgcn_perm(0u, s.ks[t], ks_pick));
-            *(half8v *)(lds_bytes + k_to + k_off) = eight_codes(s.k[t].x, sk);
-        } else if constexpr (i == 1) {
-            const half2v sk = scale_pair(__builtin_amdgcn_perm(0u, s.ks[t], ks_pick));
-            *(half8v *)(lds_bytes + (k_to ^ 16u) + k_off) = eight_codes(s.k[t].y, sk);
+            *(half8v *)(lds_bytes + (k_to ^ (i == 0 ? 0u : 16u)) + k_off) = eight_codes(i == 0 ? s.k[t].x : s.k[t].y, sk);
         } else if constexpr (i == 2) {
             // nibbles of the two tokens side by side: byte j of `even` is element 2 j of both, of `odd` element 2 j + 1
             even[t] = (s.v[t][0] & 0x0F0F0F0Fu) | ((s.v[t][1] << 4) & 0xF0F0F0F0u);
             odd[t] = ((s.v[t][0] >> 4) & 0x0F0F0F0Fu) | (s.v[t][1] & 0xF0F0F0F0u);
             sv[t] = scale_pair(__builtin_amdgcn_perm(s.vs[t][1], s.vs[t][0], vs_pick));
             const float kg = __uint_as_float(s.kg[t]), vg = __uint_as_float(s.vg[t]);
-            if constexpr (SMOOTH)
-                if (blk == 0) lds.mean[stage][token0 + t * (kThreads / NB)] = __uint_as_float((s.mean[t] >> mean_shift) << 16) * __builtin_amdgcn_rcpf(kg);
-            if (token16 == 0 && blk == 0) {
-                lds.kg[stage][group_of(t)] = kg;
-                lds.log_v[stage][group_of(t)] = __builtin_amdgcn_logf(vg);
-                lds.inv_v[stage][group_of(t)] = __builtin_amdgcn_rcpf(vg);
-                lds.valid[stage][group_of(t)] = s.valid[t] ? 1u : 0u;
+            if (blk == 0) {
+                if constexpr (SMOOTH) lds.of[stage].mean[token0 + t * (kThreads / NB)] = __uint_as_float((s.mean[t] >> mean_shift) << 16) * __builtin_amdgcn_rcpf(kg);
+                if (token16 == 0) {
+                    lds.of[stage].kg[group_of(t)] = kg;
+                    lds.of[stage].log_v[group_of(t)] = __builtin_amdgcn_logf(vg);
+                    lds.of[stage].inv_v[group_of(t)] = __builtin_amdgcn_rcpf(vg);
+                    lds.of[stage].valid[group_of(t)] = s.valid[t] ? 1u : 0u;
+                }
             }
         } else {
             constexpr int b = i - 3;                       // elements 2 b and 2 b + 1 of the eight
             const uint32_t to = v_to ^ (uint32_t)((2 * (group_of(t) ^ group_of(0))) << 4);
-            *(half2v *)(lds_v + (to ^ (2 * b) << 4) + 2 * b * kVRow) = code_pair<b>(even[t]) * sv[t];
-            *(half2v *)(lds_v + (to ^ (2 * b + 1) << 4) + (2 * b + 1) * kVRow) = code_pair<b>(odd[t]) * sv[t];
+            *(half2v *)(lds_bytes + (to ^ (2 * b) << 4) + 2 * b * kVRow) = code_pair<b>(even[t]) * sv[t];
+            *(half2v *)(lds_bytes + (to ^ (2 * b + 1) << 4) + (2 * b + 1) * kVRow) = code_pair<b>(odd[t]) * sv[t];
         }
     };
 
@@ -245,32 +246,28 @@ __global__ __launch_bounds__(64 * WAVES, D == 256 ? 1 : 2) void attention_tiles_
 
     const bool busy = row0 + 32 * wave < n_q * a.G;        // (a wave behind the last row only loads)
     // this lane's chunks: keys 2 c + hi of row c32 (+ 32), values 2 g + hi of row c32 (+ 32 c, whose key has bit 2 the other way where c is odd)
-    constexpr int KA = D / 16 < 8 ? D / 16 : 8;
-    uint32_t k_from[KA], v_from[4];
-#pragma unroll
-    for (int c = 0; c < KA; ++c) k_from[c] = (uint32_t)c32 * kKRow + (uint32_t)(((2 * c + hi) ^ (c32 & kKeyMask)) << 4);
-#pragma unroll
-    for (int g = 0; g < 4; ++g) v_from[g] = kVBase + (uint32_t)c32 * kVRow + (uint32_t)(((2 * g + hi) ^ c32 ^ (c32 >> 3)) & 7) * 16u;
+    uint32_t k_from = (uint32_t)c32 * kKRow + (uint32_t)((hi ^ (c32 & kKeyMask)) << 4);
+    uint32_t v_from = kVBase + (uint32_t)c32 * kVRow + (uint32_t)((hi ^ c32 ^ (c32 >> 3)) & 7) * 16u;
 
-    constexpr int KF = D / 16, VF = D / 32, kDepth = KF < 8 ? KF : 8;      // fragments of a tile of keys, of sixteen tokens' values; keys read ahead
-    auto turn = [&](int n, auto stage_constant) {
-        using Stage = decltype(stage_constant);
-        using Other = std::integral_constant<int, 1 - Stage::value>;
-        constexpr int stage = Stage::value;
+    constexpr int KF = D / 16, VF = D / 32, NK = 2 * KF, kDepth = 8;       // fragments of a step's keys, of sixteen tokens' values; keys read ahead
+    auto k_fragment = [&](auto f) {                            // fragment f: tile f % 2, chunk pair f / 2
+        constexpr int F = decltype(f)::value, t = F & 1, c = F >> 1;
+        return *(const half8v *)(lds_bytes + (k_from ^ (uint32_t)((c & 7) << 5)) + (t * 32 * kKRow + (c >> 3) * 256));
+    };
+    auto v_fragment = [&](auto f) {                            // fragment f: group f / VF, rows 32 (f % VF) on
+        constexpr int F = decltype(f)::value, g = F / VF, c = F % VF;
+        return *(const half8v *)(lds_bytes + (v_from ^ (uint32_t)((g ^ ((c & 1) << 1)) << 5)) + c * 32 * kVRow);
+    };
+    auto turn = [&](int n, auto runs) {
+        const int stage = (n - n0) & 1;
+        const auto &of = lds.of[stage];
         constexpr int kStore = kTasks * kPieces;
         const int first = steps.first_token(n, kTileStep);
-        auto k_fragment = [&](auto f) {                        // fragment f: tile f / KF, chunk pair f % KF
-            constexpr int F = decltype(f)::value, t = F / KF, c = F % KF;
-            return *(const half8v *)(lds_bytes + k_from[c % KA] + (stage * kKStage + t * 32 * kKRow + c / KA * 256));
-        };
-        auto v_fragment = [&](auto f) {                        // fragment f: group f / VF, rows 32 (f % VF) on
-            constexpr int F = decltype(f)::value, g = F / VF, c = F % VF;
-            return *(const half8v *)(lds_bytes + v_from[g ^ ((c & 1) << 1)] + (stage * kVStage + c * 32 * kVRow));
-        };
-        if (!busy) {
-            each<kStore>([&](auto i) { store_piece(share, Other(), i); });
+        // (what is made from these is made again in every turn: kept, it would push the queries out of the registers)
+        as_loaded(k_to), as_loaded(v_to), as_loaded(k_from), as_loaded(v_from);
+        if constexpr (!decltype(runs)::value) {
+            each<kStore>([&](auto i) { store_piece(share, stage ^ 1, i); });
             fetch(ahead, share, n + 3);
-            __syncthreads();
             return;
         }
 
@@ -280,26 +277,23 @@ __global__ __launch_bounds__(64 * WAVES, D == 256 ? 1 : 2) void attention_tiles_
         each<kDepth>([&](auto f) { kf[decltype(f)::value] = k_fragment(f); });
         float mean[2] = {0.0f, 0.0f};
         if constexpr (SMOOTH) {
-            mean[0] = lds.mean[stage][c32];
-            mean[1] = lds.mean[stage][32 + c32];
+            mean[0] = of.mean[c32];
+            mean[1] = of.mean[32 + c32];
         }
-        const uint4v valid = *(const uint4v *)lds.valid[stage];
-        const float4v kg = *(const float4v *)lds.kg[stage], log_v = *(const float4v *)lds.log_v[stage], inv_v = *(const float4v *)lds.inv_v[stage];
+        const uint4v valid = *(const uint4v *)of.valid;
+        const float4v kg = *(const float4v *)of.kg, log_v = *(const float4v *)of.log_v, inv_v = *(const float4v *)of.inv_v;
         NVFP4_FENCE;
 #pragma unroll
         for (int t = 0; t < 2; ++t)
 #pragma unroll
             for (int e = 0; e < 16; ++e) x[t][e] = 0.0f;
-        each<2 * KF>([&](auto f) {
-            constexpr int F = decltype(f)::value, t = F / KF;
-            x[t] = __builtin_amdgcn_mfma_f32_32x32x16_f16(kf[F % kDepth], q[F % KF], x[t], 0, 0, 0);
-            if constexpr (F + kDepth < 2 * KF) kf[F % kDepth] = k_fragment(std::integral_constant<int, F + kDepth>());
-            if constexpr (F == KF / 2 && SMOOTH) {
-                x[0] = __builtin_amdgcn_mfma_f32_32x32x2f32(mean[0], sum_q, x[0], 0, 0, 0);
-                x[1] = __builtin_amdgcn_mfma_f32_32x32x2f32(mean[1], sum_q, x[1], 0, 0, 0);
-            }
-            constexpr int p0 = F * kStore / (2 * KF), p1 = (F + 1) * kStore / (2 * KF);
-            each<p1 - p0>([&](auto i) { store_piece(share, Other(), std::integral_constant<int, p0 + decltype(i)::value>()); });
+        each<NK>([&](auto f) {
+            constexpr int F = decltype(f)::value, t = F & 1, c = F >> 1;
+            x[t] = __builtin_amdgcn_mfma_f32_32x32x16_f16(kf[F % kDepth], q[c], x[t], 0, 0, 0);
+            if constexpr (F + kDepth < NK) kf[F % kDepth] = k_fragment(std::integral_constant<int, F + kDepth>());
+            if constexpr (SMOOTH && c == KF / 2) x[t] = __builtin_amdgcn_mfma_f32_32x32x2f32(mean[t], sum_q, x[t], 0, 0, 0);
+            constexpr int p0 = F * kStore / NK, p1 = (F + 1) * kStore / NK;
+            each<p1 - p0>([&](auto i) { store_piece(share, stage ^ 1, std::integral_constant<int, p0 + decltype(i)::value>()); });
             NVFP4_FENCE;
         });
         half8v vf[2][VF];
@@ -373,22 +367,24 @@ __global__ __launch_bounds__(64 * WAVES, D == 256 ? 1 : 2) void attention_tiles_
         });
 #pragma unroll
         for (int g = 0; g < 4; ++g) l = __builtin_fmaf(sum[g], inv_v[g], l);
-        __syncthreads();
     };
 
     // A turn reads one stage and writes the other; the barrier behind it says that both are done.  (What is fetched past the
     // last step is the last step again.)
     if (n0 < n1) {
-        using S0 = std::integral_constant<int, 0>;
-        using S1 = std::integral_constant<int, 1>;
-        each<kTasks * kPieces>([&](auto i) { store_piece(share, S0(), i); });
+        each<kTasks * kPieces>([&](auto i) { store_piece(share, 0, i); });
         fetch(ahead, share, n0 + 2);
+        k_to ^= kKStage, v_to ^= kVStage;
         __syncthreads();
-        for (int n = n0; n < n1; n += 2) {
-            turn(n, S0());
-            if (n + 1 >= n1) break;
-            turn(n + 1, S1());
-        }
+        auto walk = [&](auto runs) {
+            for (int n = n0; n < n1; ++n) {
+                turn(n, runs);
+                k_to ^= kKStage, v_to ^= kVStage, k_from ^= kKStage, v_from ^= kVStage;
+                __syncthreads();
+            }
+        };
+        if (busy) walk(std::true_type());
+        else walk(std::false_type());
     }
 
     l += __shfl_xor(l, 32, 64);
