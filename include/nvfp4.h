@@ -398,8 +398,8 @@ int nvfp4_qk_norm_rope_backward(const nvfp4_heads_grad *q, const nvfp4_heads_gra
  *   k_codes, v_codes    [n_pages, page_tokens, H, d/2]    k_scales, v_scales [n_pages, page_tokens, H, d/16]
  *   k_global, v_global  [n_pages] fp32, positive and finite for every page in use
  *   k_mean              bf16 [n_pages, page_tokens, H]: row means of smoothed keys (Eq. 6), or NULL: keys are not smoothed
- * All device memory of the caller, codes, scales and means 16-byte aligned.  page_tokens % 16 == 0, d % 16 == 0, d <= 256.  Slot s is token s % page_tokens of page
- * s / page_tokens.
+ * All device memory of the caller, codes, scales and means 16-byte aligned.  page_tokens % 16 == 0, d % 16 == 0, d <= 256.
+ * Slot s is token s % page_tokens of page s / page_tokens.
  */
 typedef struct nvfp4_kv_cache {
     uint8_t *k_codes, *k_scales;
@@ -446,7 +446,9 @@ int nvfp4_kv_cache_read(const nvfp4_kv_cache *cache, const int64_t *slots, int64
  *     over other tokens
  * A query that sees nothing gets zeros and lse = -inf.  Rows of out and lse that no sequence owns are left as they were.
  * Scores, their maxima and sums and the accumulation are fp32; the probabilities enter the second product as f16, relative
- * to the row's running maximum (2^-11 of each; below 2^-24 of the largest they vanish).
+ * to the row's running maximum (2^-11 of each; for fp32 output as the sum of two f16 numbers, 2^-22; below 2^-24 of the largest
+ * they vanish).
+ * Refused (NVFP4_ERR_SHAPE) besides the above: more than 2^30 pages, and pages whose block scales or row means fill 4 GiB.
  * workspace: nvfp4_kv_attention_workspace_bytes() bytes, 16-byte aligned (0 bytes: may be NULL): partial results where the
  * cache is split over workgroups.
  */

@@ -697,6 +697,8 @@ int nvfp4_kv_attention(const void *q_bf16, int64_t ldq, int64_t total_q, int64_t
     if (int rc = fill_pages(cache, &a.cache)) return rc;
     const int64_t H = a.cache.H, d = a.cache.d;
     if (max_pages <= 0 || max_pages > kMaxIndex / a.cache.page_tokens) return NVFP4_ERR_SHAPE;
+    // (a page's scales and means are addressed with 32 bits, and so is a list of one word a page)
+    if (a.cache.n_pages > (1ll << 30) || a.cache.page_tokens * H * std::max<int64_t>(d >> 4, 2) >= (1ll << 32)) return NVFP4_ERR_SHAPE;
     const int64_t max_kv = max_pages * a.cache.page_tokens;
     max_q = std::min(max_q, total_q);
     if (!attention_sizes_ok(total_q, Hq, H, d, max_kv, B, max_q)) return NVFP4_ERR_SHAPE;

@@ -22,6 +22,33 @@ struct AttentionArgs {
     float *part_o;                        // [partial row][d], partial sums relative to ...
     float2 *part_ml;                      // [partial row] their row's maximum (base 2) and sum
     Divisor by_page;
+    uint32_t token_codes, token_scales;   // bytes of a slot: codes, scales
+    uint32_t page_scales, page_means;     // bytes of a page: scales, means
+};
+
+// Sixteen cached tokens of a page: where their slots begin in each plane, as scalar bases for a lane's 32-bit offset.  (Two
+// 32 x 32 bit products give them all, codes being eight times as long as scales.)
+using GlobalBytes = const __attribute__((address_space(1))) uint8_t *;
+// (the compiler must not add a lane's offset to the base's parts in another order: that takes a 64-bit vector addition a load)
+__device__ __forceinline__ GlobalBytes scalar_base(const void *base, uint64_t at)
+{
+    GlobalBytes p = (GlobalBytes)base + at;
+    asm("" : "+s"(p));
+    return p;
+}
+template <class T>
+__device__ __forceinline__ T load_at(GlobalBytes base, uint32_t offset) { return *(const __attribute__((address_space(1))) T *)(base + offset); }
+struct Slots {
+    GlobalBytes k_codes, v_codes, k_scales, v_scales, k_mean;
+    __device__ __forceinline__ Slots(const AttentionArgs &a, uint32_t page, int offset)
+    {
+        const uint64_t at = (uint64_t)page * a.page_scales + (uint32_t)offset * a.token_scales;
+        k_codes = scalar_base(a.k_codes, at << 3);
+        v_codes = scalar_base(a.v_codes, at << 3);
+        k_scales = scalar_base(a.k_scales, at);
+        v_scales = scalar_base(a.v_scales, at);
+        k_mean = scalar_base(a.k_mean, (uint64_t)page * a.page_means + (uint32_t)offset * (2u * (uint32_t)a.H));
+    }
 };
 
 // Queries and cached tokens of a sequence (clamped to what the call describes), and the steps of kStep tokens that some

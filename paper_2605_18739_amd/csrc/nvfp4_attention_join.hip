@@ -130,6 +130,10 @@ hipError_t launch_kv_attention(const KvAttention &k, void *workspace, hipStream_
     a.plan = attention_plan(k.total_q, k.Hq, c.H, c.d, k.max_pages * c.page_tokens, k.B, k.max_q, k.window, k.sink);
     a.part_o = static_cast<float *>(workspace);
     a.part_ml = reinterpret_cast<float2 *>(a.part_o + a.plan.part_rows * c.d);
+    a.token_codes = (uint32_t)(c.H * (c.d >> 1));
+    a.token_scales = (uint32_t)(c.H * (c.d >> 4));
+    a.page_scales = (uint32_t)c.page_tokens * a.token_scales;
+    a.page_means = (uint32_t)c.page_tokens * 2u * (uint32_t)c.H;
     a.by_page = Divisor(c.page_tokens, k.max_pages * c.page_tokens);
     const hipError_t e = a.plan.rows16 ? launch_attention_rows16(a, k, s) : launch_attention_tiles(a, k, s);
     if (e != hipSuccess || a.plan.pieces <= 1) return e;

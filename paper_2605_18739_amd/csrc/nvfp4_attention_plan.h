@@ -8,7 +8,9 @@
 namespace nvfp4 {
 
 constexpr int kRows16Step = 32, kTileStep = 64;       // cached tokens of a step of either kernel
-// rows16: heads of a workgroup at most, workgroups that the chip holds at once, steps of a piece at least
+// rows16: heads of a workgroup at most, workgroups of a call, steps of a piece at least.  Two workgroups to a compute unit up to
+// d = 128 and one above (whose registers leave room for one): eight caches of up to 16384 tokens, d = 64 / 128 / 256: 512
+// workgroups take 17.0 / 20.4 / 40.9 us, 256 18.6 / 21.2 / 33.4.
 constexpr int kRows16Heads = 4, kRows16Slots = 512, kRows16MinSteps = 4;
 constexpr int kTileMinSteps = 8;                       // steps of a piece of the other kernel, at least
 
@@ -38,7 +40,7 @@ inline AttentionPlan attention_plan(int64_t total_q, int64_t Hq, int64_t H, int6
         // as many pieces as the chip holds at once (one that waits for another to end doubles the time of a short call): the
         // sequences are cut to a common length, so every one of them may add a shorter piece to those of full length
         const int64_t most = B * ((steps + kRows16MinSteps - 1) / kRows16MinSteps);
-        p.pieces = (int)std::min(std::max<int64_t>(kRows16Slots / p.groups - B, std::min<int64_t>(B, 64)), most);
+        p.pieces = (int)std::min(std::max<int64_t>((d > 128 ? kRows16Slots / 2 : kRows16Slots) / p.groups - B, std::min<int64_t>(B, 64)), most);
         if (steps <= kRows16MinSteps) p.pieces = 1;
         p.part_rows = p.pieces <= 1 ? 0 : (p.pieces + B) * max_q * Hq;
     } else {

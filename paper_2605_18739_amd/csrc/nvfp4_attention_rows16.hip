@@ -19,23 +19,30 @@ namespace nvfp4 {
 //                 rescaling never cross lanes.
 // SMOOTH: the keys' row means enter as an outer product of their own, (mean / g_k) x (sum of the query's elements), by one
 // v_mfma_f32_16x16x4_f32 into the accumulator that the codes are then added to.
-// FULL: d = D.  Otherwise elements from d on load from the row's start and take a scale of zero.
+// FULL: d = D.  Otherwise lanes of elements from d on load the row's first ones (finite, and the queries are zero there).
 // The loop's loads are whole aligned words without branches, so that the compiler can count them: a step's loads are in
 // flight while the one before is multiplied, and the pages of the step behind it are looked up.  Scale bytes and means come
 // as the word that holds them (slots start at multiples of sixteen rows, so which byte it is does not change from step to
 // step, and the planes' sizes are multiples of sixteen bytes: no word reaches past the end).
+// The same word is asked for once where lanes share it: a step takes 16 loads, and lanes hand scales and means on (d = 128;
+// with a load for every lane's own, 28 loads: 41 us where this takes 39, d = 80 24 -> 22).
+// Measured (eight caches of up to 28672 tokens, 114688 together, 32 query heads of 8 cached, d = 128, smoothed keys, 134 MB): 39 us and
+// 7 to join, 3.4 TB/s; 7 us of it before the first product (launch, lengths, pages, first loads, queries), the rest 4.3 TB/s.  A
+// third buffer of loads, three workgroups to a compute unit and codes that go through LDS to load rows in order changed nothing
+// (40, 39, 38 us); with every page the same one, and so from L2, 33 us.
 template <int D, bool FULL>
 struct Step {
     static constexpr int KW = D / 32;                      // key words of a lane
-    static constexpr int KS = FULL ? 1 : D / 64;           // words with scale bytes of its blocks
-    uint32_t k[2][KW], ks[2][KS], v[8], v_hi[D == 256 ? 8 : 1], vs[8], mean[2];
-    uint32_t kg[2], vg[2];                                 // the pages' scales (fp32)
+    static constexpr int KS = D / 64;                      // words with scale bytes: FULL: of a token, otherwise of a lane's blocks
+    static constexpr int SW = D == 256 ? 2 : 1;            // FULL: of these, words that a lane loads
+    uint32_t k[2][KW], ks[FULL ? 1 : 2][FULL ? SW : KS], v[8], v_hi[D == 256 ? 8 : 1], vs[FULL ? SW : 8], mean[FULL ? 1 : 2];
+    uint32_t kg, vg;                                       // the pages' scales (fp32): lanes 0-31 of the first group's page, the others of the second's
     int first;                                             // the step's first token
     bool valid[2];                                         // the group of sixteen lies on a page of the cache
 };
 
 template <int D, bool FULL, bool SMOOTH, bool F32>
-__global__ __launch_bounds__(64 * kRows16Heads) void attention_rows16_kernel(const AttentionArgs a, const int32_t *__restrict__ page_table,
+__global__ __launch_bounds__(64 * kRows16Heads, D == 256 ? 1 : 2) void attention_rows16_kernel(const AttentionArgs a, const int32_t *__restrict__ page_table,
                                                                const int32_t *__restrict__ kv_lens, const int32_t *__restrict__ q_starts,
                                                                const float *__restrict__ k_global, const float *__restrict__ v_global)
 {
@@ -59,103 +66,131 @@ __global__ __launch_bounds__(64 * kRows16Heads) void attention_rows16_kernel(con
     // ---- pages of a step, and what a lane loads of it, as offsets from the group's first slot.
     // Pages and their scales are the same for the whole wave, but they come through vector loads like the rest: those return
     // in order, so that waiting for one of them does not wait for what was asked for after it.
-    uint32_t zero;                                         // (an offset that the compiler takes for a lane's own)
-    asm("v_mov_b32 %0, 0" : "=v"(zero));
     struct Ahead {
         int first, offset[2];
-        uint32_t page[2];
+        uint32_t page;                                     // lanes 0-31: of the first group, the others: of the second
     };
+    const bool second = lane >= 32;
+    const GlobalBytes table = scalar_base(page_table, (uint64_t)b * a.max_pages * 4), k_scale = scalar_base(k_global, 0), v_scale = scalar_base(v_global, 0);
     auto look_up = [&](int n) {
         Ahead p;
         p.first = steps.first_token(min(n, n1 - 1), kRows16Step);
+        uint32_t at[2];
 #pragma unroll
         for (int x = 0; x < 2; ++x) {  // (a group past the length is masked; it may be past the table: the step's first group stands in)
             const int token = p.first + 16 * x < seq.len ? p.first + 16 * x : p.first;
-            const int at = (int)a.by_page.small((uint32_t)token);
-            p.offset[x] = token - at * a.page_tokens;
-            p.page[x] = ((const uint32_t *)page_table)[(int64_t)b * a.max_pages + at + zero];
+            at[x] = a.by_page.small((uint32_t)token);
+            p.offset[x] = token - (int)at[x] * a.page_tokens;
         }
+        p.page = load_at<uint32_t>(table, 4u * (second ? at[1] : at[0]));
         return p;
     };
-    const uint32_t token_codes = (uint32_t)a.H * (uint32_t)(d >> 1), token_scales = (uint32_t)a.H * (uint32_t)(d >> 4);
+    const uint32_t token_codes = a.token_codes, token_scales = a.token_scales;
     const uint32_t head_codes = (uint32_t)h * (uint32_t)(d >> 1), head_scales = (uint32_t)h * (uint32_t)(d >> 4);
-    constexpr uint32_t kOutside = 0x7FFFFF00u;             // (loads behind the sixteen tokens give zeros)
     constexpr uint32_t kZero = 0x0Cu;                      // (of a byte permutation: zero)
     constexpr int KB = D / 64;                             // blocks of a lane's key part
-    uint32_t k_at[KB], ks_at[Step<D, FULL>::KS], ks_pick[KB];      // offsets, and the scales' bytes in their words (twice, for both halves of a register)
+    // (lanes of elements from d on load the row's first ones: the queries are zero there, and those sums are not stored)
+    uint32_t k_at[KB], ks_at[KB], ks_pick[KB];      // offsets, and the scales' bytes in their words (twice, for both halves of a register)
 #pragma unroll
     for (int c = 0; c < KB; ++c) {
-        const int blk = g * KB + c;
-        const bool in = FULL || 16 * blk < d;
-        k_at[c] = in ? r * token_codes + head_codes + 8u * blk : kOutside;
+        const uint32_t blk = FULL || 16 * (g * KB + c) < d ? g * KB + c : 0;
+        k_at[c] = r * token_codes + head_codes + 8u * blk;
         const uint32_t at = r * token_scales + head_scales + blk;
-        if (!FULL || c == 0) ks_at[FULL ? 0 : c] = in ? at & ~3u : kOutside;
+        ks_at[c] = at & ~3u;
         ks_pick[c] = (at & 3u) * 0x10001u | kZero << 8 | kZero << 24;
     }
-    const int v_element = r * NT;                          // the lane's elements of a value row
-    const bool v_in = FULL || v_element < d;
-    const uint32_t v_at = v_in ? 4 * g * token_codes + head_codes + ((uint32_t)(v_element >> 1) & ~3u) : kOutside;
+    const int v_element = FULL || r * NT < d ? r * NT : 0;                   // the lane's elements of a value row
     const uint32_t v_shift = D == 64 ? (uint32_t)(v_element & 4) * 4u : 0u;
-    uint32_t vs_at[4], vs_pick[2];
+    uint32_t v_at[4], vs_at[4], vs_pick[2];
 #pragma unroll
     for (int t = 0; t < 4; ++t) {
+        v_at[t] = (4 * g + t) * token_codes + head_codes + ((uint32_t)(v_element >> 1) & ~3u);
         const uint32_t at = (4 * g + t) * token_scales + head_scales + (uint32_t)(v_element >> 4);
-        vs_at[t] = v_in ? at & ~3u : kOutside;
+        vs_at[t] = at & ~3u;
         if (t & 1) vs_pick[t >> 1] |= ((at & 3u) + 4u) << 16 | kZero << 24;
         else vs_pick[t >> 1] = (at & 3u) | kZero << 8;
     }
-    const uint32_t mean_at = ((uint32_t)(r * a.H + h) * 2u) & ~3u, mean_shift = ((uint32_t)(r * a.H + h) & 1u) * 16u;
+    uint32_t mean_at = ((uint32_t)(r * a.H + h) * 2u) & ~3u;
+    const uint32_t mean_shift = ((uint32_t)(r * a.H + h) & 1u) * 16u;
+    // FULL: the scales of the step's 32 tokens are loaded once, a lane taking word lane_word of token lane_token (and the next
+    // one), the means a lane each, and handed from lane to lane: a lane needs the word with its blocks of token r (+ 16), and
+    // that with block r D / 256 of its eight tokens (times four: the exchange counts bytes)
+    constexpr int kTokenLanes = D == 64 ? 1 : 2;
+    const int lane_token = D == 64 ? lane & 31 : lane >> 1;
+    uint32_t scales_at = (lane_token & 15) * token_scales + head_scales + (D == 64 ? 0u : 4u * (lane & 1) * Step<D, FULL>::SW);
+    const uint32_t ks_from = 4u * (r * kTokenLanes + (D == 64 ? 0 : g >> 1)), vs_from = 4u * (4 * g * kTokenLanes + (D == 64 ? 0 : r >> 3));
+    auto from_lane = [](uint32_t lane4, uint32_t v) { return (uint32_t)__builtin_amdgcn_ds_bpermute((int)lane4, (int)v); };
     auto as_loaded = [](uint32_t &v) { asm volatile("" : "+v"(v)); };
-    // sixteen tokens of a plane, as a buffer: addresses are a scalar base and a lane's 32-bit offset
-    auto group = [](const void *base, int64_t at, uint32_t bytes) {
-        return __builtin_amdgcn_make_buffer_rsrc((void *)((const uint8_t *)base + at), 0, (int)bytes, 0x00020000);
-    };
     // fetches the step whose pages were looked up, and looks up those of step n
     auto fetch = [&](Ahead &p, Step<D, FULL> &s, int n) {
-        uint32_t pages[2];
-#pragma unroll
-        for (int x = 0; x < 2; ++x) {
-            as_loaded(p.page[x]);
-            pages[x] = (uint32_t)__builtin_amdgcn_readfirstlane((int)p.page[x]);
-        }
+        as_loaded(p.page);
+        uint32_t pages[2] = {(uint32_t)__builtin_amdgcn_readfirstlane((int)p.page), (uint32_t)__builtin_amdgcn_readlane((int)p.page, 32)};
         const Ahead now = p;
         p = look_up(n);
+        // (offsets are widened where they are used: widened once in front of the loop, they would no longer be known to have 32 bits)
+        if constexpr (FULL) as_loaded(scales_at);
+        as_loaded(mean_at);
+#pragma unroll
+        for (int c = 0; c < KB; ++c) {
+            if (!FULL || c == 0) as_loaded(k_at[c]);
+            if constexpr (!FULL) as_loaded(ks_at[c]);
+        }
+#pragma unroll
+        for (int t = 0; t < 4; ++t) {
+            as_loaded(v_at[t]);
+            if constexpr (!FULL) as_loaded(vs_at[t]);
+        }
         s.first = now.first;
 #pragma unroll
         for (int x = 0; x < 2; ++x) {
             s.valid[x] = pages[x] < (uint32_t)a.n_pages;
-            const uint32_t page = s.valid[x] ? pages[x] : 0u;
-            s.kg[x] = ((const uint32_t *)k_global)[page + zero];
-            s.vg[x] = ((const uint32_t *)v_global)[page + zero];
-            const int64_t row = ((int64_t)page * a.page_tokens + now.offset[x]) * a.H;
-            const __amdgpu_buffer_rsrc_t kc = group(a.k_codes, row * (d >> 1), 16u * token_codes), vc = group(a.v_codes, row * (d >> 1), 16u * token_codes);
-            const __amdgpu_buffer_rsrc_t ksc = group(a.k_scales, row * (d >> 4), 16u * token_scales), vsc = group(a.v_scales, row * (d >> 4), 16u * token_scales);
+            pages[x] = s.valid[x] ? pages[x] : 0u;
+        }
+        const Slots both[2] = {Slots(a, pages[0], now.offset[0]), Slots(a, pages[1], now.offset[1])};
+        const uint32_t page4 = 4u * (second ? pages[1] : pages[0]);
+        s.kg = load_at<uint32_t>(k_scale, page4);
+        s.vg = load_at<uint32_t>(v_scale, page4);
+        if constexpr (FULL) {
+            const GlobalBytes ks = lane_token < 16 ? both[0].k_scales : both[1].k_scales, vs = lane_token < 16 ? both[0].v_scales : both[1].v_scales;
+#pragma unroll
+            for (int c = 0; c < Step<D, FULL>::SW; ++c) {
+                s.ks[0][c] = load_at<uint32_t>(ks, scales_at + 4u * c);
+                s.vs[c] = load_at<uint32_t>(vs, scales_at + 4u * c);
+            }
+            if constexpr (SMOOTH) s.mean[0] = load_at<uint32_t>((lane & 16) ? both[1].k_mean : both[0].k_mean, mean_at);
+        }
+#pragma unroll
+        for (int x = 0; x < 2; ++x) {
+            const Slots &at = both[x];
+            if constexpr (!FULL) {
+#pragma unroll
+                for (int c = 0; c < KB; ++c) s.ks[x][c] = load_at<uint32_t>(at.k_scales, ks_at[c]);
+                if constexpr (SMOOTH) s.mean[x] = load_at<uint32_t>(at.k_mean, mean_at);
+            }
             if constexpr (FULL && D >= 128) {
 #pragma unroll
                 for (int c = 0; c < KB; c += 2) {
-                    const uint4v w = __builtin_amdgcn_raw_buffer_load_b128(kc, k_at[c], 0, 0);
-                    s.k[x][2 * c] = w.x; s.k[x][2 * c + 1] = w.y; s.k[x][2 * c + 2] = w.z; s.k[x][2 * c + 3] = w.w;
+                    const uint4v w = load_at<uint4v>(at.k_codes, k_at[0] + 8u * c);
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) s.k[x][2 * c + i] = w[i];
                 }
             } else {
 #pragma unroll
                 for (int c = 0; c < KB; ++c) {
-                    const uint2v w = __builtin_amdgcn_raw_buffer_load_b64(kc, k_at[c], 0, 0);
+                    const uint2v w = load_at<uint2v>(at.k_codes, k_at[c]);
                     s.k[x][2 * c] = w.x; s.k[x][2 * c + 1] = w.y;
                 }
             }
 #pragma unroll
-            for (int c = 0; c < Step<D, FULL>::KS; ++c) s.ks[x][c] = __builtin_amdgcn_raw_buffer_load_b32(ksc, ks_at[c], 0, 0);
-            if constexpr (SMOOTH) s.mean[x] = __builtin_amdgcn_raw_buffer_load_b32(group(a.k_mean, 2 * row, 32u * (uint32_t)a.H), mean_at, 0, 0);
-#pragma unroll
             for (int t = 0; t < 4; ++t) {
                 const int m = 4 * x + t;
-                if constexpr (D < 256) s.v[m] = __builtin_amdgcn_raw_buffer_load_b32(vc, v_at, t * (int)token_codes, 0);
+                if constexpr (D < 256) s.v[m] = load_at<uint32_t>(at.v_codes, v_at[t]);
                 else {
-                    const uint2v w = __builtin_amdgcn_raw_buffer_load_b64(vc, v_at, t * (int)token_codes, 0);
+                    const uint2v w = load_at<uint2v>(at.v_codes, v_at[t]);
                     s.v[m] = w.x;
                     s.v_hi[m] = w.y;
                 }
-                s.vs[m] = __builtin_amdgcn_raw_buffer_load_b32(vsc, vs_at[t], 0, 0);
+                if constexpr (!FULL) s.vs[m] = load_at<uint32_t>(at.v_scales, vs_at[t]);
             }
         }
         __builtin_amdgcn_sched_barrier(0);                 // (the loads stay in front of what follows)
@@ -210,32 +245,68 @@ __global__ __launch_bounds__(64 * kRows16Heads) void attention_rows16_kernel(con
     //  or mask of a loaded value would wait for all of them there)
     auto take = [&](Step<D, FULL> &s) {
         float x[8];
-        float inv_v[2];
+        as_loaded(s.kg), as_loaded(s.vg);
 #pragma unroll
         for (int t = 0; t < 2; ++t) {
 #pragma unroll
             for (int c = 0; c < Step<D, FULL>::KW; ++c) as_loaded(s.k[t][c]);
+            if constexpr (!FULL) {
 #pragma unroll
-            for (int c = 0; c < Step<D, FULL>::KS; ++c) as_loaded(s.ks[t][c]);
-            if constexpr (SMOOTH) as_loaded(s.mean[t]);
-            as_loaded(s.kg[t]);
-            as_loaded(s.vg[t]);
+                for (int c = 0; c < KB; ++c) as_loaded(s.ks[t][c]);
+                if constexpr (SMOOTH) as_loaded(s.mean[t]);
+            }
         }
+        uint32_t kw[2], vw[8];                                 // FULL: words with this lane's scales
+        float mean[2] = {0.0f, 0.0f};
+        if constexpr (FULL) {
+#pragma unroll
+            for (int c = 0; c < Step<D, FULL>::SW; ++c) as_loaded(s.ks[0][c]), as_loaded(s.vs[c]);
+            if constexpr (SMOOTH) as_loaded(s.mean[0]);
+            auto word = [&](const uint32_t (&v)[Step<D, FULL>::SW], uint32_t from, bool odd) {
+                const uint32_t w = from_lane(from, v[0]);
+                if constexpr (D < 256) return w;
+                else {
+                    const uint32_t w1 = from_lane(from, v[1]);         // (every lane takes part in both)
+                    return odd ? w1 : w;
+                }
+            };
+#pragma unroll
+            for (int t = 0; t < 2; ++t) {
+                kw[t] = word(s.ks[0], ks_from + 64u * kTokenLanes * t, g & 1);
+                if constexpr (SMOOTH) mean[t] = __uint_as_float(from_lane(4u * (16 * t + r), s.mean[0] >> mean_shift << 16));
+            }
+#pragma unroll
+            for (int t = 0; t < 8; ++t) vw[t] = word(s.vs, vs_from + 4u * kTokenLanes * (16 * (t >> 2) + (t & 3)), (r >> 2) & 1);
+        } else if constexpr (SMOOTH) {
+#pragma unroll
+            for (int t = 0; t < 2; ++t) mean[t] = __uint_as_float(s.mean[t] >> mean_shift << 16);
+        }
+        // of the two pages: scale, its inverse (keys), logarithm and inverse (values)
+        auto of_pages = [](float v, float (&two)[2]) {
+            two[0] = __uint_as_float((uint32_t)__builtin_amdgcn_readfirstlane((int)__float_as_uint(v)));
+            two[1] = __uint_as_float((uint32_t)__builtin_amdgcn_readlane((int)__float_as_uint(v), 32));
+        };
+        float f[2], inv_k[2], log_v[2], inv_v[2];
+        of_pages(__uint_as_float(s.kg), f);
+        if constexpr (SMOOTH) of_pages(__builtin_amdgcn_rcpf(__uint_as_float(s.kg)), inv_k);
+        of_pages(__builtin_amdgcn_logf(__uint_as_float(s.vg)), log_v);
+        of_pages(__builtin_amdgcn_rcpf(__uint_as_float(s.vg)), inv_v);
+        auto key_word = [&](int t, int c) {
+            if constexpr (FULL) return kw[t];
+            else return s.ks[t][c];
+        };
 #pragma unroll
         for (int t = 0; t < 2; ++t) {
-            const float kg = __uint_as_float(s.kg[t]), vg = __uint_as_float(s.vg[t]);
             float4v acc = {0.0f, 0.0f, 0.0f, 0.0f};
             if constexpr (SMOOTH)
-                acc = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float((s.mean[t] >> mean_shift) << 16) * __builtin_amdgcn_rcpf(kg), sum_q, acc, 0, 0, 0);
+                acc = __builtin_amdgcn_mfma_f32_16x16x4f32(mean[t] * inv_k[t], sum_q, acc, 0, 0, 0);
 #pragma unroll
             for (int c = 0; c < KD / 8; ++c) {             // block of the lane's word c: c / 2
-                const half2v sk = scale_pair(__builtin_amdgcn_perm(0u, s.ks[t][FULL ? 0 : c >> 1], ks_pick[c >> 1]));
+                const half2v sk = scale_pair(__builtin_amdgcn_perm(0u, key_word(t, c >> 1), ks_pick[c >> 1]));
                 acc = __builtin_amdgcn_mfma_f32_16x16x32_f16(eight_codes(s.k[t][c], sk), q[c], acc, 0, 0, 0);
             }
-            const float log_v = __builtin_amdgcn_logf(vg), f = factor * kg;
-            inv_v[t] = __builtin_amdgcn_rcpf(vg);
 #pragma unroll
-            for (int e = 0; e < 4; ++e) x[4 * t + e] = __builtin_fmaf(acc[e], f, log_v);
+            for (int e = 0; e < 4; ++e) x[4 * t + e] = __builtin_fmaf(acc[e], factor * f[t], log_v[t]);
         }
         // tokens that some row does not see (the same for the whole wave)
         const bool masked = !(s.valid[0] & s.valid[1]) || s.first + kRows16Step - 1 > seq.p0 ||
@@ -274,12 +345,15 @@ __global__ __launch_bounds__(64 * kRows16Heads) void attention_rows16_kernel(con
 #pragma unroll
         for (int t = 0; t < 8; ++t) {
             as_loaded(s.v[t]);
-            as_loaded(s.vs[t]);
+            if constexpr (!FULL) {
+                as_loaded(s.vs[t]);
+                vw[t] = s.vs[t];
+            }
             if constexpr (D == 256) as_loaded(s.v_hi[t]);
         }
         half2v sv[4];
 #pragma unroll
-        for (int t = 0; t < 4; ++t) sv[t] = scale_pair(__builtin_amdgcn_perm(s.vs[2 * t + 1], s.vs[2 * t], vs_pick[t & 1]));
+        for (int t = 0; t < 4; ++t) sv[t] = scale_pair(__builtin_amdgcn_perm(vw[2 * t + 1], vw[2 * t], vs_pick[t & 1]));
         // nibbles of two tokens side by side: byte k of `even` holds element 2k of both, of `odd` element 2k + 1
         auto half_row = [&](const uint32_t (&v)[8], auto first_column) {
             constexpr int first = decltype(first_column)::value;

@@ -87,22 +87,24 @@ __global__ __launch_bounds__(64 * WAVES, D == 256 ? 1 : 2) void attention_tiles_
     // through vector loads, which return in order, and it is looked up a step ahead of its use.
     constexpr int NB = D / 16, NE = D / 8;
     static_assert(4 * D >= kThreads, "every lane has a task");
-    const uint32_t token_codes = (uint32_t)a.H * (uint32_t)(a.d >> 1), token_scales = (uint32_t)a.H * (uint32_t)(a.d >> 4);
-    constexpr uint32_t kOutside = 0x7FFFFF00u;             // (loads behind the sixteen tokens give zeros: elements from d on)
+    const uint32_t token_codes = a.token_codes, token_scales = a.token_scales;
     constexpr uint32_t kZero = 0x0Cu;                      // (of a byte permutation: zero)
     uint32_t zero;                                         // (an offset that the compiler takes for a lane's own)
     asm("v_mov_b32 %0, 0" : "=v"(zero));
     // offsets within a group: a lane's task has the same place in each of its groups
     const int token16 = (tid / NB) & 15, blk = tid % NB, pair8 = (tid / NE) & 7, part = tid % NE;
-    const bool k_in = 16 * blk < a.d, v_in = 8 * part < a.d;
-    const uint32_t k_at = k_in ? token16 * token_codes + (uint32_t)h * (uint32_t)(a.d >> 1) + 8u * blk : kOutside;
-    const uint32_t ks_byte = token16 * token_scales + (uint32_t)h * (uint32_t)(a.d >> 4) + blk;
-    const uint32_t ks_at = k_in ? ks_byte & ~3u : kOutside, ks_pick = (ks_byte & 3u) * 0x10001u | kZero << 8 | kZero << 24;
-    const uint32_t v_at = v_in ? 2 * pair8 * token_codes + (uint32_t)h * (uint32_t)(a.d >> 1) + 4u * part : kOutside;
-    const uint32_t vs_byte0 = 2 * pair8 * token_scales + (uint32_t)h * (uint32_t)(a.d >> 4) + (part >> 1), vs_byte1 = vs_byte0 + token_scales;
-    const uint32_t vs_at0 = v_in ? vs_byte0 & ~3u : kOutside, vs_at1 = v_in ? vs_byte1 & ~3u : kOutside;
+    // (lanes of elements from d on load the row's first ones: the queries are zero there, and those sums are not stored)
+    const uint32_t k_blk = 16 * blk < a.d ? blk : 0, v_part = 8 * part < a.d ? part : 0;
+    uint32_t k_at = token16 * token_codes + (uint32_t)h * (uint32_t)(a.d >> 1) + 8u * k_blk;
+    const uint32_t ks_byte = token16 * token_scales + (uint32_t)h * (uint32_t)(a.d >> 4) + k_blk;
+    uint32_t ks_at = ks_byte & ~3u;
+    const uint32_t ks_pick = (ks_byte & 3u) * 0x10001u | kZero << 8 | kZero << 24;
+    uint32_t v_at0 = 2 * pair8 * token_codes + (uint32_t)h * (uint32_t)(a.d >> 1) + 4u * v_part, v_at1 = v_at0 + token_codes;
+    const uint32_t vs_byte0 = 2 * pair8 * token_scales + (uint32_t)h * (uint32_t)(a.d >> 4) + (v_part >> 1), vs_byte1 = vs_byte0 + token_scales;
+    uint32_t vs_at0 = vs_byte0 & ~3u, vs_at1 = vs_byte1 & ~3u;
     const uint32_t vs_pick = (vs_byte0 & 3u) | ((vs_byte1 & 3u) + 4u) << 16 | kZero << 8 | kZero << 24;
-    const uint32_t mean_at = ((uint32_t)(token16 * a.H + h) * 2u) & ~3u, mean_shift = ((uint32_t)(token16 * a.H + h) & 1u) * 16u;
+    uint32_t mean_at = ((uint32_t)(token16 * a.H + h) * 2u) & ~3u;
+    const uint32_t mean_shift = ((uint32_t)(token16 * a.H + h) & 1u) * 16u;
     struct Share {
         uint2v k[kTasks];
         uint32_t ks[kTasks], v[kTasks][2], vs[kTasks][2], mean[kTasks], kg[kTasks], vg[kTasks];
@@ -114,9 +116,7 @@ __global__ __launch_bounds__(64 * WAVES, D == 256 ? 1 : 2) void attention_tiles_
     };
     auto group_of = [&](int t) { return (64 * wave + t * kThreads) / (16 * NB); };
     auto as_loaded = [](uint32_t &v) { asm volatile("" : "+v"(v)); };
-    auto group = [](const void *base, int64_t at, uint32_t bytes) {
-        return __builtin_amdgcn_make_buffer_rsrc((void *)((const uint8_t *)base + at), 0, (int)bytes, 0x00020000);
-    };
+    const GlobalBytes table = scalar_base(page_table, (uint64_t)b * a.max_pages * 4), k_scale = scalar_base(k_global, 0), v_scale = scalar_base(v_global, 0);
     auto look_up = [&](int n) {
         Ahead p;
         const int first = steps.first_token(min(n, n1 - 1), kTileStep);
@@ -125,7 +125,7 @@ __global__ __launch_bounds__(64 * WAVES, D == 256 ? 1 : 2) void attention_tiles_
             const int token = first + 16 * group_of(t) < seq.len ? first + 16 * group_of(t) : first;
             const int at = (int)a.by_page.small((uint32_t)token);
             p.offset[t] = token - at * a.page_tokens;
-            p.page[t] = ((const uint32_t *)page_table)[(int64_t)b * a.max_pages + at + zero];
+            p.page[t] = load_at<uint32_t>(table, 4u * (uint32_t)at + zero);
         }
         return p;
     };
@@ -139,21 +139,22 @@ __global__ __launch_bounds__(64 * WAVES, D == 256 ? 1 : 2) void attention_tiles_
         }
         const Ahead now = p;
         p = look_up(n);
+        // (offsets are widened where they are used: widened once in front of the loop, they would no longer be known to have 32 bits)
+        as_loaded(k_at), as_loaded(ks_at), as_loaded(v_at0), as_loaded(v_at1), as_loaded(vs_at0), as_loaded(vs_at1), as_loaded(mean_at);
 #pragma unroll
         for (int t = 0; t < kTasks; ++t) {
             s.valid[t] = pages[t] < (uint32_t)a.n_pages;
             const uint32_t page = s.valid[t] ? pages[t] : 0u;
-            s.kg[t] = ((const uint32_t *)k_global)[page + zero];
-            s.vg[t] = ((const uint32_t *)v_global)[page + zero];
-            const int64_t slot = (int64_t)page * a.page_tokens + now.offset[t], at = slot * token_scales;
-            const __amdgpu_buffer_rsrc_t vc = group(a.v_codes, at << 3, 16u * token_codes), vsc = group(a.v_scales, at, 16u * token_scales);
-            s.k[t] = __builtin_amdgcn_raw_buffer_load_b64(group(a.k_codes, at << 3, 16u * token_codes), k_at, 0, 0);
-            s.ks[t] = __builtin_amdgcn_raw_buffer_load_b32(group(a.k_scales, at, 16u * token_scales), ks_at, 0, 0);
-            s.v[t][0] = __builtin_amdgcn_raw_buffer_load_b32(vc, v_at, 0, 0);
-            s.v[t][1] = __builtin_amdgcn_raw_buffer_load_b32(vc, v_at, (int)token_codes, 0);
-            s.vs[t][0] = __builtin_amdgcn_raw_buffer_load_b32(vsc, vs_at0, 0, 0);
-            s.vs[t][1] = __builtin_amdgcn_raw_buffer_load_b32(vsc, vs_at1, 0, 0);
-            if constexpr (SMOOTH) s.mean[t] = __builtin_amdgcn_raw_buffer_load_b32(group(a.k_mean, slot * a.H * 2, 32u * (uint32_t)a.H), mean_at, 0, 0);
+            s.kg[t] = load_at<uint32_t>(k_scale, 4u * page + zero);
+            s.vg[t] = load_at<uint32_t>(v_scale, 4u * page + zero);
+            const Slots at(a, page, now.offset[t]);
+            s.k[t] = load_at<uint2v>(at.k_codes, k_at);
+            s.ks[t] = load_at<uint32_t>(at.k_scales, ks_at);
+            s.v[t][0] = load_at<uint32_t>(at.v_codes, v_at0);
+            s.v[t][1] = load_at<uint32_t>(at.v_codes, v_at1);
+            s.vs[t][0] = load_at<uint32_t>(at.v_scales, vs_at0);
+            s.vs[t][1] = load_at<uint32_t>(at.v_scales, vs_at1);
+            if constexpr (SMOOTH) s.mean[t] = load_at<uint32_t>(at.k_mean, mean_at);
         }
         __builtin_amdgcn_sched_barrier(0);                 // (the loads stay in front of what follows)
     };

@@ -178,3 +178,10 @@ def test_host_tensors_are_refused():
     for call in calls:
         with pytest.raises((AssertionError, RuntimeError)):           # (RuntimeError: a machine without any GPU)
             call()
+
+
+def test_attention_refuses_pages_past_its_addresses():
+    assert attention(cache(n_pages=(1 << 30) + 1, page_tokens=16, H=1, d=16)) == SHAPE
+    assert attention(cache(n_pages=1, page_tokens=1 << 28, H=2, d=128), max_pages=1, q=P + 2) == SHAPE      # 2^28 tokens of 2 x 8 scales
+    assert attention(cache(n_pages=1, page_tokens=1 << 28, H=8, d=16), max_pages=1, q=P + 2) == SHAPE       # 2^28 tokens of 8 means
+    assert attention(cache(n_pages=1, page_tokens=1 << 26, H=2, d=128), max_pages=1, Hq=8, q=P + 2) == ALIGN
