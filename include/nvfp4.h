@@ -396,7 +396,7 @@ int nvfp4_qk_norm_rope_backward(const nvfp4_heads_grad *q, const nvfp4_heads_gra
  * neighbouring pages, can be filled by the chunk quantizers above (a page that all of a latent frame fills, its scale from
  * the frame's maximum) as well as token by token:
  *   k_codes, v_codes    [n_pages, page_tokens, H, d/2]    k_scales, v_scales [n_pages, page_tokens, H, d/16]
- *   k_global, v_global  [n_pages] fp32, positive and finite for every page in use
+ *   k_global, v_global  [n_pages] fp32, positive normal numbers for every page in use
  *   k_mean              bf16 [n_pages, page_tokens, H]: row means of smoothed keys (Eq. 6), or NULL: keys are not smoothed
  * All device memory of the caller, codes, scales and means 16-byte aligned.  page_tokens % 16 == 0, d % 16 == 0, d <= 256.
  * Slot s is token s % page_tokens of page s / page_tokens.

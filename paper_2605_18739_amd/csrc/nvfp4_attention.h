@@ -26,15 +26,20 @@ struct AttentionArgs {
     uint32_t page_scales, page_means;     // bytes of a page: scales, means
 };
 
+// A page's tensor scale.  Pages that are not in use may hold anything: where a step touches one its tokens are masked, and a
+// scale of one keeps NaN and infinities out of the sums that they enter with weight zero.
+__device__ __forceinline__ float page_scale(uint32_t bits)
+{
+    return __uint_as_float(bits - 0x00800000u < 0x7F000000u ? bits : 0x3F800000u);      // (positive and normal)
+}
+
 // Sixteen cached tokens of a page: where their slots begin in each plane, as scalar bases for a lane's 32-bit offset.  (Two
 // 32 x 32 bit products give them all, codes being eight times as long as scales.)
 using GlobalBytes = const __attribute__((address_space(1))) uint8_t *;
 // (the compiler must not add a lane's offset to the base's parts in another order: that takes a 64-bit vector addition a load)
 __device__ __forceinline__ GlobalBytes scalar_base(const void *base, uint64_t at)
 {
-    GlobalBytes p = (GlobalBytes)base + at;
-    asm("" : "+s"(p));
-    return p;
+    return (GlobalBytes)base + at;
 }
 template <class T>
 __device__ __forceinline__ T load_at(GlobalBytes base, uint32_t offset) { return *(const __attribute__((address_space(1))) T *)(base + offset); }

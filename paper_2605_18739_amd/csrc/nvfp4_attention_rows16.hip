@@ -286,11 +286,12 @@ __global__ __launch_bounds__(64 * kRows16Heads, D == 256 ? 1 : 2) void attention
             two[0] = __uint_as_float((uint32_t)__builtin_amdgcn_readfirstlane((int)__float_as_uint(v)));
             two[1] = __uint_as_float((uint32_t)__builtin_amdgcn_readlane((int)__float_as_uint(v), 32));
         };
+        const float kg = page_scale(s.kg), vg = page_scale(s.vg);
         float f[2], inv_k[2], log_v[2], inv_v[2];
-        of_pages(__uint_as_float(s.kg), f);
-        if constexpr (SMOOTH) of_pages(__builtin_amdgcn_rcpf(__uint_as_float(s.kg)), inv_k);
-        of_pages(__builtin_amdgcn_logf(__uint_as_float(s.vg)), log_v);
-        of_pages(__builtin_amdgcn_rcpf(__uint_as_float(s.vg)), inv_v);
+        of_pages(kg, f);
+        if constexpr (SMOOTH) of_pages(__builtin_amdgcn_rcpf(kg), inv_k);
+        of_pages(__builtin_amdgcn_logf(vg), log_v);
+        of_pages(__builtin_amdgcn_rcpf(vg), inv_v);
         auto key_word = [&](int t, int c) {
             if constexpr (FULL) return kw[t];
             else return s.ks[t][c];

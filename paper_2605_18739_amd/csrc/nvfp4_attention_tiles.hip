@@ -182,8 +182,8 @@ __global__ __launch_bounds__(64 * WAVES, D == 256 ? 1 : 2) void attention_tiles_
             even[t] = (s.v[t][0] & 0x0F0F0F0Fu) | ((s.v[t][1] << 4) & 0xF0F0F0F0u);
             odd[t] = ((s.v[t][0] >> 4) & 0x0F0F0F0Fu) | (s.v[t][1] & 0xF0F0F0F0u);
             sv[t] = scale_pair(__builtin_amdgcn_perm(s.vs[t][1], s.vs[t][0], vs_pick));
-            const float kg = __uint_as_float(s.kg[t]), vg = __uint_as_float(s.vg[t]);
             if (blk == 0) {
+                const float kg = page_scale(s.kg[t]), vg = page_scale(s.vg[t]);
                 if constexpr (SMOOTH) lds.of[stage].mean[token0 + t * (kThreads / NB)] = __uint_as_float((s.mean[t] >> mean_shift) << 16) * __builtin_amdgcn_rcpf(kg);
                 if (token16 == 0) {
                     lds.of[stage].kg[group_of(t)] = kg;
