@@ -448,7 +448,8 @@ int nvfp4_kv_cache_read(const nvfp4_kv_cache *cache, const int64_t *slots, int64
  * Scores, their maxima and sums and the accumulation are fp32; the probabilities enter the second product as f16, relative
  * to the row's running maximum (2^-11 of each; for fp32 output as the sum of two f16 numbers, 2^-22; below 2^-24 of the largest
  * they vanish).
- * Refused (NVFP4_ERR_SHAPE) besides the above: more than 2^30 pages, and pages whose block scales or row means fill 4 GiB.
+ * Refused (NVFP4_ERR_SHAPE) besides the above: more than 2^30 pages, pages whose block scales or row means fill 4 GiB, and
+ * more rows or sequences than one launch covers (2^32 lanes).
  * workspace: nvfp4_kv_attention_workspace_bytes() bytes, 16-byte aligned (0 bytes: may be NULL): partial results where the
  * cache is split over workgroups.
  */

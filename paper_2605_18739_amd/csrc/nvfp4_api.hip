@@ -139,6 +139,8 @@ static_assert(kRopeMaxAxes == NVFP4_ROPE_MAX_AXES);
 inline bool aligned(const void *p, size_t bytes) { return (reinterpret_cast<uintptr_t>(p) & (bytes - 1)) == 0; }
 constexpr int64_t kMaxIndex = 1ll << 30;                       // tokens, rows and units that kernels count in 32 bits
 constexpr int64_t kMaxRow = 1ll << 24;                         // elements of a token (all heads)
+constexpr int64_t kMaxLanes = 0xFFFFFFFFll;                    // of a launch
+constexpr int64_t kMaxWaves = (1ll << 26) - 64;                // (and so waves of one, whole workgroups of up to four)
 
 bool head_size_ok(int64_t H, int64_t d)
 {
@@ -171,7 +173,7 @@ int fill_rope(const nvfp4_rope *rope, int64_t d, NormRopeArgs *a)
 }
 int fill_norm(int64_t T, int64_t d, float eps, bool normed, NormRopeArgs *a)
 {
-    if (T <= 0 || T > kMaxIndex) return NVFP4_ERR_SHAPE;
+    if (T <= 0 || T > kMaxWaves - 8192) return NVFP4_ERR_SHAPE;       // (a wave a token, or up to 4096 + T of them)
     if (normed && !(std::isnormal(eps) && eps > 0.0f)) return NVFP4_ERR_SHAPE;
     a->d = (int)d;
     a->eps = eps;
@@ -233,10 +235,11 @@ bool attention_sizes_ok(int64_t total_q, int64_t Hq, int64_t H, int64_t d, int64
            max_kv > 0 && max_kv <= kMaxIndex && B > 0 && B <= kMaxIndex && max_q > 0 && max_q <= total_q && max_q <= kMaxIndex / Hq &&
            B <= kMaxIndex / (max_q * Hq);
 }
-bool attention_grid_ok(const AttentionPlan &p, int64_t H, int64_t B)
+bool attention_grid_ok(const AttentionPlan &p, int64_t Hq, int64_t H, int64_t B, int64_t max_q)
 {
-    if (p.rows16) return p.pieces + B + 8 <= kMaxIndex / p.groups;
-    return B * H <= kMaxIndex / p.groups && p.whole + (p.rest + 8) * p.pieces <= kMaxIndex && p.rest * 32 * p.waves <= kMaxIndex;
+    const int64_t most = kMaxLanes / (64 * p.waves);                              // workgroups
+    if (p.rows16) return p.pieces + B + 8 <= most / p.groups && (p.pieces <= 1 || B * max_q * Hq <= kMaxLanes / 256);      // (a row's partial results: 256 lanes)
+    return B * H <= kMaxIndex / p.groups && p.whole + (p.rest + 8) * p.pieces <= most;
 }
 
 }  // namespace
@@ -659,7 +662,7 @@ int nvfp4_kv_cache_write(const nvfp4_kv_cache *cache, const void *k_bf16, int64_
     KvPages c;
     if (int rc = fill_pages(cache, &c)) return rc;
     const int64_t nb = c.d >> 4, parts = (c.H * nb + 63) / 64;
-    if (T <= 0 || T > kMaxIndex / (2 * parts)) return NVFP4_ERR_SHAPE;
+    if (T <= 0 || T > kMaxWaves / (2 * parts)) return NVFP4_ERR_SHAPE;
     if ((k_bf16 && !row_stride_ok(ldk, c.H, c.d)) || (v_bf16 && !row_stride_ok(ldv, c.H, c.d))) return NVFP4_ERR_SHAPE;
     if (k_bf16 && c.k_mean && (nb & (nb - 1)) != 0) return NVFP4_ERR_SHAPE;       // the lanes of a row reduce by shuffles
     if (!aligned16(k_bf16) || !aligned16(v_bf16) || (k_bf16 && (ldk & 7) != 0) || (v_bf16 && (ldv & 7) != 0) || !aligned(slots, 8))
@@ -678,7 +681,7 @@ int nvfp4_kv_cache_read(const nvfp4_kv_cache *cache, const int64_t *slots, int64
     if ((!k_bf16_out && !v_bf16_out) || !slots) return NVFP4_ERR_NULL;
     KvPages c;
     if (int rc = fill_pages(cache, &c)) return rc;
-    if (T <= 0 || T > kMaxIndex / (2 * ((c.H * (c.d >> 3) + 63) / 64))) return NVFP4_ERR_SHAPE;
+    if (T <= 0 || T > kMaxWaves / (2 * ((c.H * (c.d >> 3) + 63) / 64))) return NVFP4_ERR_SHAPE;
     if (!aligned16(k_bf16_out) || !aligned16(v_bf16_out) || !aligned(slots, 8)) return NVFP4_ERR_ALIGN;
     std::lock_guard<std::mutex> lk(g_mu);
     hipStream_t s = static_cast<hipStream_t>(stream);
@@ -709,7 +712,7 @@ int nvfp4_kv_attention(const void *q_bf16, int64_t ldq, int64_t total_q, int64_t
         !aligned(page_table, 4) || !aligned(kv_lens, 4) || !aligned(q_starts, 4) || !aligned(lse, 4))
         return NVFP4_ERR_ALIGN;
     const AttentionPlan plan = attention_plan(total_q, Hq, H, d, max_kv, B, max_q, window, sink);
-    if (!attention_grid_ok(plan, H, B)) return NVFP4_ERR_SHAPE;
+    if (!attention_grid_ok(plan, Hq, H, B, max_q)) return NVFP4_ERR_SHAPE;
     const size_t need = attention_workspace_bytes(plan, d);
     if (need > 0 && (!workspace || workspace_bytes < need)) return NVFP4_ERR_WORKSPACE;
     if (need > 0 && !aligned16(workspace)) return NVFP4_ERR_ALIGN;
@@ -742,7 +745,8 @@ size_t nvfp4_kv_attention_workspace_bytes(int64_t total_q, int64_t Hq, int64_t H
 {
     max_q = std::min(max_q, total_q);
     if (!attention_sizes_ok(total_q, Hq, H, d, max_kv, B, max_q) || window < 0 || sink < 0) return 0;
-    return attention_workspace_bytes(attention_plan(total_q, Hq, H, d, max_kv, B, max_q, window, sink), d);
+    const AttentionPlan plan = attention_plan(total_q, Hq, H, d, max_kv, B, max_q, window, sink);
+    return attention_grid_ok(plan, Hq, H, B, max_q) ? attention_workspace_bytes(plan, d) : 0;
 }
 
 size_t nvfp4_workspace_bytes(int op, int64_t a, int64_t b, int64_t c)

@@ -362,6 +362,12 @@ const at::Tensor &vector_of(const OnDevice &on, PyObject *o, at::ScalarType type
     require(x.scalar_type() == type && x.dim() == dims && x.is_contiguous(), text);
     return x;
 }
+const at::Tensor &workspace_of(const OnDevice &on, PyObject *o)
+{
+    const at::Tensor &x = on(tensor(o));
+    require(x.is_contiguous(), "expected a contiguous workspace");               // (an expanded one has fewer bytes than it says)
+    return x;
+}
 double real(PyObject *o)
 {
     const double v = PyFloat_AsDouble(o);
@@ -455,7 +461,7 @@ PyObject *qk_norm_rope_backward(PyObject *const *a)
     const Rope rope(on, a[6], T);
     const float eps = (float)real(a[7]);
     at::Tensor ws;
-    if (a[12] != Py_None) ws = on(tensor(a[12]));
+    if (a[12] != Py_None) ws = workspace_of(on, a[12]);
     else if (weights) ws = bytes_on(on.device, std::max<int64_t>(16, (int64_t)nvfp4_workspace_bytes(NVFP4_OP_QK_NORM_ROPE_BACKWARD, T, d, 0)));
     void *s = stream_of(a[13]), *w = ws.defined() ? ws.data_ptr() : nullptr;
     const size_t n = ws.defined() ? (size_t)ws.nbytes() : 0;
@@ -546,7 +552,7 @@ PyObject *kv_attention(PyObject *const *a)
         lse = static_cast<float *>(l.data_ptr());
     }
     at::Tensor ws;
-    if (a[13] != Py_None) ws = on(tensor(a[13]));
+    if (a[13] != Py_None) ws = workspace_of(on, a[13]);
     else if (const size_t n = nvfp4_kv_attention_workspace_bytes(total_q, Hq, c.H, c.d, table.size(1) * c.page_tokens, B, max_q, window, sink)) ws = bytes_on(on.device, (int64_t)n);
     void *s = stream_of(a[14]), *w = ws.defined() ? ws.data_ptr() : nullptr, *pq = q.data_ptr(), *po = out.data_ptr();
     const size_t n = ws.defined() ? (size_t)ws.nbytes() : 0;

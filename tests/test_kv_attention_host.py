@@ -185,3 +185,20 @@ def test_attention_refuses_pages_past_its_addresses():
     assert attention(cache(n_pages=1, page_tokens=1 << 28, H=2, d=128), max_pages=1, q=P + 2) == SHAPE      # 2^28 tokens of 2 x 8 scales
     assert attention(cache(n_pages=1, page_tokens=1 << 28, H=8, d=16), max_pages=1, q=P + 2) == SHAPE       # 2^28 tokens of 8 means
     assert attention(cache(n_pages=1, page_tokens=1 << 26, H=2, d=128), max_pages=1, Hq=8, q=P + 2) == ALIGN
+
+
+def test_more_than_a_launch_covers_is_refused():
+    """A launch has at most 2^32 - 1 lanes."""
+    for T in (1 << 26, 1 << 30):
+        assert norm(heads(), T=T) == SHAPE and backward(grad(), T=T) == SHAPE
+    assert norm(heads(weight=P + 4), T=1 << 25) == ALIGN
+    assert write(cache(), T=1 << 25) == SHAPE and read(cache(), T=1 << 25) == SHAPE        # two tensors, 32 blocks and 64 half blocks a row: a wave each
+    assert write(cache(), T=1 << 24, slots=P + 4) == ALIGN
+    ws = nv.nvfp4_kv_attention_workspace_bytes
+    one = dict(Hq=8, max_q=1, max_pages=100)
+    for B in (1 << 21, 1 << 26):                                                         # 2^24 rows of partial results and more
+        assert attention(**one, total_q=B, B=B) == SHAPE and ws(B, 8, 4, 128, 3200, B, 1) == 0
+    assert attention(**one, total_q=1 << 20, B=1 << 20, q=P + 2) == ALIGN and ws(1 << 20, 8, 4, 128, 3200, 1 << 20, 1) > 0
+    many = dict(Hq=4, max_q=17, max_pages=1, total_q=1 << 27)                            # 17 rows of 4 heads: a workgroup each
+    assert attention(**many, B=1 << 23) == SHAPE and ws(1 << 27, 4, 4, 128, 32, 1 << 23, 17) == 0
+    assert attention(**many, B=1 << 20, q=P + 2) == ALIGN
