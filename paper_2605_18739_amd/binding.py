@@ -452,11 +452,8 @@ def nvfp4_qk_norm_rope(q, k, q_weight, k_weight, rope, eps=1e-6, q_out=None, k_o
     weights bf16 [d] (None: rotated only), then the rotation (an NVFP4Rope, or None).  q_out, k_out may be q and k.  Returns (q_out, k_out)."""
     if stream is not None and _elsewhere(stream):
         return _on(stream, nvfp4_qk_norm_rope, q, k, q_weight, k_weight, rope, eps, q_out, k_out)
-    if q is not None and q_out is None:
-        q_out = torch.empty(q.shape, dtype=torch.bfloat16, device=q.device)
-    if k is not None and k_out is None:
-        k_out = torch.empty(k.shape, dtype=torch.bfloat16, device=k.device)
-    _check(_host().qk_norm_rope(q, k, q_weight, k_weight, rope and rope._native(), eps, q_out, k_out, _stream(stream)))
+    rc, q_out, k_out = _host().qk_norm_rope(q, k, q_weight, k_weight, rope and rope._native(), eps, q_out, k_out, _stream(stream))
+    _check(rc)
     return q_out, k_out
 
 
@@ -466,16 +463,9 @@ def nvfp4_qk_norm_rope_backward(dq, dk, q, k, q_weight, k_weight, rope, eps=1e-6
     dk_weight): bf16 like dq and dk, and fp32 [d] (None without a weight, or with weight_grads=False)."""
     if stream is not None and _elsewhere(stream):
         return _on(stream, nvfp4_qk_norm_rope_backward, dq, dk, q, k, q_weight, k_weight, rope, eps, dq_in, dk_in, dq_weight, dk_weight, weight_grads, workspace)
-    if dq is not None and dq_in is None:
-        dq_in = torch.empty(dq.shape, dtype=torch.bfloat16, device=dq.device)
-    if dk is not None and dk_in is None:
-        dk_in = torch.empty(dk.shape, dtype=torch.bfloat16, device=dk.device)
-    if weight_grads and dq is not None and q_weight is not None and dq_weight is None:
-        dq_weight = torch.empty(q_weight.shape, dtype=torch.float32, device=dq.device)
-    if weight_grads and dk is not None and k_weight is not None and dk_weight is None:
-        dk_weight = torch.empty(k_weight.shape, dtype=torch.float32, device=dk.device)
-    _check(_host().qk_norm_rope_backward(dq, dk, q, k, q_weight, k_weight, rope and rope._native(), eps, dq_in, dk_in, dq_weight, dk_weight,
-                                         workspace, _stream(stream)))
+    rc, dq_in, dk_in, dq_weight, dk_weight = _host().qk_norm_rope_backward(dq, dk, q, k, q_weight, k_weight, rope and rope._native(), eps, dq_in, dk_in,
+                                                                           dq_weight, dk_weight, 1 if weight_grads else 0, workspace, _stream(stream))
+    _check(rc)
     return dq_in, dk_in, dq_weight, dk_weight
 
 
@@ -527,9 +517,8 @@ def nvfp4_kv_cache_read(cache, slots, k_out=None, v_out=None, stream=None):
     """Slots (int64 [T]) back to bf16 [T, H, d].  Returns (k_out, v_out); with one of the two given, the other is not read (None)."""
     if stream is not None and _elsewhere(stream):
         return _on(stream, nvfp4_kv_cache_read, cache, slots, k_out, v_out)
-    if k_out is None and v_out is None:
-        k_out, v_out = (torch.empty((slots.shape[0], cache.H, cache.d), dtype=torch.bfloat16, device=slots.device) for _ in range(2))
-    _check(_host().kv_cache_read(cache._native, slots, k_out, v_out, _stream(stream)))
+    rc, k_out, v_out = _host().kv_cache_read(cache._native, slots, k_out, v_out, _stream(stream))
+    _check(rc)
     return k_out, v_out
 
 
@@ -543,14 +532,9 @@ def nvfp4_kv_attention(q, cache, page_table, kv_lens, q_starts, max_q, softmax_s
     kv_lens int32 [B], q_starts int32 [B + 1]; softmax_scale d ** -0.5 by default.  Returns (out [total_q, Hq, d], lse fp32 [total_q, Hq])."""
     if stream is not None and _elsewhere(stream):
         return _on(stream, nvfp4_kv_attention, q, cache, page_table, kv_lens, q_starts, max_q, softmax_scale, causal, window, sink, out_dtype, out, lse, workspace)
-    if q.dim() != 3:
-        raise _wrong_rank(q, 3)
-    if out is None:
-        out = torch.empty(q.shape, dtype=torch.float32 if out_dtype == OUT_F32 else torch.bfloat16, device=q.device)
-    if lse is None:
-        lse = torch.empty(q.shape[:2], dtype=torch.float32, device=q.device)
-    _check(_host().kv_attention(q, cache._native, page_table, kv_lens, q_starts, max_q, cache.d ** -0.5 if softmax_scale is None else softmax_scale,
-                                1 if causal else 0, window, sink, out_dtype, out, lse, workspace, _stream(stream)))
+    rc, out, lse = _host().kv_attention(q, cache._native, page_table, kv_lens, q_starts, max_q, cache.d ** -0.5 if softmax_scale is None else softmax_scale,
+                                        1 if causal else 0, window, sink, out_dtype, out, lse, workspace, _stream(stream))
+    _check(rc)
     return out, lse
 
 

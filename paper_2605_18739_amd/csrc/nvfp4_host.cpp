@@ -349,12 +349,12 @@ struct OnDevice {
     }
 };
 // [T, H, d] with whole rows: heads one behind the other, any distance from token to token
-const at::Tensor &rows(const OnDevice &on, PyObject *o)
+const at::Tensor &rows(const at::Tensor &x)
 {
-    const at::Tensor &x = on(tensor(o));
     require(x.scalar_type() == at::kBFloat16 && x.dim() == 3 && x.stride(2) == 1 && x.stride(1) == x.size(2), "expected a bf16 tensor [T, H, d] with contiguous [H, d]");
     return x;
 }
+const at::Tensor &rows(const OnDevice &on, PyObject *o) { return rows(on(tensor(o))); }
 int64_t token_stride(const at::Tensor &x) { return x.size(0) > 1 ? x.stride(0) : x.size(1) * x.size(2); }
 const at::Tensor &vector_of(const OnDevice &on, PyObject *o, at::ScalarType type, int dims, const char *text)
 {
@@ -367,6 +367,45 @@ const at::Tensor &workspace_of(const OnDevice &on, PyObject *o)
     const at::Tensor &x = on(tensor(o));
     require(x.is_contiguous(), "expected a contiguous workspace");               // (an expanded one has fewer bytes than it says)
     return x;
+}
+// An output: the caller's tensor, or a new one (an allocation here costs 0.7 us, one through torch.empty 2.3), handed back with the status
+struct Output {
+    PyObject *given = Py_None;
+    at::Tensor t;
+    Output() = default;                                               // none
+    Output(const OnDevice &on, PyObject *o, at::IntArrayRef sizes, at::ScalarType type) : given(o)
+    {
+        t = o == Py_None ? at::empty(sizes, at::TensorOptions().device(on.device).dtype(type)) : on(tensor(o));
+    }
+    PyObject *handed_back() const
+    {
+        if (given == Py_None && t.defined()) return THPVariable_Wrap(t);
+        Py_INCREF(given);
+        return given;
+    }
+};
+// (status, output, ...) of a call
+template <class F>
+PyObject *status_and(std::initializer_list<const Output *> outputs, F &&call)
+{
+    PyObject *rc = status(call), *r = rc ? PyTuple_New(1 + (Py_ssize_t)outputs.size()) : nullptr;
+    if (!r) {
+        Py_XDECREF(rc);
+        throw Fail();
+    }
+    PyTuple_SET_ITEM(r, 0, rc);
+    try {
+        Py_ssize_t i = 1;
+        for (const Output *o : outputs) {
+            PyObject *t = o->handed_back();
+            if (!t) throw Fail();
+            PyTuple_SET_ITEM(r, i++, t);
+        }
+    } catch (...) {
+        Py_DECREF(r);
+        throw;
+    }
+    return r;
 }
 double real(PyObject *o)
 {
@@ -408,10 +447,13 @@ PyObject *qk_norm_rope(PyObject *const *a)                          // q, k, q_w
 {
     const OnDevice on;
     nvfp4_heads h[2]{}, *given[2] = {nullptr, nullptr};
+    Output out[2];
     int64_t T = -1, d = -1;
     for (int i = 0; i < 2; ++i) {
         if (a[i] == Py_None) continue;
-        const at::Tensor &x = rows(on, a[i]), &y = rows(on, a[6 + i]);
+        const at::Tensor &x = rows(on, a[i]);
+        out[i] = Output(on, a[6 + i], x.sizes(), at::kBFloat16);
+        const at::Tensor &y = rows(out[i].t);
         require((T < 0 || T == x.size(0)) && (d < 0 || d == x.size(2)), "queries and keys of the same tokens and head size");
         require(y.sizes() == x.sizes(), "an output has its input's shape");
         T = x.size(0);
@@ -422,18 +464,21 @@ PyObject *qk_norm_rope(PyObject *const *a)                          // q, k, q_w
     const Rope rope(on, a[4], T);
     const float eps = (float)real(a[5]);
     void *s = stream_of(a[8]);
-    return status([&] { return nvfp4_qk_norm_rope(given[0], given[1], T, d, eps, rope.c, s); });
+    return status_and({&out[0], &out[1]}, [&] { return nvfp4_qk_norm_rope(given[0], given[1], T, d, eps, rope.c, s); });
 }
-// dq, dk, q, k, q_weight, k_weight, rope, eps, dq_in, dk_in, dq_weight, dk_weight, workspace, stream
+// dq, dk, q, k, q_weight, k_weight, rope, eps, dq_in, dk_in, dq_weight, dk_weight, weight_grads, workspace, stream
 PyObject *qk_norm_rope_backward(PyObject *const *a)
 {
     const OnDevice on;
     nvfp4_heads_grad h[2]{}, *given[2] = {nullptr, nullptr};
+    Output out[2], dweight[2];
     int64_t T = -1, d = -1;
     bool weights = false;
     for (int i = 0; i < 2; ++i) {
         if (a[i] == Py_None) continue;
-        const at::Tensor &dy = rows(on, a[i]), &dx = rows(on, a[8 + i]);
+        const at::Tensor &dy = rows(on, a[i]);
+        out[i] = Output(on, a[8 + i], dy.sizes(), at::kBFloat16);
+        const at::Tensor &dx = rows(out[i].t);
         require((T < 0 || T == dy.size(0)) && (d < 0 || d == dy.size(2)), "queries and keys of the same tokens and head size");
         require(dx.sizes() == dy.sizes(), "a gradient has its input's shape");
         T = dy.size(0);
@@ -449,23 +494,25 @@ PyObject *qk_norm_rope_backward(PyObject *const *a)
             h[i].x = x.data_ptr();
             h[i].ld_x = token_stride(x);
             h[i].weight = weight_of(on, a[4 + i], d).data_ptr();
-            if (a[10 + i] != Py_None) {
-                const at::Tensor &dw = vector_of(on, a[10 + i], at::kFloat, 1, "expected a contiguous fp32 weight gradient [d]");
-                require(dw.size(0) == d, "expected a weight gradient of d elements");
+            if (a[10 + i] != Py_None || number(a[12])) {
+                dweight[i] = Output(on, a[10 + i], {d}, at::kFloat);
+                const at::Tensor &dw = dweight[i].t;
+                require(dw.scalar_type() == at::kFloat && dw.dim() == 1 && dw.is_contiguous() && dw.size(0) == d, "expected a contiguous fp32 weight gradient [d]");
                 h[i].dweight = static_cast<float *>(dw.data_ptr());
                 weights = true;
             }
         }
+        else dweight[i].given = a[10 + i];
         given[i] = &h[i];
     }
     const Rope rope(on, a[6], T);
     const float eps = (float)real(a[7]);
     at::Tensor ws;
-    if (a[12] != Py_None) ws = workspace_of(on, a[12]);
+    if (a[13] != Py_None) ws = workspace_of(on, a[13]);
     else if (weights) ws = bytes_on(on.device, std::max<int64_t>(16, (int64_t)nvfp4_workspace_bytes(NVFP4_OP_QK_NORM_ROPE_BACKWARD, T, d, 0)));
-    void *s = stream_of(a[13]), *w = ws.defined() ? ws.data_ptr() : nullptr;
+    void *s = stream_of(a[14]), *w = ws.defined() ? ws.data_ptr() : nullptr;
     const size_t n = ws.defined() ? (size_t)ws.nbytes() : 0;
-    return status([&] { return nvfp4_qk_norm_rope_backward(given[0], given[1], T, d, eps, rope.c, w, n, s); });
+    return status_and({&out[0], &out[1], &dweight[0], &dweight[1]}, [&] { return nvfp4_qk_norm_rope_backward(given[0], given[1], T, d, eps, rope.c, w, n, s); });
 }
 
 // the tuple that an NVFP4KvCache keeps: k_codes, k_scales, k_global, k_mean or None, v_codes, v_scales, v_global
@@ -518,14 +565,17 @@ PyObject *kv_cache_read(PyObject *const *a)                         // cache, sl
     const Pages pages(on, a[0]);
     const at::Tensor &slots = vector_of(on, a[1], at::kLong, 1, "expected contiguous int64 slots [T]");
     void *p[2] = {};
+    Output out[2];
     for (int i = 0; i < 2; ++i) {
-        if (a[2 + i] == Py_None) continue;
-        const at::Tensor &x = on(heads(a[2 + i]));
+        if (a[2 + i] == Py_None && a[3 - i] != Py_None) continue;           // (one of them alone)
+        out[i] = Output(on, a[2 + i], {slots.size(0), pages.c.H, pages.c.d}, at::kBFloat16);
+        const at::Tensor &x = out[i].t;
+        require(x.scalar_type() == at::kBFloat16 && x.dim() == 3 && x.is_contiguous(), "expected a contiguous bf16 tensor [T, H, d]");
         require(x.size(0) == slots.size(0) && x.size(1) == pages.c.H && x.size(2) == pages.c.d, "expected room for a token of the cache's heads for each slot");
         p[i] = x.data_ptr();
     }
     void *s = stream_of(a[4]);
-    return status([&] { return nvfp4_kv_cache_read(&pages.c, static_cast<const int64_t *>(slots.data_ptr()), slots.size(0), p[0], p[1], s); });
+    return status_and({&out[0], &out[1]}, [&] { return nvfp4_kv_cache_read(&pages.c, static_cast<const int64_t *>(slots.data_ptr()), slots.size(0), p[0], p[1], s); });
 }
 // q, cache, page_table, kv_lens, q_starts, max_q, softmax_scale, causal, window, sink, out_dtype, out, lse, workspace, stream
 PyObject *kv_attention(PyObject *const *a)
@@ -542,22 +592,19 @@ PyObject *kv_attention(PyObject *const *a)
     require(q.size(2) == c.d, "expected queries of the cache's head size");
     const float scale = (float)real(a[6]);
     const int causal = (int)number(a[7]), dtype = (int)number(a[10]);
-    const at::Tensor &out = on(tensor(a[11]));
+    const Output o(on, a[11], q.sizes(), dtype == NVFP4_OUT_F32 ? at::kFloat : at::kBFloat16), log_sum(on, a[12], {total_q, Hq}, at::kFloat);
+    const at::Tensor &out = o.t, &l = log_sum.t;
     require(out.scalar_type() == (dtype == NVFP4_OUT_F32 ? at::kFloat : at::kBFloat16) && out.sizes() == q.sizes() && out.stride(2) == 1 && out.stride(1) == c.d,
             "expected an output of the queries' shape and the chosen type with contiguous [H, d]");
-    float *lse = nullptr;
-    if (a[12] != Py_None) {
-        const at::Tensor &l = vector_of(on, a[12], at::kFloat, 2, "expected a contiguous fp32 lse [total_q, H]");
-        require(l.size(0) == total_q && l.size(1) == Hq, "expected an lse for each query and head");
-        lse = static_cast<float *>(l.data_ptr());
-    }
+    require(l.scalar_type() == at::kFloat && l.dim() == 2 && l.is_contiguous() && l.size(0) == total_q && l.size(1) == Hq, "expected a contiguous fp32 lse [total_q, H]");
+    float *const lse = static_cast<float *>(l.data_ptr());
     at::Tensor ws;
     if (a[13] != Py_None) ws = workspace_of(on, a[13]);
     else if (const size_t n = nvfp4_kv_attention_workspace_bytes(total_q, Hq, c.H, c.d, table.size(1) * c.page_tokens, B, max_q, window, sink)) ws = bytes_on(on.device, (int64_t)n);
     void *s = stream_of(a[14]), *w = ws.defined() ? ws.data_ptr() : nullptr, *pq = q.data_ptr(), *po = out.data_ptr();
     const size_t n = ws.defined() ? (size_t)ws.nbytes() : 0;
     const int32_t *pt = static_cast<const int32_t *>(table.data_ptr()), *pl = static_cast<const int32_t *>(lens.data_ptr()), *ps = static_cast<const int32_t *>(starts.data_ptr());
-    return status([&] {
+    return status_and({&o, &log_sum}, [&] {
         return nvfp4_kv_attention(pq, token_stride(q), total_q, Hq, &c, pt, table.size(1), pl, ps, B, max_q, scale, causal, window, sink, po, token_stride(out), dtype, lse, w, n, s);
     });
 }
@@ -596,7 +643,7 @@ extern "C" PyObject *PyInit__host(void)
         method<kv_dequant, 6>("kv_dequant"), method<kv_dequant_gather, 5>("kv_dequant_gather"), method<gemm, 5>("gemm"),
         method<gemm_scale_out, 6>("gemm_scale_out"), method<lora_down, 5>("lora_down"), method<gemm_lora, 8>("gemm_lora"),
         method<gemm_act_quant, 8>("gemm_act_quant"), method<qk_norm_rope, 9>("qk_norm_rope"),
-        method<qk_norm_rope_backward, 14>("qk_norm_rope_backward"), method<kv_cache_write, 6>("kv_cache_write"),
+        method<qk_norm_rope_backward, 15>("qk_norm_rope_backward"), method<kv_cache_write, 6>("kv_cache_write"),
         method<kv_cache_read, 5>("kv_cache_read"), method<kv_attention, 15>("kv_attention"), {nullptr, nullptr, 0, nullptr}};
     static PyModuleDef module = {PyModuleDef_HEAD_INIT, "_host", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
     s_codes = PyUnicode_InternFromString("codes");
