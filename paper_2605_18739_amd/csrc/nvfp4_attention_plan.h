@@ -8,10 +8,16 @@
 namespace nvfp4 {
 
 constexpr int kRows16Step = 32, kTileStep = 64;       // cached tokens of a step of either kernel
-// rows16: heads of a workgroup at most, workgroups of a call, steps of a piece at least.  Two workgroups to a compute unit up to
+// rows16: heads of a workgroup at most, workgroups of a call, and steps of a piece at least.  Two workgroups to a compute unit up to
 // d = 128 and one above (whose registers leave room for one): eight caches of up to 16384 tokens, d = 64 / 128 / 256: 512
 // workgroups take 17.0 / 20.4 / 40.9 us, 256 18.6 / 21.2 / 33.4.
-constexpr int kRows16Heads = 4, kRows16Slots = 512, kRows16MinSteps = 4;
+// Steps of a piece: a step of a wave that has its SIMD alone takes 0.8 us, a partial result more next to nothing (five caches of up
+// to 704 tokens, d = 64: pieces of four steps 9.0 + 5.2 us, of two 7.2 + 5.5).
+constexpr int kRows16Heads = 4, kRows16Slots = 512, kRows16MinSteps = 2;
+// Steps up to which a sequence is not cut: the second launch costs about 6 us (one cache, d = 128: 320 tokens in pieces 7.4 + 5.6 us
+// and the gap between the launches, whole 13.5; 512 tokens 7.4 + 5.6, 18.4), twice as many where the sequences fill a quarter
+// of the chip by themselves (64 caches of 512 tokens of 8 heads: 16.9 + 8.2 us, whole 19.9).
+constexpr int kRows16Whole = 10;
 constexpr int kTileMinSteps = 8;                       // steps of a piece of the other kernel, at least
 
 struct AttentionPlan {
@@ -41,7 +47,7 @@ inline AttentionPlan attention_plan(int64_t total_q, int64_t Hq, int64_t H, int6
         // sequences are cut to a common length, so every one of them may add a shorter piece to those of full length
         const int64_t most = B * ((steps + kRows16MinSteps - 1) / kRows16MinSteps);
         p.pieces = (int)std::min(std::max<int64_t>((d > 128 ? kRows16Slots / 2 : kRows16Slots) / p.groups - B, std::min<int64_t>(B, 64)), most);
-        if (steps <= kRows16MinSteps) p.pieces = 1;
+        if (steps <= (B * p.groups >= kRows16Slots / 4 ? 2 : 1) * kRows16Whole) p.pieces = 1;
         p.part_rows = p.pieces <= 1 ? 0 : (p.pieces + B) * max_q * Hq;
     } else {
         p.waves = d > 64 && d <= 128 && rows > 128 ? 8 : 4;
