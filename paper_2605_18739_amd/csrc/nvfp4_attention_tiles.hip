@@ -16,6 +16,10 @@ namespace nvfp4 {
 //    the order in which S^T leaves its tokens: of every sixteen {0-3, 8-11} for lanes 0-31 and {4-7, 12-15} for lanes 32-63.
 // LDS rows are 16-byte chunks, the chunk's place exclusive-or'ed with bits of the row, so that eight neighbouring rows read
 // (or written) at one chunk lie in different banks.
+// Measured (24 heads of 128, 3520 queries over 18480 tokens, smoothed keys): 930 us and 19 to join, 840 TFLOP/s, where a
+// library's product of 8192 x 8192 matrices holds 1170 to 1215: no single pipe is full (the matrix instructions alone take 410 us
+// at 2.14 GHz), and the clock depends on the operands (all zeros: 790 us).  2000 queries over 8192 tokens of
+// 16 heads: d = 64 126 us, 128 157 us, 256 448 us.  Four waves for up to 128 rows, because waves without rows only load.
 template <int D, int WAVES>
 struct Tiles {
     static constexpr int kThreads = 64 * WAVES;

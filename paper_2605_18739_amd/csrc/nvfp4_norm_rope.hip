@@ -119,7 +119,9 @@ struct Turns {
 
 // A wave takes a token and some of its heads, kWave / LPR of them at a time: LPR lanes of eight elements hold a row, so the
 // sines and cosines (an fp64 product and two polynomials a pair) are made once and serve every head of the token.
-// Queries come first, then keys; a turn of the loop is all queries or all keys.
+// Queries come first, then keys; a turn of the loop is all queries or all keys, the next turn's loads in flight.
+// Measured (17600 tokens, 24 + 24 heads of 128, three axes): 90 us, 4.8 TB/s; 8 tokens of 32 + 8 heads: 4.4 us, latency (launch,
+// positions, angles, rows).
 struct Unit {
     int64_t t;
     int g0, g1;
@@ -178,7 +180,8 @@ __global__ __launch_bounds__(kNormThreads) void norm_rope_kernel(const NormRopeA
 }
 
 // Backward: the same units, but a workgroup takes one after another, because each leaves its sum of the weights' gradients:
-// partial[workgroup][q, k][d], added in order by norm_rope_weights_kernel.
+// partial[workgroup][q, k][d], added in order by norm_rope_weights_kernel.  Measured (17600 tokens, 24 + 24 heads of 128): 133 us,
+// 4.9 TB/s.
 // WAVES: sixteen to a workgroup where that leaves a unit to a wave, four otherwise.  (777 tokens of 16 + 4 heads of 64: 146
 // partial sums instead of 583, 10.6 us and 3.8 to add them instead of 9.1 and 6.4; 17600 of 24 + 24 heads of 128, where the
 // workgroups go round: 142 and 5 instead of 134 and 8.)

@@ -269,6 +269,16 @@ def test_ids_outside_the_pool_are_not_seen(queries):
     run_attention(c, table, [200, 90], starts, q, queries, False)
 
 
+@pytest.mark.parametrize("queries", [1, 24])
+def test_sequences_that_share_pages(queries):
+    say("[use] shared pages", queries)
+    c, table, starts, q = attention_case(50, [150, 150, 40], [queries] * 3, 4, 2, 128, 16, True)
+    table[1] = table[0]
+    table[2, :2] = table[0, 0]                             # and a sequence that holds one page twice
+    run_attention(c, table, [150, 133, 40], starts, q, queries, True)
+    run_attention(c, table, [150, 133, 40], starts, q, queries, False, window=50, sink=3)
+
+
 def test_lengths_and_queries_are_cut_off():
     say("[use] cut off")
     for queries in ([1, 1], [3, 20], [60, 30]):
