@@ -27,7 +27,8 @@ struct AttentionArgs {
 };
 
 // A page's tensor scale.  Pages that are not in use may hold anything: where a step touches one its tokens are masked, and a
-// scale of one keeps NaN and infinities out of the sums that they enter with weight zero.
+// scale of one keeps NaN and infinities out of the sums that they enter with weight zero.  (Blocks of rows see to it in the
+// turns that mask: tested for every step that they load, it costs the accumulators of d = 256 their registers, 432 -> 500 us.)
 __device__ __forceinline__ float page_scale(uint32_t bits)
 {
     return __uint_as_float(bits - 0x00800000u < 0x7F000000u ? bits : 0x3F800000u);      // (positive and normal)
@@ -36,11 +37,7 @@ __device__ __forceinline__ float page_scale(uint32_t bits)
 // Sixteen cached tokens of a page: where their slots begin in each plane, as scalar bases for a lane's 32-bit offset.  (Two
 // 32 x 32 bit products give them all, codes being eight times as long as scales.)
 using GlobalBytes = const __attribute__((address_space(1))) uint8_t *;
-// (the compiler must not add a lane's offset to the base's parts in another order: that takes a 64-bit vector addition a load)
-__device__ __forceinline__ GlobalBytes scalar_base(const void *base, uint64_t at)
-{
-    return (GlobalBytes)base + at;
-}
+__device__ __forceinline__ GlobalBytes scalar_base(const void *base, uint64_t at) { return (GlobalBytes)base + at; }
 template <class T>
 __device__ __forceinline__ T load_at(GlobalBytes base, uint32_t offset) { return *(const __attribute__((address_space(1))) T *)(base + offset); }
 struct Slots {

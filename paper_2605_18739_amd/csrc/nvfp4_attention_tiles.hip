@@ -19,7 +19,7 @@ namespace nvfp4 {
 // Measured (24 heads of 128, 3520 queries over 18480 tokens, smoothed keys): 930 us and 19 to join, 840 TFLOP/s, where a
 // library's product of 8192 x 8192 matrices holds 1170 to 1215: no single pipe is full (the matrix instructions alone take 410 us
 // at 2.14 GHz), and the clock depends on the operands (all zeros: 790 us).  2000 queries over 8192 tokens of
-// 16 heads: d = 64 126 us, 128 157 us, 256 448 us.  Four waves for up to 128 rows, because waves without rows only load.
+// 16 heads: d = 64 126 us, 128 157 us, 256 432 us.  Four waves for up to 128 rows, because waves without rows only load.
 template <int D, int WAVES>
 struct Tiles {
     static constexpr int kThreads = 64 * WAVES;
@@ -187,7 +187,7 @@ __global__ __launch_bounds__(64 * WAVES, D == 256 ? 1 : 2) void attention_tiles_
             odd[t] = ((s.v[t][0] >> 4) & 0x0F0F0F0Fu) | (s.v[t][1] & 0xF0F0F0F0u);
             sv[t] = scale_pair(__builtin_amdgcn_perm(s.vs[t][1], s.vs[t][0], vs_pick));
             if (blk == 0) {
-                const float kg = page_scale(s.kg[t]), vg = page_scale(s.vg[t]);
+                const float kg = __uint_as_float(s.kg[t]), vg = __uint_as_float(s.vg[t]);
                 if constexpr (SMOOTH) lds.of[stage].mean[token0 + t * (kThreads / NB)] = __uint_as_float((s.mean[t] >> mean_shift) << 16) * __builtin_amdgcn_rcpf(kg);
                 if (token16 == 0) {
                     lds.of[stage].kg[group_of(t)] = kg;
@@ -286,7 +286,7 @@ __global__ __launch_bounds__(64 * WAVES, D == 256 ? 1 : 2) void attention_tiles_
             mean[1] = of.mean[32 + c32];
         }
         const uint4v valid = *(const uint4v *)of.valid;
-        const float4v kg = *(const float4v *)of.kg, log_v = *(const float4v *)of.log_v, inv_v = *(const float4v *)of.inv_v;
+        float4v kg = *(const float4v *)of.kg, log_v = *(const float4v *)of.log_v, inv_v = *(const float4v *)of.inv_v;
         NVFP4_FENCE;
 #pragma unroll
         for (int t = 0; t < 2; ++t)
@@ -317,6 +317,13 @@ __global__ __launch_bounds__(64 * WAVES, D == 256 ? 1 : 2) void attention_tiles_
                     const bool there = (all >> (2 * t + (e >> 3)) & 1u) != 0u;
                     x[t][e] = (there & sight.of(first + at)) ? x[t][e] : -__builtin_inff();
                 }
+            // (a page that is not in use, all of whose tokens are masked: anything may stand there)
+#pragma unroll
+            for (int g = 0; g < 4; ++g) {
+                kg[g] = kg[g] > 0.0f && kg[g] < __builtin_inff() ? kg[g] : 1.0f;
+                log_v[g] = fabsf(log_v[g]) < 1024.0f ? log_v[g] : 0.0f;
+                inv_v[g] = fabsf(inv_v[g]) < __builtin_inff() ? inv_v[g] : 0.0f;
+            }
         }
         float f[4], top = kLowest;
 #pragma unroll
