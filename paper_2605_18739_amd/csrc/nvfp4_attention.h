@@ -57,6 +57,7 @@ struct Slots {
 // query among i0 .. i1 sees: sink_steps steps from token 0, then those from lo_step on.
 struct Sequence {
     int start, n_q, len, p0;              // p0: position of query 0; query i stands at p0 + i (causal) or p0
+    Sequence() = default;
     __device__ __forceinline__ Sequence(const AttentionArgs &a, const int32_t *__restrict__ q_starts, const int32_t *__restrict__ kv_lens, int b)
     {
         start = min(max(q_starts[b], 0), a.total_q);
@@ -89,48 +90,62 @@ struct Pieces {
     int steps;                            // of a piece
     int first, count;                     // pieces in front of sequence b, and its own
     int b;                                // sequence of piece number `at`, B: behind the last one
-    __device__ __forceinline__ static int sequence_steps(const AttentionArgs &a, const int32_t *__restrict__ q_starts, const int32_t *__restrict__ kv_lens, int b)
+    Sequence seq;
+    // steps of sequence s (-1: no queries, or behind the last one)
+    __device__ __forceinline__ static int sequence_steps(const AttentionArgs &a, const Sequence &s, bool there)
     {
-        if (b >= a.B) return -1;
-        const Sequence seq(a, q_starts, kv_lens, b);
-        const int n_q = min(seq.n_q, a.max_q);
-        return n_q > 0 ? Steps(a, seq, 0, n_q - 1, kRows16Step).total : -1;
+        const int n_q = min(s.n_q, a.max_q);
+        return there && n_q > 0 ? Steps(a, s, 0, max(n_q, 1) - 1, kRows16Step).total : -1;
+    }
+    // inclusive sum over the lanes up to each: within rows of sixteen, then row 0 into 1 and 2 into 3, then the lower half into the upper
+    __device__ __forceinline__ static uint32_t up_to(uint32_t v)
+    {
+        v += (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x111, 0xF, 0xF, true);
+        v += (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x112, 0xF, 0xF, true);
+        v += (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x114, 0xF, 0xF, true);
+        v += (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x118, 0xF, 0xF, true);
+        v += (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x142, 0xA, 0xF, false);
+        v += (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x143, 0xC, 0xF, false);
+        return v;
     }
     // by_sequence: `at` is a sequence, its pieces are what is asked for
     __device__ __forceinline__ Pieces(const AttentionArgs &a, const int32_t *__restrict__ q_starts, const int32_t *__restrict__ kv_lens, int at, bool by_sequence)
     {
         const int lane = threadIdx.x & 63;
-        int total = 0, mine = sequence_steps(a, q_starts, kv_lens, lane);
-        for (int b0 = 0; b0 < a.B; b0 += 64) {
-            int n = max(b0 == 0 ? mine : sequence_steps(a, q_starts, kv_lens, b0 + lane), 0);
-#pragma unroll
-            for (int x = 32; x > 0; x >>= 1) n += __shfl_xor(n, x, 64);
-            total = total > 0x3FFFFFFF - n ? 0x3FFFFFFF : total + n;
+        const int last = a.B - 1;
+        Sequence lanes(a, q_starts, kv_lens, min(lane, last));               // this lane's sequence, of 64 (the first 64 until the second loop asks for more)
+        int mine = sequence_steps(a, lanes, lane <= last);
+        int64_t total = (uint32_t)__builtin_amdgcn_readlane((int)up_to((uint32_t)max(mine, 0)), 63);         // (64 of at most 2^25 steps)
+        for (int b0 = 64; b0 < a.B; b0 += 64) {
+            const Sequence other(a, q_starts, kv_lens, min(b0 + lane, last));
+            total += (uint32_t)__builtin_amdgcn_readlane((int)up_to((uint32_t)max(sequence_steps(a, other, b0 + lane <= last), 0)), 63);
         }
-        steps = max(__builtin_amdgcn_readfirstlane((total + a.plan.pieces - 1) / a.plan.pieces), a.plan.piece_steps);
-        if (a.plan.pieces <= 1) steps = 0x3FFFFFFF;
+        steps = a.plan.pieces <= 1 ? 0x3FFFFFFF : max((int)min((total + a.plan.pieces - 1) / a.plan.pieces, (int64_t)0x3FFFFFFF), a.plan.piece_steps);
         int before = 0;
         for (int b0 = 0; b0 < a.B; b0 += 64) {
-            const int s = b0 == 0 ? mine : sequence_steps(a, q_starts, kv_lens, b0 + lane);
-            const int n = s < 0 ? 0 : max((s + steps - 1) / steps, 1);       // (a sequence without tokens has one, which writes its zeros)
-            int upto = n;                                                    // inclusive sum over the lanes
-#pragma unroll
-            for (int x = 1; x < 64; x <<= 1) {
-                const int o = __shfl_up(upto, x, 64);
-                upto += lane >= x ? o : 0;
+            if (b0 > 0) {
+                lanes = Sequence(a, q_starts, kv_lens, min(b0 + lane, last));
+                mine = sequence_steps(a, lanes, b0 + lane <= last);
             }
+            const int n = mine < 0 ? 0 : max((int)(((uint32_t)mine + (uint32_t)steps - 1u) / (uint32_t)steps), 1);       // (a sequence without tokens has one, which writes its zeros)
+            const int upto = (int)up_to((uint32_t)n);
             const bool here = by_sequence ? b0 + lane == at : (at >= before + upto - n) & (at < before + upto);
             if (const uint64_t found = __ballot(here)) {
                 const int l = (int)__builtin_ctzll(found);
                 b = b0 + l;
                 count = __builtin_amdgcn_readlane(n, l);
                 first = before + __builtin_amdgcn_readlane(upto, l) - count;
+                seq.start = __builtin_amdgcn_readlane(lanes.start, l);
+                seq.n_q = __builtin_amdgcn_readlane(lanes.n_q, l);
+                seq.len = __builtin_amdgcn_readlane(lanes.len, l);
+                seq.p0 = __builtin_amdgcn_readlane(lanes.p0, l);
                 return;
             }
             before += __builtin_amdgcn_readlane(upto, 63);
         }
         b = a.B;
         first = count = 0;
+        seq = lanes;
     }
 };
 

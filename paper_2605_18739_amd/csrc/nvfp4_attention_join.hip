@@ -7,7 +7,7 @@ namespace nvfp4 {
 // their partial sums, d / 4 lanes to a piece, as many pieces side by side as there are lanes for.  Pieces are added in an
 // order that does not depend on when they finished.  A wave a row where there are few pieces and many rows (chunks: 84480
 // rows in three pieces took 53 us, a workgroup to each 182), a workgroup where there are many pieces (single tokens: 256
-// rows in 50 pieces 9 us and 7).
+// rows in 50 pieces 9 us and 6).
 constexpr int kJoinThreads = 256, kJoinFew = 8;
 template <int THREADS>
 __global__ __launch_bounds__(kJoinThreads) void attention_join_kernel(const AttentionArgs a, const int32_t *__restrict__ kv_lens, const int32_t *__restrict__ q_starts,
@@ -35,16 +35,18 @@ __global__ __launch_bounds__(kJoinThreads) void attention_join_kernel(const Atte
         first = j * a.plan.pieces * rows + (id - j * rows);
         stride = rows;
     }
-    const Sequence seq(a, q_starts, kv_lens, b);
-    const int n_q = min(seq.n_q, a.max_q);
-    if (i >= n_q) return;
-    const int64_t query = (int64_t)seq.start + i, out_row = query * a.Hq + head;
+    Sequence seq;
     if (a.plan.rows16) {
         const Pieces p(a, q_starts, kv_lens, b, true);
+        seq = p.seq;
         pieces = p.count;
         first = ((int64_t)p.first * a.max_q + i) * a.Hq + head;
         stride = (int64_t)a.max_q * a.Hq;
-    } else {
+    } else seq = Sequence(a, q_starts, kv_lens, b);
+    const int n_q = min(seq.n_q, a.max_q);
+    if (i >= n_q) return;
+    const int64_t query = (int64_t)seq.start + i, out_row = query * a.Hq + head;
+    if (!a.plan.rows16) {
         const int rows = 32 * a.plan.waves, row0 = (i * a.G + head % a.G) / rows * rows;
         const Steps steps(a, seq, row0 / a.G, min((row0 + rows - 1) / a.G, n_q - 1), kTileStep);
         const int piece_steps = tile_piece_steps(a, steps.total);

@@ -26,8 +26,8 @@ namespace nvfp4 {
 // step, and the planes' sizes are multiples of sixteen bytes: no word reaches past the end).
 // The same word is asked for once where lanes share it: a step takes 16 loads, and lanes hand scales and means on (d = 128;
 // with a load for every lane's own, 28 loads: 41 us where this takes 39, d = 80 24 -> 22).
-// Measured (eight caches of up to 28672 tokens, 114688 together, 32 query heads of 8 cached, d = 128, smoothed keys, 134 MB): 39 us and
-// 7 to join, 3.4 TB/s; 7 us of it before the first product (launch, lengths, pages, first loads, queries), the rest 4.3 TB/s.  A
+// Measured (eight caches of up to 28672 tokens, 114688 together, 32 query heads of 8 cached, d = 128, smoothed keys, 134 MB): 38 us and
+// 6 to join, 3.5 TB/s; 7 us of it before the first product (launch, lengths, pages, first loads, queries), the rest 4.3 TB/s.  A
 // third buffer of loads, three workgroups to a compute unit and codes that go through LDS to load rows in order changed nothing
 // (40, 39, 38 us); with every page the same one, and so from L2, 33 us.
 template <int D, bool FULL>
@@ -57,7 +57,7 @@ __global__ __launch_bounds__(64 * kRows16Heads, D == 256 ? 1 : 2) void attention
     if (b >= a.B) return;
     const int h = hg * a.plan.waves + __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
     if (h >= a.H) return;
-    const Sequence seq(a, q_starts, kv_lens, b);
+    const Sequence seq = pieces.seq;
     const int n_q = min(seq.n_q, a.max_q);
     const Steps steps(a, seq, 0, n_q - 1, kRows16Step);
     const bool alone = pieces.count == 1;                  // no partial results

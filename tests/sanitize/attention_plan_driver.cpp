@@ -39,9 +39,9 @@ int main()
             for (int64_t &s : steps) {
                 const int64_t len = upto(4) == 1 ? max_kv : upto(5) == 1 ? 0 : upto(max_kv);
                 s = (len + kRows16Step - 1) / kRows16Step;
-                total = std::min<int64_t>(total + s, 0x3FFFFFFF);
+                total += s;
             }
-            const int64_t length = p.pieces <= 1 ? 0x3FFFFFFF : std::max<int64_t>((total + p.pieces - 1) / p.pieces, p.piece_steps);
+            const int64_t length = p.pieces <= 1 ? 0x3FFFFFFF : std::max<int64_t>(std::min<int64_t>((total + p.pieces - 1) / p.pieces, 0x3FFFFFFF), p.piece_steps);
             for (int64_t s : steps) pieces += std::max<int64_t>((s + length - 1) / length, 1);
             const int64_t launched = p.pieces > 1 ? p.pieces + B : B;
             check(pieces <= launched, "pieces", pieces, launched);
