@@ -180,9 +180,11 @@ struct Sight {
 
 // A token's weight is 2^(s + log2 g_v - m): with its page's value scale g_v in the exponent the values enter the product
 // as code * block scale, exact in f16, and the sum of the weights takes the factor out again (weight / g_v).
-// m is the row's running maximum of s + log2 g_v, raised only when a score exceeds it by kSlack binades: weights of up to
-// 2^kSlack are as good in f16 as those up to one, and most steps then need no reduction between lanes and no rescaling.
-constexpr float kSlack = 8.0f, kLowest = -3.0e38f;      // (kLowest: below every score, and 2^(-inf - kLowest) is still 0)
+// m lies kBelow binades under the row's running maximum of s + log2 g_v, and is raised to there only when a score exceeds it by
+// kAbove: weights of up to 2^kAbove fit f16, and most steps then need no reduction between lanes and no rescaling.  What f16
+// cannot hold is 2^-25, 2^-34 of the largest weight: with the maximum itself for m, 2^-25 of it, a long tail behind a token that
+// holds nearly all of the sum was lost from the product while the sum kept it.  (The six binades between the two keep raises rare.)
+constexpr float kBelow = 9.0f, kAbove = 15.0f, kLowest = -3.0e38f;      // (kLowest: below every score, and 2^(-inf - kLowest) is still 0)
 
 // E4M3 bytes in the low halves of two 16-bit lanes -> f16 values times 2^-8, exact (subnormal f16 where the byte is
 // below 2^-6), for every byte: sign bit dropped, no NaN, so slots that were never written cannot reach a sum.

@@ -320,10 +320,10 @@ __global__ __launch_bounds__(64 * kRows16Heads, D == 256 ? 1 : 2) void attention
             }
         }
         const float top = fmaxf(fmaxf(fmaxf(x[0], x[1]), fmaxf(x[2], x[3])), fmaxf(fmaxf(x[4], x[5]), fmaxf(x[6], x[7])));
-        if (__ballot(top > m + kSlack) != 0ull) {
+        if (__ballot(top > m + kAbove) != 0ull) {
             float t = fmaxf(top, __shfl_xor(top, 16, 64));
             t = fmaxf(t, __shfl_xor(t, 32, 64));
-            t = fmaxf(t, m);
+            t = fmaxf(t - kBelow, m);
             const float f = __builtin_amdgcn_exp2f(m - t);
             m = t;
             l *= f;

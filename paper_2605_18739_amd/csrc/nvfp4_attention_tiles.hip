@@ -334,8 +334,8 @@ __global__ __launch_bounds__(64 * WAVES, D == 256 ? 1 : 2) void attention_tiles_
             const float t0 = fmaxf(fmaxf(v[e], v[e + 1]), v[e + 2]), t1 = fmaxf(fmaxf(v[e + 3], v[e + 4]), v[e + 5]);
             top = fmaxf(top, __builtin_fmaf(fmaxf(fmaxf(t0, t1), fmaxf(v[e + 6], v[e + 7])), f[g], log_v[g]));
         }
-        if (__ballot(top > m + kSlack) != 0ull) {
-            const float raised = fmaxf(fmaxf(top, __shfl_xor(top, 32, 64)), m);
+        if (__ballot(top > m + kAbove) != 0ull) {
+            const float raised = fmaxf(fmaxf(top, __shfl_xor(top, 32, 64)) - kBelow, m);
             const float r = __builtin_amdgcn_exp2f(m - raised);
             m = raised;
             l *= r;
