@@ -445,9 +445,10 @@ int nvfp4_kv_cache_read(const nvfp4_kv_cache *cache, const int64_t *slots, int64
  *   lse: fp32 [total_q, Hq], log of the sum of the exponentials (natural), or NULL; what joins this result with attention
  *     over other tokens
  * A query that sees nothing gets zeros and lse = -inf.  Rows of out and lse that no sequence owns are left as they were.
- * Scores, their maxima and sums and the accumulation are fp32.  The probabilities, times their page's value scale, enter the second
- * product as f16 (fp32 output: as the sum of two f16 numbers): within 2^-11 (2^-22) of each, and no closer than 2^-34 of the row's
- * largest such product.  Their sum is that of the unrounded ones.
+ * Scores, their maxima and sums and the accumulation are fp32.  The probabilities enter the second product as f16 (fp32 output: as
+ * the sum of two f16 numbers): within 2^-11 (2^-22) of each, and no closer than 2^-30 of the row's largest, whatever the pages'
+ * scales are; their sum is that of the unrounded ones.  Pages whose value scale is below 2^-64 of another one's of the same
+ * sequence, or below 2^-100, lose digits of their values.
  * Refused (NVFP4_ERR_SHAPE) besides the above: more than 2^30 pages, pages whose block scales or row means fill 4 GiB, and
  * more rows or sequences than one launch covers (2^32 lanes).
  * workspace: nvfp4_kv_attention_workspace_bytes() bytes, 16-byte aligned (0 bytes: may be NULL): partial results where the

@@ -20,19 +20,11 @@ struct AttentionArgs {
     float *lse;
     AttentionPlan plan;
     float *part_o;                        // [partial row][d], partial sums relative to ...
-    float2 *part_ml;                      // [partial row] their row's maximum (base 2) and sum
+    float2 *part_ml;                      // [partial row] ... 2^r of their row, and r (base 2) and the sum of its weights
     Divisor by_page;
     uint32_t token_codes, token_scales;   // bytes of a slot: codes, scales
     uint32_t page_scales, page_means;     // bytes of a page: scales, means
 };
-
-// A page's tensor scale.  Pages that are not in use may hold anything: where a step touches one its tokens are masked, and a
-// scale of one keeps NaN and infinities out of the sums that they enter with weight zero.  (Blocks of rows see to it in the
-// turns that mask: tested for every step that they load, it costs the accumulators of d = 256 their registers, 432 -> 500 us.)
-__device__ __forceinline__ float page_scale(uint32_t bits)
-{
-    return __uint_as_float(bits - 0x00800000u < 0x7F000000u ? bits : 0x3F800000u);      // (positive and normal)
-}
 
 // Sixteen cached tokens of a page: where their slots begin in each plane, as scalar bases for a lane's 32-bit offset.  (Two
 // 32 x 32 bit products give them all, codes being eight times as long as scales.)
@@ -178,13 +170,81 @@ struct Sight {
     __device__ __forceinline__ bool of(int j) const { return (j <= p) & ((j > after) | (j < sink)); }
 };
 
-// A token's weight is 2^(s + log2 g_v - m): with its page's value scale g_v in the exponent the values enter the product
-// as code * block scale, exact in f16, and the sum of the weights takes the factor out again (weight / g_v).
-// m lies kBelow binades under the row's running maximum of s + log2 g_v, and is raised to there only when a score exceeds it by
-// kAbove: weights of up to 2^kAbove fit f16, and most steps then need no reduction between lanes and no rescaling.  What f16
-// cannot hold is 2^-25, 2^-34 of the largest weight: with the maximum itself for m, 2^-25 of it, a long tail behind a token that
-// holds nearly all of the sum was lost from the product while the sum kept it.  (The six binades between the two keep raises rare.)
-constexpr float kBelow = 9.0f, kAbove = 15.0f, kLowest = -3.0e38f;      // (kLowest: below every score, and 2^(-inf - kLowest) is still 0)
+// A token's weight in the second product is 2^(s - m) g / 2^U = 2^(s + log2 g - r), r = m + U, and the values enter it as code *
+// block scale, exact in f16.
+//   m   lies kBelow binades (rounded down to a whole number, which r then is too) under the row's running maximum of s, and is
+//       raised to there only when a score exceeds it by kAbove: most steps then need no reduction between lanes and no rescaling.
+//   g   value scale of the token's page; the sum of the weights takes it out again.
+//   2^U the unit in which a wave counts.  It stays where it is while the exponents of a step's pages are kUnitLow .. kUnitHigh from it
+//       (pages whose scales differ by a few times), else it moves and the accumulators are rescaled.  Pages of one step that no
+//       unit holds for together are taken in walks of their own over the steps that have such ones.  (With weights relative
+//       to the largest 2^s g, a page of large scale and small values cost the others their digits; a page of zeros has scale one.)
+// Weights stay below 2^(kAbove + 1 + kUnitHigh) = 2^15.  What f16 cannot hold is 2^-25, and so 2^-30 of the largest 2^s (kBelow
+// and kUnitLow) whatever the pages' scales are; with the maximum itself for m a long tail behind a token with nearly all of the
+// sum was lost from the product while the sum kept it.
+// The unit does not go below 2^-100, nor further than kUnitReach below the largest that it has been: no rescaling overflows (2^15 *
+// 2688 * 2^30 tokens are 2^57), and neither does a sum of weights / g.  Pages that it does not reach lose digits, and from kUnitLost
+// below it on their weights count in the sum alone.
+constexpr float kBelow = 7.0f, kAbove = 13.0f, kLowest = -3.0e38f;      // (kLowest: below every score, and 2^(-inf - kLowest) is still 0)
+constexpr int kUnitLow = -2, kUnitHigh = 1, kUnitReach = 64, kUnitLost = 40, kUnitBias = 127, kUnitLeast = 27;       // (exponent fields as in fp32)
+constexpr int kNoUnit = -512;
+struct Units {
+    int now, top;                         // U as an fp32 exponent field (at first kNoUnit), and the largest it has been
+    __device__ __forceinline__ bool holds(int e) const { return (uint32_t)(e - now - kUnitLow) <= (uint32_t)(kUnitHigh - kUnitLow); }
+    // for a page with exponent field e: log2 g and 1 / g as they enter a weight and the sum
+    __device__ __forceinline__ void page(int e, float &log_g, float &inv_g) const
+    {
+        if (e < now - kUnitLost) {
+            log_g = (float)(now - kUnitBias - kUnitLost);
+            inv_g = __builtin_amdgcn_exp2f(-log_g);
+        }
+    }
+    // Groups of sixteen tokens, a bit each in `groups`, their pages' exponent fields the bytes of e.  Those that one unit can hold for
+    // make a class, from the largest on (so that the classes do not depend on the unit).  Of class number `pass` the bits, and
+    // in `groups` what the classes behind it have; the unit is made to hold.
+    template <int GROUPS>
+    __device__ __forceinline__ uint32_t enter(uint32_t e, uint32_t &groups, int pass)
+    {
+        uint32_t mine = 0u;
+        int largest = 0;
+        bool held = true;
+        for (int k = 0; k <= pass; ++k) {
+            groups &= ~mine;
+            mine = 0u;
+            largest = 0;
+            held = true;
+#pragma unroll
+            for (int g = 0; g < GROUPS; ++g)
+                if ((groups >> g & 1u) != 0u) largest = max(largest, (int)(e >> 8 * g & 255u));
+#pragma unroll
+            for (int g = 0; g < GROUPS; ++g) {
+                const int eg = (int)(e >> 8 * g & 255u);
+                if ((groups >> g & 1u) == 0u || eg < largest - (kUnitHigh - kUnitLow)) continue;
+                mine |= 1u << g;
+                held &= holds(eg);
+            }
+        }
+        groups &= ~mine;
+        if (!held) {
+            now = max(max(largest - kUnitHigh, kUnitLeast), top - kUnitReach);
+            top = max(top, now);
+        }
+        return mine;
+    }
+};
+// Does a unit hold for the exponent fields in the four bytes of e?  Its lowest one in every byte, subtracted, leaves less than four in each; a
+// difference that is negative borrows and leaves higher bits.
+static_assert(kUnitHigh - kUnitLow == 3);
+__device__ __forceinline__ uint32_t unit_lowest4(int now) { return (uint32_t)(now + kUnitLow) * 0x01010101u; }
+__device__ __forceinline__ bool unit_holds4(uint32_t lowest4, uint32_t e) { return ((e - lowest4) & 0xFCFCFCFCu) == 0u; }
+// exponent field of a page's scale: 4 .. 254 whatever stands there (255: not a page of the cache), so that zero is the lowest one of no unit
+__device__ __forceinline__ uint32_t scale_exponent(uint32_t bits) { return min(max(bits >> 23 & 255u, 4u), 254u); }
+constexpr uint32_t kNoPage = 255u;
+// do some of the rows at positions p0 .. p1 see some of the sixteen tokens from `first` on?
+__device__ __forceinline__ bool group_seen(int first, int p0, int p1, int window, int sink)
+{
+    return (first <= p1) & ((window <= 0) | (first + 15 > p0 - window) | (first < sink));
+}
 
 // E4M3 bytes in the low halves of two 16-bit lanes -> f16 values times 2^-8, exact (subnormal f16 where the byte is
 // below 2^-6), for every byte: sign bit dropped, no NaN, so slots that were never written cannot reach a sum.

@@ -72,9 +72,9 @@ __global__ __launch_bounds__(64 * kRows16Heads, D == 256 ? 1 : 2) void attention
     };
     const bool second = lane >= 32;
     const GlobalBytes table = scalar_base(page_table, (uint64_t)b * a.max_pages * 4), k_scale = scalar_base(k_global, 0), v_scale = scalar_base(v_global, 0);
-    auto look_up = [&](int n) {
+    auto look_up = [&](int n, int to) {
         Ahead p;
-        p.first = steps.first_token(min(n, n1 - 1), kRows16Step);
+        p.first = steps.first_token(min(n, to - 1), kRows16Step);
         uint32_t at[2];
 #pragma unroll
         for (int x = 0; x < 2; ++x) {  // (a group past the length is masked; it may be past the table: the step's first group stands in)
@@ -121,12 +121,12 @@ __global__ __launch_bounds__(64 * kRows16Heads, D == 256 ? 1 : 2) void attention
     const uint32_t ks_from = 4u * (r * kTokenLanes + (D == 64 ? 0 : g >> 1)), vs_from = 4u * (4 * g * kTokenLanes + (D == 64 ? 0 : r >> 3));
     auto from_lane = [](uint32_t lane4, uint32_t v) { return (uint32_t)__builtin_amdgcn_ds_bpermute((int)lane4, (int)v); };
     auto as_loaded = [](uint32_t &v) { asm volatile("" : "+v"(v)); };
-    // fetches the step whose pages were looked up, and looks up those of step n
-    auto fetch = [&](Ahead &p, Step<D, FULL> &s, int n) {
+    // fetches the step whose pages were looked up, and looks up those of step n (or of the last one, to - 1)
+    auto fetch = [&](Ahead &p, Step<D, FULL> &s, int n, int to) {
         as_loaded(p.page);
         uint32_t pages[2] = {(uint32_t)__builtin_amdgcn_readfirstlane((int)p.page), (uint32_t)__builtin_amdgcn_readlane((int)p.page, 32)};
         const Ahead now = p;
-        p = look_up(n);
+        p = look_up(n, to);
         // (offsets are widened where they are used: widened once in front of the loop, they would no longer be known to have 32 bits)
         if constexpr (FULL) as_loaded(scales_at);
         as_loaded(mean_at);
@@ -200,8 +200,8 @@ __global__ __launch_bounds__(64 * kRows16Heads, D == 256 ? 1 : 2) void attention
     Step<D, FULL> sa, sb;
     Ahead ahead = {};
     if (n0 < n1) {
-        ahead = look_up(n0);
-        fetch(ahead, sa, n0 + 1);
+        ahead = look_up(n0, n1);
+        fetch(ahead, sa, n0 + 1, n1);
     }
 
     // ---- queries
@@ -236,14 +236,18 @@ __global__ __launch_bounds__(64 * kRows16Heads, D == 256 ? 1 : 2) void attention
         sum_q = g == 0 ? __builtin_amdgcn_ldexpf(sum, e) : 0.0f;       // (the outer product has four terms, three of them zero)
     }
 
-    float m = kLowest, l = 0.0f;
+    float m = kLowest, ref = kLowest, l = 0.0f;            // ref: the r of a weight
+    Units units = {kNoUnit, kNoUnit};
+    constexpr uint32_t kNoLowest = 0x10000u;
+    uint32_t lowest = kNoLowest;                           // lowest exponent that the unit holds for (none: not the first walk)
+    int pass = 0, again_from = 0x7FFFFFFF, again_to = 0;   // walks over the steps; those with a page for the next walk
     float4v o[NT];
 #pragma unroll
     for (int j = 0; j < NT; ++j) o[j] = float4v{0.0f, 0.0f, 0.0f, 0.0f};
 
     // (what a step loaded is used as it is where it is taken, and no earlier: folded into the turn before, the first shift
     //  or mask of a loaded value would wait for all of them there)
-    auto take = [&](Step<D, FULL> &s) {
+    auto take = [&](Step<D, FULL> &s, int n) {
         float x[8];
         as_loaded(s.kg), as_loaded(s.vg);
 #pragma unroll
@@ -286,12 +290,13 @@ __global__ __launch_bounds__(64 * kRows16Heads, D == 256 ? 1 : 2) void attention
             two[0] = __uint_as_float((uint32_t)__builtin_amdgcn_readfirstlane((int)__float_as_uint(v)));
             two[1] = __uint_as_float((uint32_t)__builtin_amdgcn_readlane((int)__float_as_uint(v), 32));
         };
-        const float kg = page_scale(s.kg), vg = page_scale(s.vg);
+        const float kg = __uint_as_float(s.kg), vg = __uint_as_float(s.vg);        // (of a page that is not in use, anything)
         float f[2], inv_k[2], log_v[2], inv_v[2];
         of_pages(kg, f);
         if constexpr (SMOOTH) of_pages(__builtin_amdgcn_rcpf(kg), inv_k);
         of_pages(__builtin_amdgcn_logf(vg), log_v);
         of_pages(__builtin_amdgcn_rcpf(vg), inv_v);
+        const bool known = __ballot((s.vg >> 23) - lowest > (uint32_t)(kUnitHigh - kUnitLow)) == 0ull;         // (the unit holds for both pages)
         auto key_word = [&](int t, int c) {
             if constexpr (FULL) return kw[t];
             else return s.ks[t][c];
@@ -307,25 +312,48 @@ __global__ __launch_bounds__(64 * kRows16Heads, D == 256 ? 1 : 2) void attention
                 acc = __builtin_amdgcn_mfma_f32_16x16x32_f16(eight_codes(s.k[t][c], sk), q[c], acc, 0, 0, 0);
             }
 #pragma unroll
-            for (int e = 0; e < 4; ++e) x[4 * t + e] = __builtin_fmaf(acc[e], factor * f[t], log_v[t]);
+            for (int e = 0; e < 4; ++e) x[4 * t + e] = acc[e] * (factor * f[t]);
         }
         // tokens that some row does not see (the same for the whole wave)
         const bool masked = !(s.valid[0] & s.valid[1]) || s.first + kRows16Step - 1 > seq.p0 ||
                             (a.window > 0 && s.first <= seq.position(a, n_q - 1) - a.window);
-        if (masked) {
+        bool moved = false;
+        if (masked | !known) {
+            uint32_t left = 0u;                                // pages of which some row sees some token
 #pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                const int j = s.first + 16 * (e >> 2) + 4 * g + (e & 3);
-                x[e] = (s.valid[e >> 2] & sight.of(j)) ? x[e] : -__builtin_inff();
+            for (int t = 0; t < 2; ++t)
+                if (s.valid[t] & group_seen(s.first + 16 * t, seq.p0, seq.position(a, n_q - 1), a.window, a.sink)) left |= 1u << t;
+            if (masked) {
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    const int j = s.first + 16 * (e >> 2) + 4 * g + (e & 3);
+                    x[e] = (s.valid[e >> 2] & sight.of(j)) ? x[e] : -__builtin_inff();
+                }
+            }
+            // the unit of the pages: it moves in front of the step, and a page that is far from the other one waits for another walk
+            if (!known | (left != 3u)) {
+                const uint32_t ev = scale_exponent((uint32_t)__builtin_amdgcn_readfirstlane((int)s.vg)) | scale_exponent((uint32_t)__builtin_amdgcn_readlane((int)s.vg, 32)) << 8;
+                const int before = units.now;
+                if (__ballot(m > kLowest) != 0ull) units.top = max(units.top, before);        // (it has been used)
+                const uint32_t mine = units.enter<2>(ev, left, pass);
+                if (left != 0u) again_from = min(again_from, n), again_to = n + 1;
+#pragma unroll
+                for (int t = 0; t < 2; ++t) {
+                    units.page((int)(ev >> 8 * t & 255u), log_v[t], inv_v[t]);
+                    log_v[t] = (mine >> t & 1u) != 0u ? log_v[t] : -__builtin_inff();
+                    inv_v[t] = (mine >> t & 1u) != 0u ? inv_v[t] : 0.0f;
+                }
+                moved = units.now != before;
+                lowest = pass == 0 ? (uint32_t)(units.now + kUnitLow) : kNoLowest;
             }
         }
         const float top = fmaxf(fmaxf(fmaxf(x[0], x[1]), fmaxf(x[2], x[3])), fmaxf(fmaxf(x[4], x[5]), fmaxf(x[6], x[7])));
-        if (__ballot(top > m + kAbove) != 0ull) {
+        if (__ballot(top > m + kAbove) != 0ull || moved) {
             float t = fmaxf(top, __shfl_xor(top, 16, 64));
             t = fmaxf(t, __shfl_xor(t, 32, 64));
-            t = fmaxf(t - kBelow, m);
-            const float f = __builtin_amdgcn_exp2f(m - t);
-            m = t;
+            m = fmaxf(floorf(t - kBelow), m);
+            const float to = m + (float)(units.now - kUnitBias), f = __builtin_amdgcn_exp2f(ref - to);
+            ref = to;
             l *= f;
 #pragma unroll
             for (int j = 0; j < NT; ++j) o[j] *= f;
@@ -334,15 +362,17 @@ __global__ __launch_bounds__(64 * kRows16Heads, D == 256 ? 1 : 2) void attention
 #pragma unroll
         for (int t = 0; t < 2; ++t) {
             float sum = 0.0f;
+            const float add = log_v[t] - ref;
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
-                const float v = __builtin_amdgcn_exp2f(x[4 * t + e] - m);
+                const float v = __builtin_amdgcn_exp2f(x[4 * t + e] + add);
                 sum += v;
                 w[4 * t + e] = (_Float16)v;
                 if constexpr (F32) w_low[4 * t + e] = (_Float16)(v - (float)w[4 * t + e]);
             }
             l = __builtin_fmaf(sum, inv_v[t], l);
         }
+        asm volatile("" : "+v"(l));                            // (here: put off, the weights would wait for it in registers)
 #pragma unroll
         for (int t = 0; t < 8; ++t) {
             as_loaded(s.v[t]);
@@ -386,14 +416,27 @@ __global__ __launch_bounds__(64 * kRows16Heads, D == 256 ? 1 : 2) void attention
         if constexpr (D == 256) half_row(s.v_hi, std::integral_constant<int, 8>());
     };
 
-    // two steps a turn, so that neither is copied; what is fetched past the last step is the last step again
-    __builtin_amdgcn_s_waitcnt(0x0F70);                    // vmcnt(0): the turns count their own loads alone
-    for (int n = n0; n < n1; n += 2) {
-        fetch(ahead, sb, n + 2);
-        take(sa);
-        if (n + 1 >= n1) break;
-        fetch(ahead, sa, n + 3);
-        take(sb);
+    // two steps a turn, so that neither is copied; what is fetched past the last step is the last step again.  Pages that a walk
+    // leaves out are taken by another one over the steps that have some.
+    for (int from = n0, to = n1; from < to; ++pass) {
+        __builtin_amdgcn_s_waitcnt(0x0F70);                // vmcnt(0): the turns count their own loads alone
+        if (pass == 0) {                                   // (the unit of the first page, which most first steps find to hold)
+            units.now = max((int)scale_exponent((uint32_t)__builtin_amdgcn_readfirstlane((int)sa.vg)), kUnitLeast);
+            lowest = (uint32_t)(units.now + kUnitLow);
+        }
+        for (int n = from; n < to; n += 2) {
+            fetch(ahead, sb, n + 2, to);
+            take(sa, n);
+            if (n + 1 >= to) break;
+            fetch(ahead, sa, n + 3, to);
+            take(sb, n + 1);
+        }
+        from = again_from, to = again_to;
+        again_from = 0x7FFFFFFF, again_to = 0, lowest = kNoLowest;
+        if (from < to) {
+            ahead = look_up(from, to);
+            fetch(ahead, sa, from + 1, to);
+        }
     }
 
     // ---- the row's sum, and the result: element (4 g + e) NT + j of row r stands in o[j][e]
@@ -403,7 +446,7 @@ __global__ __launch_bounds__(64 * kRows16Heads, D == 256 ? 1 : 2) void attention
     const int64_t out_row = query * a.Hq + head;
     if (alone) {
         const float inv = l > 0.0f ? 1.0f / l : 0.0f;
-        if (a.lse && g == 0) a.lse[out_row] = l > 0.0f ? (m + __builtin_amdgcn_logf(l)) * 0.6931471805599453f : -__builtin_inff();
+        if (a.lse && g == 0) a.lse[out_row] = l > 0.0f ? (ref + __builtin_amdgcn_logf(l)) * 0.6931471805599453f : -__builtin_inff();
         const int64_t at = query * a.ldo + (int64_t)head * d;
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
@@ -420,7 +463,7 @@ __global__ __launch_bounds__(64 * kRows16Heads, D == 256 ? 1 : 2) void attention
         return;
     }
     const int64_t part = ((int64_t)at * a.max_q + i) * a.Hq + head;
-    if (g == 0) a.part_ml[part] = float2{m, l};
+    if (g == 0) a.part_ml[part] = float2{ref, l};
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
         const int first = (4 * g + e) * NT;

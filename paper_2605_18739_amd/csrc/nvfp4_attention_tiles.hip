@@ -26,11 +26,17 @@ struct Tiles {
     static constexpr int kTasks = 4 * D / kThreads;       // blocks of keys, and pieces of values, of a lane
     uint8_t k[2][kTileStep * D * 2];      // [token][D] f16
     uint8_t v[2][D * kTileStep * 2];      // [element][token] f16
-    struct {
+    struct alignas(16) {
         float mean[kTileStep];            // row mean / g_k
         float kg[4], log_v[4], inv_v[4];  // of the four groups of sixteen tokens
-        uint32_t valid[4];
+        uint8_t exponent[4];              // of their value scales
     } of[2];
+    // what only some steps ask for, kept out of the scalar registers, which the addresses of a step's loads fill
+    struct {
+        int p0, p1, window, sink;         // positions of the block's first and last query
+        int unit[WAVES], unit_top[WAVES];
+        int pass, again_from[4], again_to[4];       // number of the walk, and of each the steps with groups for the next one
+    } rare;
 };
 
 // (integral constants 0 .. N - 1, for code that has to be laid out by hand)
@@ -121,9 +127,9 @@ __global__ __launch_bounds__(64 * WAVES, D == 256 ? 1 : 2) void attention_tiles_
     auto group_of = [&](int t) { return (64 * wave + t * kThreads) / (16 * NB); };
     auto as_loaded = [](uint32_t &v) { asm volatile("" : "+v"(v)); };
     const GlobalBytes table = scalar_base(page_table, (uint64_t)b * a.max_pages * 4), k_scale = scalar_base(k_global, 0), v_scale = scalar_base(v_global, 0);
-    auto look_up = [&](int n) {
+    auto look_up = [&](int n, int to) {
         Ahead p;
-        const int first = steps.first_token(min(n, n1 - 1), kTileStep);
+        const int first = steps.first_token(min(n, to - 1), kTileStep);
 #pragma unroll
         for (int t = 0; t < kTasks; ++t) {  // (a group past the length is masked; it may be past the table: the step's first group stands in)
             const int token = first + 16 * group_of(t) < seq.len ? first + 16 * group_of(t) : first;
@@ -133,8 +139,8 @@ __global__ __launch_bounds__(64 * WAVES, D == 256 ? 1 : 2) void attention_tiles_
         }
         return p;
     };
-    // fetches the step whose pages were looked up, and looks up those of step n
-    auto fetch = [&](Ahead &p, Share &s, int n) {
+    // fetches the step whose pages were looked up, and looks up those of step n (or of the last one, to - 1)
+    auto fetch = [&](Ahead &p, Share &s, int n, int to) {
         uint32_t pages[kTasks];
 #pragma unroll
         for (int t = 0; t < kTasks; ++t) {
@@ -142,7 +148,7 @@ __global__ __launch_bounds__(64 * WAVES, D == 256 ? 1 : 2) void attention_tiles_
             pages[t] = (uint32_t)__builtin_amdgcn_readfirstlane((int)p.page[t]);
         }
         const Ahead now = p;
-        p = look_up(n);
+        p = look_up(n, to);
         // (offsets are widened where they are used: widened once in front of the loop, they would no longer be known to have 32 bits)
         as_loaded(k_at), as_loaded(ks_at), as_loaded(v_at0), as_loaded(v_at1), as_loaded(vs_at0), as_loaded(vs_at1), as_loaded(mean_at);
 #pragma unroll
@@ -193,7 +199,7 @@ __global__ __launch_bounds__(64 * WAVES, D == 256 ? 1 : 2) void attention_tiles_
                     lds.of[stage].kg[group_of(t)] = kg;
                     lds.of[stage].log_v[group_of(t)] = __builtin_amdgcn_logf(vg);
                     lds.of[stage].inv_v[group_of(t)] = __builtin_amdgcn_rcpf(vg);
-                    lds.of[stage].valid[group_of(t)] = s.valid[t] ? 1u : 0u;
+                    lds.of[stage].exponent[group_of(t)] = (uint8_t)(s.valid[t] ? scale_exponent(s.vg[t]) : kNoPage);
                 }
             }
         } else {
@@ -208,8 +214,8 @@ __global__ __launch_bounds__(64 * WAVES, D == 256 ? 1 : 2) void attention_tiles_
     Share share;
     Ahead ahead = {};
     if (n0 < n1) {
-        ahead = look_up(n0);
-        fetch(ahead, share, n0 + 1);
+        ahead = look_up(n0, n1);
+        fetch(ahead, share, n0 + 1, n1);
     }
 
     // ---- queries of this wave's rows: lane holds row c32, elements 16 step + 8 hi .. + 7 of every k step
@@ -242,13 +248,19 @@ __global__ __launch_bounds__(64 * WAVES, D == 256 ? 1 : 2) void attention_tiles_
         sum_q = hi == 0 ? __builtin_amdgcn_ldexpf(sum, e) : 0.0f;        // (the outer product has two terms, one of them zero)
     }
 
-    float m = kLowest, l = 0.0f;
+    float m = kLowest, r = kLowest, l = 0.0f;
+    uint32_t lowest4 = 0u;                                 // of the wave's unit (0: none yet, or not the first walk)
     float16v o[D / 32];
 #pragma unroll
     for (int t = 0; t < D / 32; ++t)
 #pragma unroll
         for (int e = 0; e < 16; ++e) o[t][e] = 0.0f;
 
+    // steps from sure_from on (a window's rear) up to sure_to (the first query) are seen whole by all rows
+    const int sure_to = seq.position(a, i0) - kTileStep + 1, sure_from = a.window > 0 ? seq.position(a, i1) - a.window : -1;
+    if (tid == 0) lds.rare.p0 = seq.position(a, i0), lds.rare.p1 = seq.position(a, i1), lds.rare.window = a.window, lds.rare.sink = a.sink;
+    if (lane == 0) lds.rare.unit[tid >> 6] = lds.rare.unit_top[tid >> 6] = kNoUnit;
+    if (tid < 4) lds.rare.again_from[tid] = 0x7FFFFFFF, lds.rare.again_to[tid] = 0;
     const bool busy = row0 + 32 * wave < n_q * a.G;        // (a wave behind the last row only loads)
     // this lane's chunks: keys 2 c + hi of row c32 (+ 32), values 2 g + hi of row c32 (+ 32 c, whose key has bit 2 the other way where c is odd)
     uint32_t k_from = (uint32_t)c32 * kKRow + (uint32_t)((hi ^ (c32 & kKeyMask)) << 4);
@@ -263,8 +275,8 @@ __global__ __launch_bounds__(64 * WAVES, D == 256 ? 1 : 2) void attention_tiles_
         constexpr int F = decltype(f)::value, g = F / VF, c = F % VF;
         return *(const half8v *)(lds_bytes + (v_from ^ (uint32_t)((g ^ ((c & 1) << 1)) << 5)) + c * 32 * kVRow);
     };
-    auto turn = [&](int n, auto runs) {
-        const int stage = (n - n0) & 1;
+    auto turn = [&](int n, int from, int to, auto runs) {
+        const int stage = (n - from) & 1;
         const auto &of = lds.of[stage];
         constexpr int kStore = kTasks * kPieces;
         const int first = steps.first_token(n, kTileStep);
@@ -272,7 +284,7 @@ __global__ __launch_bounds__(64 * WAVES, D == 256 ? 1 : 2) void attention_tiles_
         as_loaded(k_to), as_loaded(v_to), as_loaded(k_from), as_loaded(v_from);
         if constexpr (!decltype(runs)::value) {
             each<kStore>([&](auto i) { store_piece(share, stage ^ 1, i); });
-            fetch(ahead, share, n + 3);
+            fetch(ahead, share, n + 3, to);
             return;
         }
 
@@ -285,7 +297,7 @@ __global__ __launch_bounds__(64 * WAVES, D == 256 ? 1 : 2) void attention_tiles_
             mean[0] = of.mean[c32];
             mean[1] = of.mean[32 + c32];
         }
-        const uint4v valid = *(const uint4v *)of.valid;
+        const uint32_t exponents = *(const uint32_t *)of.exponent;
         float4v kg = *(const float4v *)of.kg, log_v = *(const float4v *)of.log_v, inv_v = *(const float4v *)of.inv_v;
         NVFP4_FENCE;
 #pragma unroll
@@ -301,29 +313,51 @@ __global__ __launch_bounds__(64 * WAVES, D == 256 ? 1 : 2) void attention_tiles_
             each<p1 - p0>([&](auto i) { store_piece(share, stage ^ 1, std::integral_constant<int, p0 + decltype(i)::value>()); });
             NVFP4_FENCE;
         });
+        const uint32_t there = (uint32_t)__builtin_amdgcn_readfirstlane((int)exponents);
+        const bool known = unit_holds4(lowest4, there);        // (all four pages are ones of the cache, among other things)
+        const bool masked = (first > sure_to) | (first <= sure_from);
         half8v vf[2][VF];
         each<VF>([&](auto f) { vf[0][decltype(f)::value] = v_fragment(f); });
-        fetch(ahead, share, n + 3);
+        fetch(ahead, share, n + 3, to);
 
         // ---- the row's maximum.  x[t][e]: token 32 t + 8 (e / 4) + 4 hi + e % 4, group 2 t + e / 8
-        const uint32_t all = __builtin_amdgcn_readfirstlane((int)(valid.x | valid.y << 1 | valid.z << 2 | valid.w << 3));
-        const bool masked = all != 15u || first + kTileStep - 1 > seq.position(a, i0) || (a.window > 0 && first <= seq.position(a, i1) - a.window);
-        if (masked) {
+        bool moved = false;
+        if (masked | !known) {
+            int at = first;
+            asm volatile("" : "+s"(at));                        // (what is made from it stays in here)
+            const int p0 = __builtin_amdgcn_readfirstlane(lds.rare.p0), p1 = __builtin_amdgcn_readfirstlane(lds.rare.p1);
+            const int window = __builtin_amdgcn_readfirstlane(lds.rare.window), sink = __builtin_amdgcn_readfirstlane(lds.rare.sink);
+            uint32_t seen = 0u;                                 // groups of which some row sees some token
 #pragma unroll
-            for (int t = 0; t < 2; ++t)
+            for (int g = 0; g < 4; ++g)
+                if ((there >> 8 * g & 255u) != kNoPage && group_seen(at + 16 * g, p0, p1, window, sink)) seen |= 1u << g;
+            if (masked | (seen != 15u)) {
 #pragma unroll
-                for (int e = 0; e < 16; ++e) {
-                    const int at = 32 * t + 8 * (e >> 2) + 4 * hi + (e & 3);
-                    const bool there = (all >> (2 * t + (e >> 3)) & 1u) != 0u;
-                    x[t][e] = (there & sight.of(first + at)) ? x[t][e] : -__builtin_inff();
-                }
-            // (a page that is not in use, all of whose tokens are masked: anything may stand there)
+                for (int t = 0; t < 2; ++t)
+#pragma unroll
+                    for (int e = 0; e < 16; ++e) {
+                        const int j = 32 * t + 8 * (e >> 2) + 4 * hi + (e & 3), g = 2 * t + (e >> 3);
+                        x[t][e] = (((seen >> g & 1u) != 0u) & sight.of(at + j)) ? x[t][e] : -__builtin_inff();
+                    }
+                // (of a page that is not in use anything may stand there)
+#pragma unroll
+                for (int g = 0; g < 4; ++g) kg[g] = (seen >> g & 1u) != 0u ? kg[g] : 1.0f;
+            }
+            // the unit of the pages: it moves in front of the step, and groups whose pages are far from the others' wait for another walk
+            const int before = __builtin_amdgcn_readfirstlane(lds.rare.unit[tid >> 6]), pass = __builtin_amdgcn_readfirstlane(lds.rare.pass);
+            Units units = {before, __builtin_amdgcn_readfirstlane(lds.rare.unit_top[tid >> 6])};
+            const uint32_t mine = units.enter<4>(there, seen, pass);
+            if (seen != 0u) lds.rare.again_from[pass] = min(lds.rare.again_from[pass], n), lds.rare.again_to[pass] = n + 1;      // (every wave writes the same)
 #pragma unroll
             for (int g = 0; g < 4; ++g) {
-                kg[g] = kg[g] > 0.0f && kg[g] < __builtin_inff() ? kg[g] : 1.0f;
-                log_v[g] = fabsf(log_v[g]) < 1024.0f ? log_v[g] : 0.0f;
-                inv_v[g] = fabsf(inv_v[g]) < __builtin_inff() ? inv_v[g] : 0.0f;
+                float log_g = log_v[g], inv_g = inv_v[g];
+                units.page((int)(there >> 8 * g & 255u), log_g, inv_g);
+                log_v[g] = (mine >> g & 1u) != 0u ? log_g : -__builtin_inff();
+                inv_v[g] = (mine >> g & 1u) != 0u ? inv_g : 0.0f;
             }
+            moved = units.now != before;
+            lds.rare.unit[tid >> 6] = units.now, lds.rare.unit_top[tid >> 6] = units.top;
+            lowest4 = pass == 0 && units.now != kNoUnit ? unit_lowest4(units.now) : 0u;
         }
         float f[4], top = kLowest;
 #pragma unroll
@@ -332,15 +366,15 @@ __global__ __launch_bounds__(64 * WAVES, D == 256 ? 1 : 2) void attention_tiles_
             const float16v &v = x[g >> 1];
             const int e = 8 * (g & 1);
             const float t0 = fmaxf(fmaxf(v[e], v[e + 1]), v[e + 2]), t1 = fmaxf(fmaxf(v[e + 3], v[e + 4]), v[e + 5]);
-            top = fmaxf(top, __builtin_fmaf(fmaxf(fmaxf(t0, t1), fmaxf(v[e + 6], v[e + 7])), f[g], log_v[g]));
+            top = fmaxf(top, fmaxf(fmaxf(t0, t1), fmaxf(v[e + 6], v[e + 7])) * f[g]);
         }
-        if (__ballot(top > m + kAbove) != 0ull) {
-            const float raised = fmaxf(fmaxf(top, __shfl_xor(top, 32, 64)) - kBelow, m);
-            const float r = __builtin_amdgcn_exp2f(m - raised);
-            m = raised;
-            l *= r;
+        if (__ballot(top > m + kAbove) != 0ull || moved) {
+            m = fmaxf(floorf(fmaxf(top, __shfl_xor(top, 32, 64)) - kBelow), m);
+            const float to = m + (float)(lds.rare.unit[tid >> 6] - kUnitBias), f = __builtin_amdgcn_exp2f(r - to);
+            r = to;
+            l *= f;
 #pragma unroll
-            for (int t = 0; t < VF; ++t) o[t] *= r;
+            for (int t = 0; t < VF; ++t) o[t] *= f;
         }
 
         // ---- weights, O^T = V^T P^T
@@ -348,7 +382,7 @@ __global__ __launch_bounds__(64 * WAVES, D == 256 ? 1 : 2) void attention_tiles_
         float sum[4] = {0.0f, 0.0f, 0.0f, 0.0f};
         auto weights = [&](auto group, auto pair_constant) {   // two of a group's eight
             constexpr int g = decltype(group)::value, e = 2 * decltype(pair_constant)::value;
-            const float add = log_v[g] - m;
+            const float add = log_v[g] - r;
             const float v0 = __builtin_amdgcn_exp2f(__builtin_fmaf(x[g >> 1][8 * (g & 1) + e], f[g], add));
             const float v1 = __builtin_amdgcn_exp2f(__builtin_fmaf(x[g >> 1][8 * (g & 1) + e + 1], f[g], add));
             sum[g] += v0;
@@ -379,24 +413,35 @@ __global__ __launch_bounds__(64 * WAVES, D == 256 ? 1 : 2) void attention_tiles_
         });
 #pragma unroll
         for (int g = 0; g < 4; ++g) l = __builtin_fmaf(sum[g], inv_v[g], l);
+        asm volatile("" : "+v"(l));                             // (summed up here: sunk behind the barrier, the weights would wait for it in registers)
     };
 
     // A turn reads one stage and writes the other; the barrier behind it says that both are done.  (What is fetched past the
-    // last step is the last step again.)
-    if (n0 < n1) {
+    // last step is the last step again.)  Groups that a walk leaves out are taken by another one over the steps that have some
+    // (four groups, four walks at most).
+    for (int pass = 0, from = n0, to = n1; from < to; ++pass) {
+        if (tid == 0) lds.rare.pass = pass;
+        if (pass > 0) lowest4 = 0u;
         each<kTasks * kPieces>([&](auto i) { store_piece(share, 0, i); });
-        fetch(ahead, share, n0 + 2);
+        fetch(ahead, share, from + 2, to);
         k_to ^= kKStage, v_to ^= kVStage;
         __syncthreads();
         auto walk = [&](auto runs) {
-            for (int n = n0; n < n1; ++n) {
-                turn(n, runs);
+            for (int n = from; n < to; ++n) {
+                turn(n, from, to, runs);
                 k_to ^= kKStage, v_to ^= kVStage, k_from ^= kKStage, v_from ^= kVStage;
                 __syncthreads();
             }
         };
         if (busy) walk(std::true_type());
         else walk(std::false_type());
+        if (((to - from) & 1) == 0) k_to ^= kKStage, v_to ^= kVStage;        // (the next walk begins with stage 0 again)
+        else k_from ^= kKStage, v_from ^= kVStage;
+        from = __builtin_amdgcn_readfirstlane(lds.rare.again_from[pass]), to = __builtin_amdgcn_readfirstlane(lds.rare.again_to[pass]);
+        if (from < to) {
+            ahead = look_up(from, to);
+            fetch(ahead, share, from + 1, to);
+        }
     }
 
     l += __shfl_xor(l, 32, 64);
@@ -405,7 +450,7 @@ __global__ __launch_bounds__(64 * WAVES, D == 256 ? 1 : 2) void attention_tiles_
     const int64_t out_row = query * a.Hq + head;
     if (alone) {
         const float inv = l > 0.0f ? 1.0f / l : 0.0f;
-        if (a.lse && hi == 0) a.lse[out_row] = l > 0.0f ? (m + __builtin_amdgcn_logf(l)) * 0.6931471805599453f : -__builtin_inff();
+        if (a.lse && hi == 0) a.lse[out_row] = l > 0.0f ? (r + __builtin_amdgcn_logf(l)) * 0.6931471805599453f : -__builtin_inff();
         const int64_t at = query * a.ldo + (int64_t)head * a.d;
 #pragma unroll
         for (int c = 0; c < D / 32; ++c)
@@ -419,7 +464,7 @@ __global__ __launch_bounds__(64 * WAVES, D == 256 ? 1 : 2) void attention_tiles_
         return;
     }
     const int64_t part_row = ((at - a.plan.whole) * a.plan.pieces + piece) * kRows + (32 * wave + c32);
-    if (hi == 0) a.part_ml[part_row] = float2{m, l};
+    if (hi == 0) a.part_ml[part_row] = float2{r, l};
 #pragma unroll
     for (int c = 0; c < D / 32; ++c)
 #pragma unroll

@@ -1,8 +1,10 @@
-"""Attention over the paged cache where its weights are small: a long tail behind tokens that hold nearly all of the sum.
+"""Attention over the paged cache where its weights are small: a long tail behind tokens that hold nearly all of the sum, pages whose
+scales say little about their values.
 
 Bounds (u = 2^-24), for weights w relative to the row's largest and W their sum:
- weights   2^-11 w (two f16 numbers for fp32 output: 2^-22 w), and no less than 2^-31, each times its own token's |v|: what f16 holds
-           (2^-25 at least) where the running maximum stands at 2^9 or more, and three binades to spare.
+ weights   2^-11 w (two f16 numbers for fp32 output: 2^-22 w), and no less than 2^-30, each times its own token's |v|: what f16 holds
+           (2^-25 at least) where the running maximum stands at 2^7 or more and a page's scale takes up to two binades of it; 2^-31
+           where all pages have the scale one, an exponent that takes none.
  scores    a relative error E of every weight, numerator and denominator: 2 E A, A = sum w |v| / W.  Scores that are exact
            sums: 5 u |x| for the factor and the product (x = s log2(e)), u (|x| + 16) for what is added in the exponent, 2 u for the exponential:
            below (8 |s| + 16) u.  Others as in test_kv_attention: (d + 16) u (scale sum |q k| + 8) + 4 u |s|.
@@ -14,12 +16,12 @@ import pytest
 import torch
 
 import paper_2605_18739_amd as nv
-from tests.test_kv_attention import BF, F32, U, gen, held, run_attention, say
+from tests.test_kv_attention import BF, CHUNKS, DECODE, F32, U, attention_case, gen, held, run_attention, say
 
 pytestmark = pytest.mark.gpu
 
 
-def check_weights(got, q, c, table, lens, starts, scale, causal, out_f32, exact_scores=False):
+def check_weights(got, q, c, table, lens, starts, scale, causal, out_f32, exact_scores=False, least=2.0 ** -30, window=0, sink=0):
     """out of run_attention against 64 bits, every weight's error with its own token's values."""
     G, page, d, planes = q.shape[1] // c.H, c.page_tokens, c.d, [None if t is None else t.cpu() for t in c._native]
     got, worst = got.cpu().double(), 0.0
@@ -32,6 +34,8 @@ def check_weights(got, q, c, table, lens, starts, scale, causal, out_f32, exact_
         k, v = held(planes[0], planes[1], planes[2], planes[3], page, slots), held(planes[4], planes[5], planes[6], None, page, slots)
         p = n - rows + torch.arange(rows) if causal else torch.full((rows,), n - 1)
         see = j[None] <= p[:, None]
+        if window:
+            see &= (j[None] > p[:, None] - window) | (j[None] < sink)
         for h in range(q.shape[1]):
             qh, kh, va = q[i0:i0 + rows, h].cpu().double(), k[:, h // G], v[:, h // G].abs()
             s = (qh @ kh.T * scale).masked_fill(~see, -math.inf)
@@ -41,7 +45,7 @@ def check_weights(got, q, c, table, lens, starts, scale, causal, out_f32, exact_
             w = torch.exp(s - torch.where(some, s.amax(-1, keepdim=True), 0.0))
             W = w.sum(-1, keepdim=True).clamp(min=1e-300)
             o, A = w @ v[:, h // G] / W, w @ va / W
-            lost = torch.where(see, (w * 2.0 ** (-22 if out_f32 else -11)).clamp(min=2.0 ** -31), 0.0) @ va / W
+            lost = torch.where(see, (w * 2.0 ** (-22 if out_f32 else -11)).clamp(min=least), 0.0) @ va / W
             bound = (4 * U if out_f32 else 2.0 ** -8) * o.abs() + lost + (2 * E + (n + 8) * U) * A
             err = (got[i0:i0 + rows, h] - o).abs()
             worst = max(worst, float((err / bound.clamp(min=1e-300)).max()))
@@ -75,4 +79,75 @@ def test_a_long_tail_behind_dominant_tokens(queries, out_f32, d, n):
         q[:, 1] = 0.9375                                            # (the other head's distance is a sixteenth less)
         scale = below * math.log(2) / d
         out, _ = run_attention(c, table, [n], [0, queries], q, queries, False, scale=scale, out_f32=out_f32, check=False)
-        check_weights(out, q, c, table, [n], [0, queries], float(torch.tensor(scale, dtype=F32)), False, out_f32, exact_scores=True)
+        check_weights(out, q, c, table, [n], [0, queries], float(torch.tensor(scale, dtype=F32)), False, out_f32, exact_scores=True, least=2.0 ** -31)
+
+@pytest.mark.parametrize("out_f32", [False, True])
+def test_weights_of_ordinary_caches(out_f32):
+    for causal, cases in ((True, [(lens, [1] * len(lens), *rest) for lens, *rest in DECODE]), (True, CHUNKS), (False, CHUNKS)):
+        for lens, queries, Hq, H, d, page, smooth, what in cases:
+            say("[precision] ordinary", what, causal, out_f32)
+            c, table, starts, q = attention_case(61, lens, queries, Hq, H, d, page, smooth, gain=2.0)
+            out, _ = run_attention(c, table, lens, starts, q, max(queries), causal, out_f32=out_f32, check=False)
+            check_weights(out, q, c, table, lens, starts, d ** -0.5, causal, out_f32)
+
+# ---------------------------------------------------------------------------------------------------------------------
+# page scales
+# ---------------------------------------------------------------------------------------------------------------------
+@pytest.mark.parametrize("queries", [1, 40])
+@pytest.mark.parametrize("out_f32", [False, True])
+@pytest.mark.parametrize("d,page,smooth", [(64, 16, False), (80, 48, False), (128, 64, True), (128, 16, True), (256, 32, False)])
+@pytest.mark.parametrize("scale", [1e-5, 2e-7, 2e-8, 1e-15])
+def test_pages_of_zeros_with_a_scale_of_one(queries, out_f32, d, page, smooth, scale):
+    """A page of zeros, whose scale the chunk quantizers set to one, first, last or in between: the others keep their digits."""
+    say("[precision] zeros", queries, out_f32, d, page, smooth, scale)
+    lens = [page, 3 * page, 7 * page + 5, 700]
+    c, table, starts, q = attention_case(62, lens, [queries] * 4, 4, 2, d, page, smooth)
+    c.v_global.copy_(scale * (0.3 + torch.rand(c.n_pages, generator=gen(63))))
+    for b, zero in enumerate(([], [0], [2, 5], [1, 3, (700 - 1) // page])):
+        for p in zero:
+            c.v_codes[table[b, p]], c.v_global[table[b, p]] = 0, 1.0
+    out, _ = run_attention(c, table, lens, starts, q, queries, False, out_f32=out_f32, check=False)
+    check_weights(out, q, c, table, lens, starts, d ** -0.5, False, out_f32)
+
+
+@pytest.mark.parametrize("queries", [1, 4, 40, 150])
+@pytest.mark.parametrize("out_f32", [False, True])
+@pytest.mark.parametrize("d,page", [(64, 16), (80, 16), (128, 16), (128, 32), (128, 80), (256, 16)])
+def test_page_scales_of_all_magnitudes(queries, out_f32, d, page):
+    """Scales up to 2^60 apart, from page to page, and what a page holds does not go by its scale."""
+    say("[precision] magnitudes", queries, out_f32, d, page)
+    lens = [900, 150, 16]
+    c, table, starts, q = attention_case(64, lens, [min(queries, n) for n in lens], 4, 2, d, page, False)
+    g = gen(65)
+    c.v_global.copy_(2.0 ** (60 * torch.rand(c.n_pages, generator=g) - 30))
+    c.v_scales[torch.rand(c.n_pages, generator=g) < 0.5] = 0
+    for causal, window, sink in ((True, 0, 0), (False, 0, 0), (True, 100, 20)):
+        out, lse = run_attention(c, table, lens, starts, q, queries, causal, window=window, sink=sink, out_f32=out_f32, check=False)
+        check_weights(out, q, c, table, lens, starts, d ** -0.5, causal, out_f32, window=window, sink=sink)
+        again, lse_again = run_attention(c, table, lens, starts, q, queries, causal, window=window, sink=sink, out_f32=out_f32, check=False)
+        assert torch.equal(out, again) and torch.equal(lse, lse_again)
+
+
+@pytest.mark.parametrize("queries,d", [(1, 128), (5, 64), (40, 64), (40, 256), (200, 128)])
+def test_page_scales_of_all_magnitudes_in_pieces(queries, d):
+    """The same over a cache that is cut into pieces, whose units differ."""
+    say("[precision] magnitudes in pieces", queries, d)
+    c, table, starts, q = attention_case(69, [6000], [queries], 2, 1, d, 16, False)
+    g = gen(70)
+    c.v_global.copy_(2.0 ** (60 * torch.rand(c.n_pages, generator=g) - 30))
+    c.v_scales[torch.rand(c.n_pages, generator=g) < 0.5] = 0
+    for out_f32 in (False, True):
+        out, _ = run_attention(c, table, [6000], starts, q, queries, True, out_f32=out_f32, check=False)
+        check_weights(out, q, c, table, [6000], starts, d ** -0.5, True, out_f32)
+
+
+@pytest.mark.parametrize("queries", [1, 40])
+def test_scales_at_the_ends_of_the_range(queries):
+    """Results near the largest and the smallest numbers, whole and joined from pieces."""
+    say("[precision] ends", queries)
+    for exponent in (104, -100):
+        for n in (150, 6000):
+            c, table, starts, q = attention_case(66, [n], [queries], 2, 1, 64, 16, False)
+            c.v_global.copy_(2.0 ** exponent * (0.5 + torch.rand(c.n_pages, generator=gen(67))))
+            out, _ = run_attention(c, table, [n], starts, q, queries, False, out_f32=True, check=False)
+            check_weights(out, q, c, table, [n], starts, 0.125, False, True)
