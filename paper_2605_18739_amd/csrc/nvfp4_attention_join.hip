@@ -103,7 +103,6 @@ hipError_t launch_attention_join(const AttentionArgs &a, const KvAttention &k, h
 hipError_t launch_kv_attention(const KvAttention &k, void *workspace, hipStream_t s)
 {
     const KvPages &c = k.cache;
-    constexpr int64_t far = 1ll << 30;                        // (no position is that large: as good as no limit)
     AttentionArgs a{};
     a.q = k.q;
     a.ldq = k.ldq;
@@ -125,8 +124,8 @@ hipError_t launch_kv_attention(const KvAttention &k, void *workspace, hipStream_
     a.k_mean = c.k_mean;
     a.scale = k.softmax_scale * 1.4426950408889634f;
     a.causal = k.causal;
-    a.window = (int)std::min(k.window, far);
-    a.sink = (int)std::min(k.sink, far);
+    a.window = (int)std::min(k.window, kFar);
+    a.sink = (int)std::min(k.sink, kFar);
     a.out = k.out;
     a.lse = k.lse;
     a.plan = attention_plan(k.total_q, k.Hq, c.H, c.d, k.max_pages * c.page_tokens, k.B, k.max_q, k.window, k.sink);

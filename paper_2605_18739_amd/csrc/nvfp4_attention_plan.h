@@ -30,12 +30,14 @@ struct AttentionPlan {
     int64_t part_rows;      // (query, head) rows of partial results
 };
 
+constexpr int64_t kFar = 1ll << 30;                    // no position is that large: as good as no limit
+
 // max_kv: tokens of the longest cache; a window (with its sink tokens) leaves max_q queries at most so many of them to read
 inline AttentionPlan attention_plan(int64_t total_q, int64_t Hq, int64_t H, int64_t d, int64_t max_kv, int64_t B, int64_t max_q, int64_t window,
                                     int64_t sink)
 {
     AttentionPlan p{};
-    if (window > 0) max_kv = std::min(max_kv, window + max_q + std::min(sink, max_kv) + 2 * kTileStep);
+    if (window > 0) max_kv = std::min(max_kv, std::min(window, kFar) + max_q + std::min(sink, kFar) + 2 * kTileStep);
     const int64_t rows = max_q * (Hq / H);
     p.rows16 = rows <= 16;
     if (p.rows16) {

@@ -202,3 +202,13 @@ def test_more_than_a_launch_covers_is_refused():
     many = dict(Hq=4, max_q=17, max_pages=1, total_q=1 << 27)                            # 17 rows of 4 heads: a workgroup each
     assert attention(**many, B=1 << 23) == SHAPE and ws(1 << 27, 4, 4, 128, 32, 1 << 23, 17) == 0
     assert attention(**many, B=1 << 20, q=P + 2) == ALIGN
+
+
+def test_the_largest_window_is_as_good_as_none():
+    ws = nv.nvfp4_kv_attention_workspace_bytes
+    for total_q in (1, 300):
+        none = ws(total_q, 8, 2, 128, 131072, 1, total_q)
+        assert none > 0
+        for window in (131072, 1 << 40, (1 << 63) - 1):
+            for sink in (0, 1 << 40, (1 << 63) - 1):
+                assert ws(total_q, 8, 2, 128, 131072, 1, total_q, window, sink) == none, (window, sink)
