@@ -444,7 +444,8 @@ int nvfp4_kv_cache_read(const nvfp4_kv_cache *cache, const int64_t *slots, int64
  *   out: fp32 (NVFP4_OUT_F32) or bf16 (NVFP4_OUT_BF16) [total_q, Hq, d], ldo elements from token to token, rows 16-byte aligned
  *   lse: fp32 [total_q, Hq], log of the sum of the exponentials (natural), or NULL; what joins this result with attention
  *     over other tokens
- * A query that sees nothing gets zeros and lse = -inf.  Rows of out and lse that no sequence owns are left as they were.
+ * A query that sees nothing gets zeros and lse = -inf, one whose scores are no numbers NaN in both.  Rows of out and lse that no
+ * sequence owns are left as they were.
  * Scores, their maxima and sums and the accumulation are fp32.  The probabilities enter the second product as f16 (fp32 output: as
  * the sum of two f16 numbers): within 2^-11 (2^-22) of each, and no closer than 2^-30 of the row's largest, whatever the pages'
  * scales are; their sum is that of the unrounded ones.  Pages whose value scale is below 2^-64 of another one's of the same

@@ -246,6 +246,11 @@ __device__ __forceinline__ bool group_seen(int first, int p0, int p1, int window
     return (first <= p1) & ((window <= 0) | (first + 15 > p0 - window) | (first < sink));
 }
 
+// Of a row's sum of weights l relative to 2^r: what its products are multiplied by, and its log-sum-exp.  Nothing seen: zero and
+// -inf; a sum that is no number (scores that are none) stays one.
+__device__ __forceinline__ float inverse_sum(float l) { return l == 0.0f ? 0.0f : 1.0f / l; }
+__device__ __forceinline__ float log_sum(float r, float l) { return l == 0.0f ? -__builtin_inff() : (r + __builtin_amdgcn_logf(l)) * 0.6931471805599453f; }
+
 // E4M3 bytes in the low halves of two 16-bit lanes -> f16 values times 2^-8, exact (subnormal f16 where the byte is
 // below 2^-6), for every byte: sign bit dropped, no NaN, so slots that were never written cannot reach a sum.
 __device__ __forceinline__ half2v scale_pair(uint32_t b) { return __builtin_bit_cast(half2v, (b & 0x007F007Fu) << 7); }

@@ -82,12 +82,12 @@ __global__ __launch_bounds__(kJoinThreads) void attention_join_kernel(const Atte
             for (int s = 1; s < side; ++s) o += sums[s * lanes + tid];
     }
     if (sub == 0 && e < a.d) {
-        o *= l > 0.0f ? 1.0f / l : 0.0f;
+        o *= inverse_sum(l);
         const int64_t at = query * a.ldo + (int64_t)head * a.d + e;
         if (out_f32) *(float4v *)((float *)a.out + at) = o;
         else *(uint2v *)((uint16_t *)a.out + at) = uint2v{pack_bf16x2(o.x, o.y), pack_bf16x2(o.z, o.w)};
     }
-    if (a.lse && tid == 0) a.lse[out_row] = l > 0.0f ? (m + __builtin_amdgcn_logf(l)) * 0.6931471805599453f : -__builtin_inff();
+    if (a.lse && tid == 0) a.lse[out_row] = log_sum(m, l);
 }
 
 hipError_t launch_attention_join(const AttentionArgs &a, const KvAttention &k, hipStream_t s)

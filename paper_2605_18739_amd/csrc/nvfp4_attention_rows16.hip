@@ -445,8 +445,8 @@ __global__ __launch_bounds__(64 * kRows16Heads, D == 256 ? 1 : 2) void attention
     if (!row) return;
     const int64_t out_row = query * a.Hq + head;
     if (alone) {
-        const float inv = l > 0.0f ? 1.0f / l : 0.0f;
-        if (a.lse && g == 0) a.lse[out_row] = l > 0.0f ? (ref + __builtin_amdgcn_logf(l)) * 0.6931471805599453f : -__builtin_inff();
+        const float inv = inverse_sum(l);
+        if (a.lse && g == 0) a.lse[out_row] = log_sum(ref, l);
         const int64_t at = query * a.ldo + (int64_t)head * d;
 #pragma unroll
         for (int e = 0; e < 4; ++e) {

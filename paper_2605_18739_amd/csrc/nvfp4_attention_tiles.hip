@@ -449,8 +449,8 @@ __global__ __launch_bounds__(64 * WAVES, D == 256 ? 1 : 2) void attention_tiles_
     // o[c][e]: element 32 c + 8 (e / 4) + 4 hi + e % 4
     const int64_t out_row = query * a.Hq + head;
     if (alone) {
-        const float inv = l > 0.0f ? 1.0f / l : 0.0f;
-        if (a.lse && hi == 0) a.lse[out_row] = l > 0.0f ? (r + __builtin_amdgcn_logf(l)) * 0.6931471805599453f : -__builtin_inff();
+        const float inv = inverse_sum(l);
+        if (a.lse && hi == 0) a.lse[out_row] = log_sum(r, l);
         const int64_t at = query * a.ldo + (int64_t)head * a.d;
 #pragma unroll
         for (int c = 0; c < D / 32; ++c)

@@ -386,3 +386,19 @@ def test_a_query_that_is_not_finite_spoils_its_own_row_alone(queries, bad):
     keep[queries - 1, 1] = False
     assert ((out.cpu().double() - want).abs() <= bo)[keep].all() and ((lse.cpu().double() - want_lse).abs() <= bl)[keep].all()
     assert not torch.isfinite(out[queries - 1, 1].float()).all()
+
+@pytest.mark.parametrize("queries", [1, 20])
+@pytest.mark.parametrize("tokens", [20, 3000])
+def test_a_row_without_a_number_says_so(queries, tokens):
+    """A query whose scores are no numbers: its result and its log of the sum are NaN (-inf is for rows that see nothing)."""
+    say("[use] lse of NaN", queries, tokens)
+    c, table, starts, q = attention_case(51, [tokens, 100, 0], [queries] * 3, 4, 2, 64, 16, True)
+    q[queries - 1, 1, 5] = math.nan
+    q[2 * queries - 1, 3] = math.inf                                # (inf - inf in every score with keys of both signs)
+    out, lse = run_attention(c, table, [tokens, 100, 0], starts, q, queries, False, check=False)
+    for row, head in ((queries - 1, 1), (2 * queries - 1, 3)):
+        assert torch.isnan(out[row, head].float()).all() and torch.isnan(lse[row, head])
+    rest = torch.ones(lse[:3 * queries].shape, dtype=torch.bool)
+    rest[queries - 1, 1] = rest[2 * queries - 1, 3] = False
+    assert not torch.isnan(lse[:3 * queries].cpu()[rest]).any()
+    assert (lse[2 * queries:3 * queries] == -math.inf).all() and (out[2 * queries:3 * queries] == 0).all()
