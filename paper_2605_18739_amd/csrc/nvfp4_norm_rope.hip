@@ -68,6 +68,7 @@ template <bool INTER>
 struct Turns {
     float c[INTER ? 4 : 8], s[INTER ? 4 : 8];
     int partner;
+    int turned;                                          // pairs (INTER) or elements of the lane that turn, the first ones; the others pass
 
     // e: the lane's first element; pos: this token's positions
     __device__ __forceinline__ void load(const NormRopeArgs &a, int e, int lane, int64_t t)
@@ -76,8 +77,8 @@ struct Turns {
         const int P = a.pairs;
         const int first = INTER ? e >> 1 : (e < P ? e : e - P);
         partner = INTER ? lane : (e < P ? lane + (P >> 3) : lane - (P >> 3));
-        const bool turned = e < 2 * P;
-        if (!turned) partner = lane;
+        turned = INTER ? min(max(P - first, 0), 4) : e < 2 * P ? 8 : 0;
+        if (turned == 0) partner = lane;
         double pos[kRopeMaxAxes];
 #pragma unroll
         for (int x = 0; x < kRopeMaxAxes; ++x) pos[x] = x < a.axes ? (double)a.positions[t * a.axes + x] : 0.0;
@@ -86,7 +87,7 @@ struct Turns {
             const int j = first + i;
             c[i] = 1.0f;
             s[i] = 0.0f;
-            if (turned && j < P) {
+            if (i < turned) {
                 double p = pos[0];                       // the axis of pair j: the last one that starts at or before it
 #pragma unroll
                 for (int x = 1; x < kRopeMaxAxes; ++x) p = j >= a.axis_start[x] ? pos[x] : p;
@@ -104,14 +105,14 @@ struct Turns {
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
                 const float sn = TRANSPOSED ? -s[i] : s[i], p = y[2 * i], q = y[2 * i + 1];
-                y[2 * i] = __builtin_fmaf(p, c[i], -(q * sn));
-                y[2 * i + 1] = __builtin_fmaf(p, sn, q * c[i]);
+                y[2 * i] = i < turned ? __builtin_fmaf(p, c[i], -(q * sn)) : p;
+                y[2 * i + 1] = i < turned ? __builtin_fmaf(p, sn, q * c[i]) : q;
             }
         } else {
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
                 const float o = __shfl(y[i], partner, kWave), sn = TRANSPOSED ? -s[i] : s[i];
-                y[i] = __builtin_fmaf(y[i], c[i], o * sn);
+                y[i] = turned != 0 ? __builtin_fmaf(y[i], c[i], o * sn) : y[i];
             }
         }
     }

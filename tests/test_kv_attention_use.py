@@ -402,3 +402,24 @@ def test_a_row_without_a_number_says_so(queries, tokens):
     rest[queries - 1, 1] = rest[2 * queries - 1, 3] = False
     assert not torch.isnan(lse[:3 * queries].cpu()[rest]).any()
     assert (lse[2 * queries:3 * queries] == -math.inf).all() and (out[2 * queries:3 * queries] == 0).all()
+
+@pytest.mark.parametrize("interleaved,pairs", [(True, 21), (True, 8), (False, 8), (False, 16)])
+def test_elements_that_are_not_turned_stay_as_they_are(interleaved, pairs):
+    """Infinities, NaN and signed zeros from 2 P on, in values and in gradients: neither they nor their neighbours change."""
+    say("[norm_rope] not turned", interleaved, pairs)
+    g = gen(71)
+    T, H, d = 9, 5, 64
+    x = randn(g, T, H, d).to(BF)
+    rest = x[..., 2 * pairs:]
+    for n, special in enumerate((math.inf, -math.inf, math.nan, -0.0)):
+        rest[..., n::7] = special
+    positions = torch.randint(1, 5000, (T, 1), generator=g, dtype=torch.int32)
+    freqs = torch.rand(pairs, generator=g)
+    rope = nv.NVFP4Rope(positions.cuda(), freqs.cuda(), [pairs], interleaved)
+    clean = x.clone()
+    clean[..., 2 * pairs:] = 0
+    bits = lambda t: t.cpu().contiguous().view(torch.int16)
+    for run in (lambda t: nv.nvfp4_qk_norm_rope(t.cuda(), None, None, None, rope)[0], lambda t: nv.nvfp4_qk_norm_rope_backward(t.cuda(), None, None, None, None, None, rope)[0]):
+        y, turned = run(x), run(clean)
+        assert torch.equal(bits(y[..., 2 * pairs:]), bits(x[..., 2 * pairs:]))
+        assert torch.equal(bits(y[..., :2 * pairs]), bits(turned[..., :2 * pairs]))
