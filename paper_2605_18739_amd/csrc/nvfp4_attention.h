@@ -268,9 +268,9 @@ __device__ __forceinline__ half8v eight_codes(uint32_t w, half2v s)
     return join8(code_pair<0>(w) * s, code_pair<1>(w) * s, code_pair<2>(w) * s, code_pair<3>(w) * s);
 }
 
-// bf16 queries -> f16 times a power of two that puts the row's largest magnitude into [2^14, 2^15): exact but for elements
-// 2^-29 of it and less.  Returns the factor's inverse for the scores.
-__device__ __forceinline__ int row_exponent(float amax) { return amax > 0.0f ? min(max(15 - __builtin_amdgcn_frexp_expf(amax), -110), 110) : 0; }
+// bf16 queries -> f16 times 2^row_exponent, which puts the row's largest magnitude into [2^14, 2^15): exact but for elements 2^-29 of
+// it and less.  (-113 for the largest numbers; at most 110, which leaves every one above 2^-24.)
+__device__ __forceinline__ int row_exponent(float amax) { return amax > 0.0f ? min(15 - __builtin_amdgcn_frexp_expf(amax), 110) : 0; }
 __device__ __forceinline__ half8v query_pairs(uint4v w, int e)
 {
     half8v r;
@@ -287,10 +287,11 @@ __device__ __forceinline__ float absmax8(uint4v w, float m)
     for (int i = 0; i < 4; ++i) m = fmaxf(fmaxf(m, fabsf(bf16lo_to_f32(w[i]))), fabsf(bf16hi_to_f32(w[i])));
     return m;
 }
-__device__ __forceinline__ float sum8(uint4v w, float s)
+// (of the queries times 2^e, whose sum cannot overflow)
+__device__ __forceinline__ float sum8(uint4v w, int e, float s)
 {
 #pragma unroll
-    for (int i = 0; i < 4; ++i) s += bf16lo_to_f32(w[i]) + bf16hi_to_f32(w[i]);
+    for (int i = 0; i < 4; ++i) s += __builtin_amdgcn_ldexpf(bf16lo_to_f32(w[i]), e) + __builtin_amdgcn_ldexpf(bf16hi_to_f32(w[i]), e);
     return s;
 }
 

@@ -221,19 +221,19 @@ __global__ __launch_bounds__(64 * kRows16Heads, D == 256 ? 1 : 2) void attention
             if (row && e < d) w[c] = *(const uint4v *)(a.q + query * a.ldq + (int64_t)head * d + e);
         }
 #pragma unroll
-        for (int c = 0; c < KD / 8; ++c) {
-            amax = absmax8(w[c], amax);
-            if constexpr (SMOOTH) sum = sum8(w[c], sum);
-        }
+        for (int c = 0; c < KD / 8; ++c) amax = absmax8(w[c], amax);
         amax = fmaxf(amax, __shfl_xor(amax, 16, 64));
         amax = fmaxf(amax, __shfl_xor(amax, 32, 64));
         const int e = row_exponent(amax);
 #pragma unroll
-        for (int c = 0; c < KD / 8; ++c) q[c] = query_pairs(w[c], e);
+        for (int c = 0; c < KD / 8; ++c) {
+            q[c] = query_pairs(w[c], e);
+            if constexpr (SMOOTH) sum = sum8(w[c], e, sum);
+        }
         factor = __builtin_amdgcn_ldexpf(a.scale, -e);
         sum += __shfl_xor(sum, 16, 64);
         sum += __shfl_xor(sum, 32, 64);
-        sum_q = g == 0 ? __builtin_amdgcn_ldexpf(sum, e) : 0.0f;       // (the outer product has four terms, three of them zero)
+        sum_q = g == 0 ? sum : 0.0f;       // (the outer product has four terms, three of them zero)
     }
 
     float m = kLowest, ref = kLowest, l = 0.0f;            // ref: the r of a weight

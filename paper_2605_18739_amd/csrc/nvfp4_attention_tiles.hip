@@ -235,17 +235,17 @@ __global__ __launch_bounds__(64 * WAVES, D == 256 ? 1 : 2) void attention_tiles_
             if (row && e < a.d) w[c] = *(const uint4v *)(a.q + query * a.ldq + (int64_t)head * a.d + e);
         }
 #pragma unroll
-        for (int c = 0; c < D / 16; ++c) {
-            amax = absmax8(w[c], amax);
-            if constexpr (SMOOTH) sum = sum8(w[c], sum);
-        }
+        for (int c = 0; c < D / 16; ++c) amax = absmax8(w[c], amax);
         amax = fmaxf(amax, __shfl_xor(amax, 32, 64));
-        sum += __shfl_xor(sum, 32, 64);
         const int e = row_exponent(amax);
 #pragma unroll
-        for (int c = 0; c < D / 16; ++c) q[c] = query_pairs(w[c], e);
+        for (int c = 0; c < D / 16; ++c) {
+            q[c] = query_pairs(w[c], e);
+            if constexpr (SMOOTH) sum = sum8(w[c], e, sum);
+        }
+        sum += __shfl_xor(sum, 32, 64);
         factor = __builtin_amdgcn_ldexpf(a.scale, -e);
-        sum_q = hi == 0 ? __builtin_amdgcn_ldexpf(sum, e) : 0.0f;        // (the outer product has two terms, one of them zero)
+        sum_q = hi == 0 ? sum : 0.0f;        // (the outer product has two terms, one of them zero)
     }
 
     float m = kLowest, r = kLowest, l = 0.0f;

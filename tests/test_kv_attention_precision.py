@@ -151,3 +151,23 @@ def test_scales_at_the_ends_of_the_range(queries):
             c.v_global.copy_(2.0 ** exponent * (0.5 + torch.rand(c.n_pages, generator=gen(67))))
             out, _ = run_attention(c, table, [n], starts, q, queries, False, out_f32=True, check=False)
             check_weights(out, q, c, table, [n], starts, 0.125, False, True)
+
+@pytest.mark.parametrize("queries", [1, 40])
+@pytest.mark.parametrize("smooth", [False, True])
+def test_the_largest_queries(queries, smooth):
+    """Queries up to the largest bf16 number, the keys' scales (and means) as small: the results of 2^-125 times the queries."""
+    say("[precision] largest", queries, smooth)
+    gain, scale = 2.0 ** 125, 2.0 ** -9
+    c, table, starts, q = attention_case(68, [100, 20], [queries] * 2, 4, 2, 64, 16, smooth, gain=64.0)
+    q = q.clamp(-7.96875, 7.96875)
+    q[0, 0, 0] = 7.96875
+    want = run_attention(c, table, [100, 20], starts, q, queries, True, out_f32=True, scale=scale)
+    c.k_global.mul_(1 / gain)
+    if smooth:
+        c.k_mean.copy_((c.k_mean.double() / gain).to(BF))
+    big = (q.double() * gain).to(BF)
+    assert torch.isfinite(big.float()).all() and float(big.abs().max()) > 2.0 ** 127
+    got = run_attention(c, table, [100, 20], starts, big, queries, True, out_f32=True, scale=scale)
+    n = starts[-1]
+    if not smooth:                                                  # (the same digits; means and their quotients may round apart)
+        assert torch.equal(got[0][:n], want[0][:n])
