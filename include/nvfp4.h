@@ -450,8 +450,8 @@ int nvfp4_kv_cache_read(const nvfp4_kv_cache *cache, const int64_t *slots, int64
  * the sum of two f16 numbers): within 2^-11 (2^-22) of each, and no closer than 2^-30 of the row's largest, whatever the pages'
  * scales are; their sum is that of the unrounded ones.  Pages whose value scale is below 2^-64 of another one's of the same
  * sequence, or below 2^-100, lose digits of their values.
- * Refused (NVFP4_ERR_SHAPE) besides the above: more than 2^30 pages, pages whose block scales or row means fill 4 GiB, and
- * more rows or sequences than one launch covers (2^32 lanes).
+ * Refused (NVFP4_ERR_SHAPE) besides the above: a softmax_scale that is not positive, or not finite times log2(e), more than 2^30
+ * pages, pages whose block scales or row means fill 4 GiB, and more rows or sequences than one launch covers (2^32 lanes).
  * workspace: nvfp4_kv_attention_workspace_bytes() bytes, 16-byte aligned (0 bytes: may be NULL): partial results where the
  * cache is split over workgroups.
  */

@@ -706,7 +706,7 @@ int nvfp4_kv_attention(const void *q_bf16, int64_t ldq, int64_t total_q, int64_t
     max_q = std::min(max_q, total_q);
     if (!attention_sizes_ok(total_q, Hq, H, d, max_kv, B, max_q)) return NVFP4_ERR_SHAPE;
     if (!row_stride_ok(ldq, Hq, d) || !row_stride_ok(ldo, Hq, d) || window < 0 || sink < 0) return NVFP4_ERR_SHAPE;
-    if (!(softmax_scale > 0.0f) || !std::isfinite(softmax_scale)) return NVFP4_ERR_SHAPE;
+    if (!(softmax_scale > 0.0f) || !std::isfinite(softmax_scale * 1.4426950408889634f)) return NVFP4_ERR_SHAPE;      // (exponents of two are what it makes)
     if (out_dtype != NVFP4_OUT_F32 && out_dtype != NVFP4_OUT_BF16) return NVFP4_ERR_SHAPE;
     if (!aligned16(q_bf16) || !aligned16(out) || (ldq & 7) != 0 || (ldo & (out_dtype == NVFP4_OUT_BF16 ? 7 : 3)) != 0 ||
         !aligned(page_table, 4) || !aligned(kv_lens, 4) || !aligned(q_starts, 4) || !aligned(lse, 4))

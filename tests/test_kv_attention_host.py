@@ -212,3 +212,9 @@ def test_the_largest_window_is_as_good_as_none():
         for window in (131072, 1 << 40, (1 << 63) - 1):
             for sink in (0, 1 << 40, (1 << 63) - 1):
                 assert ws(total_q, 8, 2, 128, 131072, 1, total_q, window, sink) == none, (window, sink)
+
+
+def test_attention_refuses_a_scale_that_leaves_the_range_as_a_power_of_two():
+    for scale in (2.4e38, 3.4e38):
+        assert attention(scale=scale) == SHAPE, scale
+    assert attention(scale=2.3e38, q=P + 2) == ALIGN and attention(scale=1e-40, q=P + 2) == ALIGN
