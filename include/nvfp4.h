@@ -68,6 +68,8 @@ typedef struct nvfp4_tensor {
 } nvfp4_tensor;
 
 enum { NVFP4_OUT_F32 = 0, NVFP4_OUT_BF16 = 1 };
+/* or'ed to the type of nvfp4_kv_attention's output: out, lse hold nothing yet */
+enum { NVFP4_OUT_NEW = 0x100, NVFP4_LSE_NEW = 0x200 };
 enum { NVFP4_ACT_NONE = 0, NVFP4_ACT_GELU_TANH = 1 };
 enum { NVFP4_OP_QUANTIZE = 0, NVFP4_OP_KV_QUANT = 1, NVFP4_OP_GEMM_ACT_QUANT = 2, NVFP4_OP_GEMM = 3,
        NVFP4_OP_KV_DEQUANT = 4,
@@ -423,10 +425,13 @@ int nvfp4_kv_cache_write(const nvfp4_kv_cache *cache, const void *k_bf16, int64_
 
 /*
  * Reads T slots back: k_bf16_out, v_bf16_out [T, H, d] (contiguous; either may be NULL) receive
- * RN_bf16(code * block_scale * global_scale [+ row mean]), rounded once.  Rows of slots outside the cache are left as they were.
+ * RN_bf16(code * block_scale * global_scale [+ row mean]), rounded once.  Rows of slots outside the cache are left as they were
+ * (nvfp4_kv_cache_read) or become zeros (nvfp4_kv_cache_read_new, for outputs that hold nothing yet).
  */
 int nvfp4_kv_cache_read(const nvfp4_kv_cache *cache, const int64_t *slots, int64_t T, void *k_bf16_out, void *v_bf16_out,
                         void *stream);
+int nvfp4_kv_cache_read_new(const nvfp4_kv_cache *cache, const int64_t *slots, int64_t T, void *k_bf16_out, void *v_bf16_out,
+                            void *stream);
 
 /*
  * Attention over the paged cache, which is read in 4 bits:
@@ -445,7 +450,8 @@ int nvfp4_kv_cache_read(const nvfp4_kv_cache *cache, const int64_t *slots, int64
  *   lse: fp32 [total_q, Hq], log of the sum of the exponentials (natural), or NULL; what joins this result with attention
  *     over other tokens
  * A query that sees nothing gets zeros and lse = -inf, one whose scores are no numbers NaN in both.  Rows of out and lse that no
- * sequence owns are left as they were.
+ * sequence computes (in front of the first query, behind the last one, from max_q on) are left as they were, or with
+ * out_dtype | NVFP4_OUT_NEW and | NVFP4_LSE_NEW become zeros and -inf.
  * Scores, their maxima and sums and the accumulation are fp32.  The probabilities enter the second product as f16 (fp32 output: as
  * the sum of two f16 numbers): within 2^-11 (2^-22) of each, and no closer than 2^-30 of the row's largest, whatever the pages'
  * scales are; their sum is that of the unrounded ones.  Pages whose value scale is below 2^-64 of another one's of the same

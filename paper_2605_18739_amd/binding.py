@@ -121,6 +121,8 @@ def lib():
         L.nvfp4_kv_cache_write.argtypes = [c.POINTER(_CKvCache), vp, i64, vp, i64, vp, i64, c.c_int, vp]
         L.nvfp4_kv_cache_read.restype = c.c_int
         L.nvfp4_kv_cache_read.argtypes = [c.POINTER(_CKvCache), vp, i64, vp, vp, vp]
+        L.nvfp4_kv_cache_read_new.restype = c.c_int
+        L.nvfp4_kv_cache_read_new.argtypes = [c.POINTER(_CKvCache), vp, i64, vp, vp, vp]
         L.nvfp4_kv_attention.restype = c.c_int
         L.nvfp4_kv_attention.argtypes = [vp, i64, i64, i64, c.POINTER(_CKvCache), vp, i64, vp, vp, i64, i64, c.c_float, c.c_int, i64, i64,
                                          vp, i64, c.c_int, vp, vp, sz, vp]
@@ -514,7 +516,8 @@ def nvfp4_kv_cache_write(cache, k, v, slots, scale_search=False, stream=None):
 
 
 def nvfp4_kv_cache_read(cache, slots, k_out=None, v_out=None, stream=None):
-    """Slots (int64 [T]) back to bf16 [T, H, d].  Returns (k_out, v_out); with one of the two given, the other is not read (None)."""
+    """Slots (int64 [T]) back to bf16 [T, H, d].  Returns (k_out, v_out); with one of the two given, the other is not read (None).
+    Rows of slots outside the cache: zeros in new outputs, left as they were in given ones."""
     if stream is not None and _elsewhere(stream):
         return _on(stream, nvfp4_kv_cache_read, cache, slots, k_out, v_out)
     rc, k_out, v_out = _host().kv_cache_read(cache._native, slots, k_out, v_out, _stream(stream))
@@ -529,7 +532,9 @@ def nvfp4_kv_attention_workspace_bytes(total_q, Hq, H, d, max_kv, B, max_q, wind
 def nvfp4_kv_attention(q, cache, page_table, kv_lens, q_starts, max_q, softmax_scale=None, causal=False, window=0, sink=0, out_dtype=OUT_BF16,
                        out=None, lse=None, workspace=None, stream=None):
     """Attention of q (bf16 [total_q, Hq, d], contiguous heads, any token stride) over the cache: page_table int32 [B, max_pages],
-    kv_lens int32 [B], q_starts int32 [B + 1]; softmax_scale d ** -0.5 by default.  Returns (out [total_q, Hq, d], lse fp32 [total_q, Hq])."""
+    kv_lens int32 [B], q_starts int32 [B + 1]; softmax_scale d ** -0.5 by default.  Returns (out [total_q, Hq, d], lse fp32 [total_q, Hq]).
+    Rows that no sequence computes (before the first query, behind the last one, from max_q on): zeros and -inf in new outputs, left as
+    they were in given ones."""
     if stream is not None and _elsewhere(stream):
         return _on(stream, nvfp4_kv_attention, q, cache, page_table, kv_lens, q_starts, max_q, softmax_scale, causal, window, sink, out_dtype, out, lse, workspace)
     rc, out, lse = _host().kv_attention(q, cache._native, page_table, kv_lens, q_starts, max_q, cache.d ** -0.5 if softmax_scale is None else softmax_scale,

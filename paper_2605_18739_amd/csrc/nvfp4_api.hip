@@ -237,7 +237,7 @@ bool attention_sizes_ok(int64_t total_q, int64_t Hq, int64_t H, int64_t d, int64
 }
 bool attention_grid_ok(const AttentionPlan &p, int64_t Hq, int64_t H, int64_t B, int64_t max_q)
 {
-    const int64_t most = kMaxLanes / (64 * p.waves);                              // workgroups
+    const int64_t most = kMaxLanes / (64 * p.waves) - kClearGroups;               // workgroups
     if (p.rows16) return p.pieces + B + 8 <= most / p.groups && (p.pieces <= 1 || B * max_q * Hq <= kMaxLanes / 256);      // (a row's partial results: 256 lanes)
     return B * H <= kMaxIndex / p.groups && p.whole + (p.rest + 8) * p.pieces <= most;
 }
@@ -675,8 +675,8 @@ int nvfp4_kv_cache_write(const nvfp4_kv_cache *cache, const void *k_bf16, int64_
     return e == hipSuccess ? NVFP4_OK : NVFP4_ERR_LAUNCH;
 }
 
-int nvfp4_kv_cache_read(const nvfp4_kv_cache *cache, const int64_t *slots, int64_t T, void *k_bf16_out, void *v_bf16_out,
-                        void *stream)
+static int kv_cache_read(const nvfp4_kv_cache *cache, const int64_t *slots, int64_t T, void *k_bf16_out, void *v_bf16_out, bool clear,
+                         void *stream)
 {
     if ((!k_bf16_out && !v_bf16_out) || !slots) return NVFP4_ERR_NULL;
     KvPages c;
@@ -686,8 +686,20 @@ int nvfp4_kv_cache_read(const nvfp4_kv_cache *cache, const int64_t *slots, int64
     std::lock_guard<std::mutex> lk(g_mu);
     hipStream_t s = static_cast<hipStream_t>(stream);
     Timed t(s, NVFP4_OP_KV_CACHE_READ);
-    hipError_t e = launch_kv_cache_read(c, slots, T, static_cast<uint16_t *>(k_bf16_out), static_cast<uint16_t *>(v_bf16_out), s);
+    hipError_t e = launch_kv_cache_read(c, slots, T, static_cast<uint16_t *>(k_bf16_out), static_cast<uint16_t *>(v_bf16_out), clear, s);
     return e == hipSuccess ? NVFP4_OK : NVFP4_ERR_LAUNCH;
+}
+
+int nvfp4_kv_cache_read(const nvfp4_kv_cache *cache, const int64_t *slots, int64_t T, void *k_bf16_out, void *v_bf16_out,
+                        void *stream)
+{
+    return kv_cache_read(cache, slots, T, k_bf16_out, v_bf16_out, false, stream);
+}
+
+int nvfp4_kv_cache_read_new(const nvfp4_kv_cache *cache, const int64_t *slots, int64_t T, void *k_bf16_out, void *v_bf16_out,
+                            void *stream)
+{
+    return kv_cache_read(cache, slots, T, k_bf16_out, v_bf16_out, true, stream);
 }
 
 int nvfp4_kv_attention(const void *q_bf16, int64_t ldq, int64_t total_q, int64_t Hq, const nvfp4_kv_cache *cache,
@@ -707,6 +719,9 @@ int nvfp4_kv_attention(const void *q_bf16, int64_t ldq, int64_t total_q, int64_t
     if (!attention_sizes_ok(total_q, Hq, H, d, max_kv, B, max_q)) return NVFP4_ERR_SHAPE;
     if (!row_stride_ok(ldq, Hq, d) || !row_stride_ok(ldo, Hq, d) || window < 0 || sink < 0) return NVFP4_ERR_SHAPE;
     if (!(softmax_scale > 0.0f) || !std::isfinite(softmax_scale * 1.4426950408889634f)) return NVFP4_ERR_SHAPE;      // (exponents of two are what it makes)
+    a.clear_out = (out_dtype & NVFP4_OUT_NEW) != 0;
+    a.clear_lse = (out_dtype & NVFP4_LSE_NEW) != 0 && lse;
+    out_dtype &= ~(NVFP4_OUT_NEW | NVFP4_LSE_NEW);
     if (out_dtype != NVFP4_OUT_F32 && out_dtype != NVFP4_OUT_BF16) return NVFP4_ERR_SHAPE;
     if (!aligned16(q_bf16) || !aligned16(out) || (ldq & 7) != 0 || (ldo & (out_dtype == NVFP4_OUT_BF16 ? 7 : 3)) != 0 ||
         !aligned(page_table, 4) || !aligned(kv_lens, 4) || !aligned(q_starts, 4) || !aligned(lse, 4))

@@ -24,6 +24,8 @@ struct AttentionArgs {
     Divisor by_page;
     uint32_t token_codes, token_scales;   // bytes of a slot: codes, scales
     uint32_t page_scales, page_means;     // bytes of a page: scales, means
+    uint32_t clear_from;                  // number of the first workgroup that clears rows, 0xFFFFFFFF: none
+    int32_t clear_out, clear_lse, out_row;        // what it clears; 16-byte pieces of a row of `out`
 };
 
 // Sixteen cached tokens of a page: where their slots begin in each plane, as scalar bases for a lane's 32-bit offset.  (Two
@@ -295,8 +297,41 @@ __device__ __forceinline__ float sum8(uint4v w, int e, float s)
     return s;
 }
 
-hipError_t launch_attention_rows16(const AttentionArgs &a, const KvAttention &k, hipStream_t s);
-hipError_t launch_attention_tiles(const AttentionArgs &a, const KvAttention &k, hipStream_t s);
+// Rows that no sequence computes, in outputs that hold nothing yet: in front of the first query and behind the last one, and
+// from max_q on.  Workgroups behind those of a kernel's own work (a.clear_from on) set them to zero and -inf.
+__device__ __forceinline__ void clear_rows(const AttentionArgs &a, int64_t from, int64_t to, int64_t by, int out_bytes)
+{
+    for (int64_t row = from; row < to; row += by) {
+        uint4v *const out = (uint4v *)((uint8_t *)a.out + row * a.ldo * out_bytes);
+        for (int i = threadIdx.x; a.clear_out && i < a.out_row; i += blockDim.x) out[i] = uint4v{0u, 0u, 0u, 0u};
+        for (int i = threadIdx.x; a.clear_lse && i < a.Hq; i += blockDim.x) a.lse[row * a.Hq + i] = -__builtin_inff();
+    }
+}
+template <bool F32>
+__device__ __forceinline__ void clear_rest(const AttentionArgs &a, const int32_t *__restrict__ q_starts)
+{
+    constexpr int bytes = F32 ? 4 : 2;
+    const int part = (int)(blockIdx.x - a.clear_from), parts = (int)(gridDim.x - a.clear_from);
+    const int first = min(max(q_starts[0], 0), a.total_q), last = min(max(q_starts[a.B], first), a.total_q);
+    clear_rows(a, part, first, parts, bytes);
+    clear_rows(a, last + part, a.total_q, parts, bytes);
+    for (int b = part; b < a.B; b += parts) {
+        const int start = min(max(q_starts[b], 0), a.total_q), end = min(max(q_starts[b + 1], start), a.total_q);
+        clear_rows(a, (int64_t)start + a.max_q, end, 1, bytes);
+    }
+}
+// a grid of `own` workgroups and those that clear
+inline unsigned attention_grid(AttentionArgs &a, const KvAttention &k, unsigned own)
+{
+    a.clear_out = k.clear_out;
+    a.clear_lse = k.clear_lse;
+    a.out_row = (int32_t)(k.Hq * k.cache.d * (k.out_f32 ? 4 : 2) / 16);
+    a.clear_from = k.clear_out || k.clear_lse ? own : 0xFFFFFFFFu;
+    return own + (a.clear_from == own ? (unsigned)std::min<int64_t>(std::max<int64_t>(k.total_q / 64, 8), kClearGroups) : 0u);
+}
+
+hipError_t launch_attention_rows16(AttentionArgs a, const KvAttention &k, hipStream_t s);
+hipError_t launch_attention_tiles(AttentionArgs a, const KvAttention &k, hipStream_t s);
 hipError_t launch_attention_join(const AttentionArgs &a, const KvAttention &k, hipStream_t s);
 
 }  // namespace nvfp4

@@ -18,6 +18,7 @@ constexpr int kRows16Heads = 4, kRows16Slots = 512, kRows16MinSteps = 2;
 // and the gap between the launches, whole 13.5; 512 tokens 7.4 + 5.6, 18.4), twice as many where the sequences fill a quarter
 // of the chip by themselves (64 caches of 512 tokens of 8 heads: 16.9 + 8.2 us, whole 19.9).
 constexpr int kRows16Whole = 10;
+constexpr int kClearGroups = 256;                      // workgroups of a call that clear rows which no sequence computes, at most
 constexpr int kTileMinSteps = 8;                       // steps of a piece of the other kernel, at least
 
 struct AttentionPlan {

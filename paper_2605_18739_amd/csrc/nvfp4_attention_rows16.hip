@@ -46,6 +46,7 @@ __global__ __launch_bounds__(64 * kRows16Heads, D == 256 ? 1 : 2) void attention
                                                                const int32_t *__restrict__ kv_lens, const int32_t *__restrict__ q_starts,
                                                                const float *__restrict__ k_global, const float *__restrict__ v_global)
 {
+    if (blockIdx.x >= a.clear_from) return clear_rest<F32>(a, q_starts);
     constexpr int KD = D / 4, NT = D / 16;                 // elements of a lane's key part; column tiles of the values
     const int lane = threadIdx.x & 63, r = lane & 15, g = lane >> 4;
     const int d = FULL ? D : a.d;
@@ -475,10 +476,10 @@ __global__ __launch_bounds__(64 * kRows16Heads, D == 256 ? 1 : 2) void attention
 }
 
 template <int D>
-static void launch_rows16(const AttentionArgs &a, const KvAttention &k, hipStream_t s)
+static void launch_rows16(AttentionArgs a, const KvAttention &k, hipStream_t s)
 {
     const int64_t pieces = a.plan.pieces > 1 ? a.plan.pieces + a.B : a.B;
-    const dim3 grid((unsigned)(((pieces + 7) >> 3 << 3) * a.plan.groups)), block((unsigned)(64 * a.plan.waves));
+    const dim3 grid(attention_grid(a, k, (unsigned)(((pieces + 7) >> 3 << 3) * a.plan.groups))), block((unsigned)(64 * a.plan.waves));
     auto go = [&](auto kernel) { kernel<<<grid, block, 0, s>>>(a, k.page_table, k.kv_lens, k.q_starts, k.cache.k_global, k.cache.v_global); };
     auto smooth = [&](auto full) {
         constexpr bool FULL = decltype(full)::value;
@@ -489,7 +490,7 @@ static void launch_rows16(const AttentionArgs &a, const KvAttention &k, hipStrea
     else smooth(std::false_type());
 }
 
-hipError_t launch_attention_rows16(const AttentionArgs &a, const KvAttention &k, hipStream_t s)
+hipError_t launch_attention_rows16(AttentionArgs a, const KvAttention &k, hipStream_t s)
 {
     if (a.d <= 64) launch_rows16<64>(a, k, s);
     else if (a.d <= 128) launch_rows16<128>(a, k, s);

@@ -65,6 +65,7 @@ __global__ __launch_bounds__(64 * WAVES, D == 256 ? 1 : 2) void attention_tiles_
                                                                           const int32_t *__restrict__ kv_lens, const int32_t *__restrict__ q_starts,
                                                                           const float *__restrict__ k_global, const float *__restrict__ v_global)
 {
+    if (blockIdx.x >= a.clear_from) return clear_rest<F32>(a, q_starts);
     using Lds = Tiles<D, WAVES>;
     extern __shared__ __align__(16) uint8_t lds_bytes[];
     Lds &lds = *reinterpret_cast<Lds *>(lds_bytes);
@@ -475,7 +476,7 @@ __global__ __launch_bounds__(64 * WAVES, D == 256 ? 1 : 2) void attention_tiles_
 }
 
 template <int D, int WAVES, bool SMOOTH, bool F32>
-static hipError_t launch_variant(const AttentionArgs &a, const KvAttention &k, hipStream_t s)
+static hipError_t launch_variant(AttentionArgs a, const KvAttention &k, hipStream_t s)
 {
     auto kernel = attention_tiles_kernel<D, WAVES, SMOOTH, F32>;
     constexpr int bytes = (int)sizeof(Tiles<D, WAVES>);
@@ -487,7 +488,7 @@ static hipError_t launch_variant(const AttentionArgs &a, const KvAttention &k, h
         if (hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void *>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, bytes)) return e;
         raised[dev] = true;
     }
-    const unsigned grid = (unsigned)(a.plan.whole + ((a.plan.rest + 7) & ~(int64_t)7) * a.plan.pieces);
+    const unsigned grid = attention_grid(a, k, (unsigned)(a.plan.whole + ((a.plan.rest + 7) & ~(int64_t)7) * a.plan.pieces));
     kernel<<<grid, 64 * WAVES, bytes, s>>>(a, k.page_table, k.kv_lens, k.q_starts, k.cache.k_global, k.cache.v_global);
     return hipGetLastError();
 }
@@ -498,7 +499,7 @@ static hipError_t launch_tiles(const AttentionArgs &a, const KvAttention &k, hip
     return k.out_f32 ? launch_variant<D, WAVES, false, true>(a, k, s) : launch_variant<D, WAVES, false, false>(a, k, s);
 }
 
-hipError_t launch_attention_tiles(const AttentionArgs &a, const KvAttention &k, hipStream_t s)
+hipError_t launch_attention_tiles(AttentionArgs a, const KvAttention &k, hipStream_t s)
 {
     if (a.d > 128) return launch_tiles<256, 4>(a, k, s);
     if (a.d <= 64) return launch_tiles<64, 4>(a, k, s);

@@ -368,7 +368,8 @@ const at::Tensor &workspace_of(const OnDevice &on, PyObject *o)
     require(x.is_contiguous(), "expected a contiguous workspace");               // (an expanded one has fewer bytes than it says)
     return x;
 }
-// An output: the caller's tensor, or a new one (an allocation here costs 0.7 us, one through torch.empty 2.3), handed back with the status
+// An output: the caller's tensor, or a new one (an allocation here costs 0.7 us, one through torch.empty 2.3), handed back with the status.
+// A new one holds nothing: calls that leave rows out are told so, and set them to zero.
 struct Output {
     PyObject *given = Py_None;
     at::Tensor t;
@@ -377,9 +378,10 @@ struct Output {
     {
         t = o == Py_None ? at::empty(sizes, at::TensorOptions().device(on.device).dtype(type)) : on(tensor(o));
     }
+    bool fresh() const { return given == Py_None && t.defined(); }
     PyObject *handed_back() const
     {
-        if (given == Py_None && t.defined()) return THPVariable_Wrap(t);
+        if (fresh()) return THPVariable_Wrap(t);
         Py_INCREF(given);
         return given;
     }
@@ -575,7 +577,8 @@ PyObject *kv_cache_read(PyObject *const *a)                         // cache, sl
         p[i] = x.data_ptr();
     }
     void *s = stream_of(a[4]);
-    return status_and({&out[0], &out[1]}, [&] { return nvfp4_kv_cache_read(&pages.c, static_cast<const int64_t *>(slots.data_ptr()), slots.size(0), p[0], p[1], s); });
+    const auto read = out[0].fresh() || out[1].fresh() ? nvfp4_kv_cache_read_new : nvfp4_kv_cache_read;         // (both are new, or none)
+    return status_and({&out[0], &out[1]}, [&] { return read(&pages.c, static_cast<const int64_t *>(slots.data_ptr()), slots.size(0), p[0], p[1], s); });
 }
 // q, cache, page_table, kv_lens, q_starts, max_q, softmax_scale, causal, window, sink, out_dtype, out, lse, workspace, stream
 PyObject *kv_attention(PyObject *const *a)
@@ -598,6 +601,7 @@ PyObject *kv_attention(PyObject *const *a)
             "expected an output of the queries' shape and the chosen type with contiguous [H, d]");
     require(l.scalar_type() == at::kFloat && l.dim() == 2 && l.is_contiguous() && l.size(0) == total_q && l.size(1) == Hq, "expected a contiguous fp32 lse [total_q, H]");
     float *const lse = static_cast<float *>(l.data_ptr());
+    const int fresh = (o.fresh() ? NVFP4_OUT_NEW : 0) | (log_sum.fresh() ? NVFP4_LSE_NEW : 0);
     at::Tensor ws;
     if (a[13] != Py_None) ws = workspace_of(on, a[13]);
     else if (const size_t n = nvfp4_kv_attention_workspace_bytes(total_q, Hq, c.H, c.d, table.size(1) * c.page_tokens, B, max_q, window, sink)) ws = bytes_on(on.device, (int64_t)n);
@@ -605,7 +609,7 @@ PyObject *kv_attention(PyObject *const *a)
     const size_t n = ws.defined() ? (size_t)ws.nbytes() : 0;
     const int32_t *pt = static_cast<const int32_t *>(table.data_ptr()), *pl = static_cast<const int32_t *>(lens.data_ptr()), *ps = static_cast<const int32_t *>(starts.data_ptr());
     return status_and({&o, &log_sum}, [&] {
-        return nvfp4_kv_attention(pq, token_stride(q), total_q, Hq, &c, pt, table.size(1), pl, ps, B, max_q, scale, causal, window, sink, po, token_stride(out), dtype, lse, w, n, s);
+        return nvfp4_kv_attention(pq, token_stride(q), total_q, Hq, &c, pt, table.size(1), pl, ps, B, max_q, scale, causal, window, sink, po, token_stride(out), dtype | fresh, lse, w, n, s);
     });
 }
 

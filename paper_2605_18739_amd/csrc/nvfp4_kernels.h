@@ -108,7 +108,8 @@ struct KvPages {
 };
 hipError_t launch_kv_cache_write(const KvPages &c, const uint16_t *k, int64_t ldk, const uint16_t *v, int64_t ldv, const int64_t *slots,
                                  int64_t T, bool scale_search, hipStream_t s);
-hipError_t launch_kv_cache_read(const KvPages &c, const int64_t *slots, int64_t T, uint16_t *k_out, uint16_t *v_out, hipStream_t s);
+// clear: rows of slots outside the cache become zeros
+hipError_t launch_kv_cache_read(const KvPages &c, const int64_t *slots, int64_t T, uint16_t *k_out, uint16_t *v_out, bool clear, hipStream_t s);
 
 // Attention over the paged cache (sizes below 2^31, checked by the caller)
 struct KvAttention {
@@ -122,7 +123,7 @@ struct KvAttention {
     int64_t window, sink;
     void *out;
     int64_t ldo;
-    bool out_f32;
+    bool out_f32, clear_out, clear_lse;               // clear: rows that no sequence computes
     float *lse;
 };
 hipError_t launch_kv_attention(const KvAttention &k, void *workspace, hipStream_t s);

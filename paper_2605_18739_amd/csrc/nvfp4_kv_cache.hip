@@ -21,17 +21,17 @@ struct CacheUnits {
 struct CacheUnit {
     int64_t t, slot, page;
     int part;
-    bool is_v, live;
+    bool is_v, there, live;                  // there: a unit; live: its slot is one of the cache
     __device__ __forceinline__ CacheUnit(const CacheUnits &n, const KvPages &c, const int64_t *__restrict__ slots)
     {
         const int64_t u = (int64_t)__builtin_amdgcn_readfirstlane((int)(blockIdx.x * kCacheWaves + threadIdx.x / kWave));
-        live = u < n.units;
-        const int64_t v = divide(live ? u : 0, n.parts, n.by_parts);
-        part = (int)((live ? u : 0) - v * n.parts);
+        there = u < n.units;
+        const int64_t v = divide(there ? u : 0, n.parts, n.by_parts);
+        part = (int)((there ? u : 0) - v * n.parts);
         t = divide(v, n.tensors, n.by_tensors);
         is_v = (int)(v - t * n.tensors) + n.first != 0;
         slot = slots[t];
-        live &= slot >= 0 && slot < c.n_pages * c.page_tokens;
+        live = there && slot >= 0 && slot < c.n_pages * c.page_tokens;
         page = live ? divide(slot, c.page_tokens, n.by_page) : 0;
     }
 };
@@ -73,12 +73,18 @@ __global__ __launch_bounds__(kCacheThreads) void kv_cache_write_kernel(const KvP
 // A lane per half block (eight codes in, sixteen bytes out), kReadUnroll of them in flight.
 constexpr int kReadUnroll = 4;
 __global__ __launch_bounds__(kCacheThreads) void kv_cache_read_kernel(const KvPages c, const CacheUnits n, const int64_t *__restrict__ slots,
-                                                                      uint16_t *__restrict__ k_out, uint16_t *__restrict__ v_out)
+                                                                      uint16_t *__restrict__ k_out, uint16_t *__restrict__ v_out, int clear)
 {
     const int lane = threadIdx.x & (kWave - 1);
     const CacheUnit u(n, c, slots);
-    if (!u.live) return;
     const int nb_row = c.d >> 4, nh = c.H * (c.d >> 3);             // half blocks of the row
+    if (!u.live) {                                                  // (the whole wave)
+        if (!u.there || !clear) return;
+        uint16_t *const out = (u.is_v ? v_out : k_out) + u.t * (int64_t)(nh << 3);
+        const int h0 = u.part * (kWave * kReadUnroll) + lane;
+        for (int h = h0; h < min(nh, h0 + kWave * kReadUnroll); h += kWave) *(uint4v *)(out + (h << 3)) = uint4v{0u, 0u, 0u, 0u};
+        return;
+    }
     const int64_t at = u.slot * (int64_t)nh;
     const uint32_t *codes = (const uint32_t *)(u.is_v ? c.v_codes : c.k_codes) + at;
     const uint8_t *scales = (u.is_v ? c.v_scales : c.k_scales) + (at >> 1);
@@ -133,11 +139,11 @@ hipError_t launch_kv_cache_write(const KvPages &c, const uint16_t *k, int64_t ld
     return hipGetLastError();
 }
 
-hipError_t launch_kv_cache_read(const KvPages &c, const int64_t *slots, int64_t T, uint16_t *k_out, uint16_t *v_out, hipStream_t s)
+hipError_t launch_kv_cache_read(const KvPages &c, const int64_t *slots, int64_t T, uint16_t *k_out, uint16_t *v_out, bool clear, hipStream_t s)
 {
     constexpr int per = kWave * kReadUnroll;
     const CacheUnits n = cache_units(c, T, k_out, v_out, (c.H * (c.d >> 3) + per - 1) / per);
-    kv_cache_read_kernel<<<(unsigned)((n.units + kCacheWaves - 1) / kCacheWaves), kCacheThreads, 0, s>>>(c, n, slots, k_out, v_out);
+    kv_cache_read_kernel<<<(unsigned)((n.units + kCacheWaves - 1) / kCacheWaves), kCacheThreads, 0, s>>>(c, n, slots, k_out, v_out, clear);
     return hipGetLastError();
 }
 

@@ -218,3 +218,13 @@ def test_attention_refuses_a_scale_that_leaves_the_range_as_a_power_of_two():
     for scale in (2.4e38, 3.4e38):
         assert attention(scale=scale) == SHAPE, scale
     assert attention(scale=2.3e38, q=P + 2) == ALIGN and attention(scale=1e-40, q=P + 2) == ALIGN
+
+
+def test_flags_of_new_outputs_are_checked_like_the_calls_without():
+    for flags in (0x100, 0x200, 0x300):
+        assert attention(dtype=1 | flags, q=P + 2) == ALIGN and attention(dtype=flags, ldo=1026) == ALIGN and attention(dtype=2 | flags) == SHAPE
+    assert attention(dtype=0x401) == SHAPE
+    new = lambda c, slots=P, T=3, k=P, v=P: nv.lib().nvfp4_kv_cache_read_new(ref(c), slots, T, k, v, None)
+    for fields, status in BAD_CACHES:
+        assert new(cache(**fields)) == status, fields
+    assert new(cache(), k=None, v=None) == NULL and new(cache(), T=0) == SHAPE and new(cache(), k=P + 2) == ALIGN

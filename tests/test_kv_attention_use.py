@@ -423,3 +423,59 @@ def test_elements_that_are_not_turned_stay_as_they_are(interleaved, pairs):
         y, turned = run(x), run(clean)
         assert torch.equal(bits(y[..., 2 * pairs:]), bits(x[..., 2 * pairs:]))
         assert torch.equal(bits(y[..., :2 * pairs]), bits(turned[..., :2 * pairs]))
+
+# ---------------------------------------------------------------------------------------------------------------------
+# outputs that the calls allocate
+# ---------------------------------------------------------------------------------------------------------------------
+def leave_garbage(*sizes):
+    """Freed blocks of these sizes, full of 0xFF: what a new output finds."""
+    blocks = [torch.full((n,), 255, dtype=torch.uint8, device="cuda") for n in sizes for _ in range(4)]
+    torch.cuda.synchronize()
+    del blocks
+
+
+@pytest.mark.parametrize("d,H", [(64, 3), (80, 24), (256, 1)])
+def test_new_outputs_of_a_read_hold_zeros_for_slots_outside_the_cache(d, H):
+    say("[use] new outputs of a read", d, H)
+    c = nv.NVFP4KvCache.empty(3, 32, H, d)
+    fill_cache(c, gen(52))
+    slots = torch.randperm(96, generator=gen(53))[:70]
+    slots[[0, 5, 33, 69]] = torch.tensor([-1, 96, -(1 << 40), 1 << 40])
+    outside = (slots < 0) | (slots >= 96)
+    given = [torch.full((70, H, d), 5.0, dtype=BF, device="cuda") for _ in range(2)]
+    nv.nvfp4_kv_cache_read(c, slots.cuda(), *given)
+    for stream in (None, torch.cuda.Stream()):
+        leave_garbage(70 * H * d * 2)
+        got = nv.nvfp4_kv_cache_read(c, slots.cuda(), stream=stream)
+        torch.cuda.synchronize()
+        for x, y in zip(got, given):
+            assert same(x[~outside.cuda()], y[~outside.cuda()])
+            assert (x[outside.cuda()] == 0).all() and (y[outside.cuda()] == 5.0).all()
+
+
+@pytest.mark.parametrize("queries", [1, 3, 40])
+@pytest.mark.parametrize("out_f32", [False, True])
+@pytest.mark.parametrize("long", [False, True])
+def test_new_outputs_of_attention_hold_zeros_where_no_sequence_computes(queries, out_f32, long):
+    """Rows in front of the first sequence and behind the last one, and queries from max_q on: zeros and -inf."""
+    say("[use] new outputs of attention", queries, out_f32, long)
+    lens, n = [4000 if long else 100, 30, 0], [queries + 2, queries, queries]
+    c, table, starts, q = attention_case(54, lens, n, 4, 2, 64, 16, False)
+    table = table.cuda()
+    q = torch.cat([q[:3], q, q[:150]]).cuda()                       # rows before and behind
+    starts = [3 + s for s in starts]
+    computed = torch.zeros(q.shape[0], dtype=torch.bool)
+    for b in range(3):
+        computed[starts[b]:starts[b] + min(n[b], queries)] = True
+    kind = nv.OUT_F32 if out_f32 else nv.OUT_BF16
+    given = torch.full(q.shape, 3.0, dtype=F32 if out_f32 else BF, device="cuda"), torch.full(q.shape[:2], 4.0, device="cuda")
+    call = lambda **kw: nv.nvfp4_kv_attention(q, c, table, ints(lens), ints(starts), queries, causal=True, out_dtype=kind, **kw)
+    call(out=given[0], lse=given[1])
+    assert (given[0][~computed.cuda()] == 3.0).all() and (given[1][~computed.cuda()] == 4.0).all()
+    leave_garbage(given[0].nbytes, given[1].nbytes)
+    fresh = call()
+    torch.cuda.synchronize()
+    half = call(out=torch.full_like(given[0], 3.0)), call(lse=torch.full_like(given[1], 4.0))
+    for out, lse, rest_o, rest_l in ((*fresh, 0.0, -math.inf), (*half[0], 3.0, -math.inf), (*half[1], 0.0, 4.0)):
+        assert same(out[computed.cuda()], given[0][computed.cuda()]) and same(lse[computed.cuda()], given[1][computed.cuda()])
+        assert (out[~computed.cuda()] == rest_o).all() and (lse[~computed.cuda()] == rest_l).all()
