@@ -14,10 +14,15 @@ constexpr int kRows16Step = 32, kTileStep = 64;       // cached tokens of a step
 // Steps of a piece: a step of a wave that has its SIMD alone takes 0.8 us, a partial result more next to nothing (five caches of up
 // to 704 tokens, d = 64: pieces of four steps 9.0 + 5.2 us, of two 7.2 + 5.5).
 constexpr int kRows16Heads = 4, kRows16Slots = 512, kRows16MinSteps = 2;
-// Steps up to which a sequence is not cut: the second launch costs about 6 us (one cache, d = 128: 320 tokens in pieces 7.4 + 5.6 us
-// and the gap between the launches, whole 13.5; 512 tokens 7.4 + 5.6, 18.4), twice as many where the sequences fill a quarter
-// of the chip by themselves (64 caches of 512 tokens of 8 heads: 16.9 + 8.2 us, whole 19.9).
-constexpr int kRows16Whole = 10;
+// Steps up to which a sequence is not cut (a second launch joins pieces).  Few sequences, us a call among others, whole / in pieces:
+//   d = 64 (24 heads, one cache)   192 tokens 9.0 / 11.5, 256 10.3 / 11.8, 320 11.7 / 11.8
+//   d = 128 (8 heads, one cache)   192 tokens 9.7 / 12.0, 256 11.3 / 11.6, 320 13.0 / 11.7; 16 caches 256 11.8 / 12.3, 320 13.6 / 12.2
+//   d = 256 (8 heads, one cache)   128 tokens 12.8 / 15.1, 192 15.7 / 15.0, 256 18.8 / 15.0; 16 caches 128 13.4 / 15.3, 256 19.6 / 15.8
+// Where the sequences are a quarter of the workgroups that the chip holds, or more, they fill it uncut (in a graph, 512 and 640 tokens):
+//   d = 64, 32 x 24 heads  17.5 / 23.1, 20.7 / 26.9;  128 x 24  37.9 / 44.1, 45.0 / 51.2
+//   d = 128, 64 x 8 heads  20.1 / 23.0, 24.0 / 24.8;  128 x 2   19.8 / 21.0, 23.6 / 22.6;  with fewer, 32 x 8  19.2 / 16.8, 22.7 / 17.2
+//   d = 256, 64 x 8 heads  33.4 / 37.0, 39.2 / 43.0
+constexpr int kRows16Whole = 8, kRows16WholeWide = 4, kRows16WholeMany = 20;         // (wide: above d = 128)
 constexpr int kClearGroups = 256;                      // workgroups of a call that clear rows which no sequence computes, at most
 constexpr int kTileMinSteps = 8;                       // steps of a piece of the other kernel, at least
 
@@ -50,9 +55,10 @@ inline AttentionPlan attention_plan(int64_t total_q, int64_t Hq, int64_t H, int6
         // sequences are cut to a common length, so every one of them may add a shorter piece to those of full length
         const int64_t most = B * ((steps + kRows16MinSteps - 1) / kRows16MinSteps);
         p.pieces = (int)std::min(std::max<int64_t>((d > 128 ? kRows16Slots / 2 : kRows16Slots) / p.groups - B, std::min<int64_t>(B, 64)), most);
-        if (steps <= (B * p.groups >= kRows16Slots / 4 ? 2 : 1) * kRows16Whole) p.pieces = 1;
+        if (steps <= (B * p.groups >= kRows16Slots / 4 ? kRows16WholeMany : d > 128 ? kRows16WholeWide : kRows16Whole)) p.pieces = 1;
         p.part_rows = p.pieces <= 1 ? 0 : (p.pieces + B) * max_q * Hq;
     } else {
+        // (eight waves: up to d = 64 a step has fewer pieces of keys than lanes, above d = 128 the accumulators leave room for four)
         p.waves = d > 64 && d <= 128 && rows > 128 ? 8 : 4;
         p.groups = (int)((rows + 32 * p.waves - 1) / (32 * p.waves));
         const int64_t steps = std::max<int64_t>(1, (max_kv + kTileStep - 1) / kTileStep);

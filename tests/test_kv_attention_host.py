@@ -228,3 +228,12 @@ def test_flags_of_new_outputs_are_checked_like_the_calls_without():
     for fields, status in BAD_CACHES:
         assert new(cache(**fields)) == status, fields
     assert new(cache(), k=None, v=None) == NULL and new(cache(), T=0) == SHAPE and new(cache(), k=P + 2) == ALIGN
+
+
+def test_short_caches_are_not_cut():
+    """Up to 256 tokens (128 above d = 128) in one launch, 640 where the sequences are many."""
+    ws = nv.nvfp4_kv_attention_workspace_bytes
+    for d, tokens in ((64, 256), (128, 256), (144, 128), (256, 128)):
+        for B in (1, 16):
+            assert ws(B, 32, 8, d, tokens, B, 1) == 0 < ws(B, 32, 8, d, tokens + 32, B, 1), (d, B)
+        assert ws(64, 32, 8, d, 640, 64, 1) == 0 < ws(64, 32, 8, d, 672, 64, 1), d
