@@ -455,7 +455,8 @@ int nvfp4_kv_cache_read_new(const nvfp4_kv_cache *cache, const int64_t *slots, i
  * Scores, their maxima and sums and the accumulation are fp32.  The probabilities enter the second product as f16 (fp32 output: as
  * the sum of two f16 numbers): within 2^-11 (2^-22) of each, and no closer than 2^-30 of the row's largest, whatever the pages'
  * scales are; their sum is that of the unrounded ones.  Pages whose value scale is below 2^-64 of another one's of the same
- * sequence, or below 2^-100, lose digits of their values.
+ * sequence, or below 2^-84, lose digits of their values; the weights of those count in the sum.  Scales are below 2^126 (those
+ * that the quantizers choose are below 2^117).
  * Refused (NVFP4_ERR_SHAPE) besides the above: a softmax_scale that is not positive, or not finite times log2(e), more than 2^30
  * pages, pages whose block scales or row means fill 4 GiB, and more rows or sequences than one launch covers (2^32 lanes).
  * workspace: nvfp4_kv_attention_workspace_bytes() bytes, 16-byte aligned (0 bytes: may be NULL): partial results where the

@@ -184,11 +184,11 @@ struct Sight {
 // Weights stay below 2^(kAbove + 1 + kUnitHigh) = 2^15.  What f16 cannot hold is 2^-25, and so 2^-30 of the largest 2^s (kBelow
 // and kUnitLow) whatever the pages' scales are; with the maximum itself for m a long tail behind a token with nearly all of the
 // sum was lost from the product while the sum kept it.
-// The unit does not go below 2^-100, nor further than kUnitReach below the largest that it has been: no rescaling overflows (2^15 *
-// 2688 * 2^30 tokens are 2^57), and neither does a sum of weights / g.  Pages that it does not reach lose digits, and from kUnitLost
-// below it on their weights count in the sum alone.
+// The unit does not go below 2^-84, nor further than kUnitReach below the largest that it has been: no rescaling overflows (2^15 *
+// 2688 * 2^30 tokens are 2^57), and neither does a sum of weights / g (2^(kAbove + 30 + 84)).  Pages that it does not reach lose
+// digits, and from kUnitLost below it on their weights count in the sum alone.
 constexpr float kBelow = 7.0f, kAbove = 13.0f, kLowest = -3.0e38f;      // (kLowest: below every score, and 2^(-inf - kLowest) is still 0)
-constexpr int kUnitLow = -2, kUnitHigh = 1, kUnitReach = 64, kUnitLost = 40, kUnitBias = 127, kUnitLeast = 27;       // (exponent fields as in fp32)
+constexpr int kUnitLow = -2, kUnitHigh = 1, kUnitReach = 64, kUnitLost = 40, kUnitBias = 127, kUnitLeast = 43;       // (exponent fields as in fp32)
 constexpr int kNoUnit = -512;
 struct Units {
     int now, top;                         // U as an fp32 exponent field (at first kNoUnit), and the largest it has been
@@ -247,6 +247,9 @@ __device__ __forceinline__ bool group_seen(int first, int p0, int p1, int window
 {
     return (first <= p1) & ((window <= 0) | (first + 15 > p0 - window) | (first < sink));
 }
+
+// A sum of weights relative to 2^from, relative to 2^to (both whole numbers: units may be further apart than a factor's range).
+__device__ __forceinline__ float moved_sum(float l, float from, float to) { return __builtin_amdgcn_ldexpf(l, (int)fmaxf(from - to, -1024.0f)); }
 
 // Of a row's sum of weights l relative to 2^r: what its products are multiplied by, and its log-sum-exp.  Nothing seen: zero and
 // -inf; a sum that is no number (scores that are none) stays one.

@@ -61,7 +61,7 @@ __global__ __launch_bounds__(kJoinThreads) void attention_join_kernel(const Atte
     float l = 0.0f;
     for (int s = lane; s < pieces; s += 64) {
         const float2 v = part_ml[first + s * stride];
-        l = __builtin_fmaf(v.y, __builtin_amdgcn_exp2f(v.x - m), l);
+        l += moved_sum(v.y, v.x, m);
     }
 #pragma unroll
     for (int x = 32; x > 0; x >>= 1) l += __shfl_xor(l, x, 64);

@@ -354,8 +354,8 @@ __global__ __launch_bounds__(64 * kRows16Heads, D == 256 ? 1 : 2) void attention
             t = fmaxf(t, __shfl_xor(t, 32, 64));
             m = fmaxf(floorf(t - kBelow), m);
             const float to = m + (float)(units.now - kUnitBias), f = __builtin_amdgcn_exp2f(ref - to);
+            l = moved_sum(l, ref, to);
             ref = to;
-            l *= f;
 #pragma unroll
             for (int j = 0; j < NT; ++j) o[j] *= f;
         }

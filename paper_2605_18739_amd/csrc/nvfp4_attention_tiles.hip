@@ -372,8 +372,8 @@ __global__ __launch_bounds__(64 * WAVES, D == 256 ? 1 : 2) void attention_tiles_
         if (__ballot(top > m + kAbove) != 0ull || moved) {
             m = fmaxf(floorf(fmaxf(top, __shfl_xor(top, 32, 64)) - kBelow), m);
             const float to = m + (float)(lds.rare.unit[tid >> 6] - kUnitBias), f = __builtin_amdgcn_exp2f(r - to);
+            l = moved_sum(l, r, to);
             r = to;
-            l *= f;
 #pragma unroll
             for (int t = 0; t < VF; ++t) o[t] *= f;
         }

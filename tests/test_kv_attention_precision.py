@@ -145,7 +145,7 @@ def test_page_scales_of_all_magnitudes_in_pieces(queries, d):
 def test_scales_at_the_ends_of_the_range(queries):
     """Results near the largest and the smallest numbers, whole and joined from pieces."""
     say("[precision] ends", queries)
-    for exponent in (104, -100):
+    for exponent in (104, -84):
         for n in (150, 6000):
             c, table, starts, q = attention_case(66, [n], [queries], 2, 1, 64, 16, False)
             c.v_global.copy_(2.0 ** exponent * (0.5 + torch.rand(c.n_pages, generator=gen(67))))
@@ -171,3 +171,37 @@ def test_the_largest_queries(queries, smooth):
     n = starts[-1]
     if not smooth:                                                  # (the same digits; means and their quotients may round apart)
         assert torch.equal(got[0][:n], want[0][:n])
+
+
+@pytest.mark.parametrize("n", [40, 900, 6000])
+@pytest.mark.parametrize("queries,d", [(1, 64), (1, 128), (5, 256), (40, 64), (200, 128), (40, 256)])
+def test_the_sum_counts_pages_of_every_scale(queries, d, n):
+    """Value scales over the whole range of normal numbers (below 2^126), page by page: each token is in the sum with its weight.  The scores are
+    zero, so the sum is the number of tokens: 8 u for a token's weight (its exponent, of up to 2^8, within u 2^8: 2^8 u), (n + 8) u for the sum."""
+    say("[precision] sums", queries, d, n)
+    g = gen(71)
+    for low, high in ((-126, 125), (-126, -90), (100, 125)):
+        c = bare_cache(-(-n // 16), 16, 1, d)
+        c.v_scales.zero_()
+        scales = (1 + torch.rand(c.n_pages, generator=g, dtype=torch.float64)) * 2.0 ** torch.randint(low, high + 1, (c.n_pages,), generator=g).double()
+        c.v_global.copy_(scales.to(F32))
+        table = torch.arange(c.n_pages, dtype=torch.int32).view(1, -1)
+        out, lse = run_attention(c, table, [n], [0, queries], torch.ones((queries, 2, d), dtype=BF), queries, False, out_f32=True, check=False)
+        assert (out == 0).all()
+        assert float((lse.double() - math.log(n)).abs().max()) <= (2 ** 8 + n + 16) * U + 4 * U * math.log(n), (low, high)
+
+
+def test_the_sum_of_millions_of_tokens_on_pages_of_the_least_scales():
+    """2^22 tokens with equal weights: lanes add up to 2^16 of them, (2^16 + 2^8 + 16) u."""
+    n = 1 << 22
+    c = bare_cache(n // 4096, 4096, 1, 16)
+    c.v_codes.fill_(0x22)
+    c.v_scales.fill_(0x38)
+    table = torch.arange(c.n_pages, dtype=torch.int32).view(1, -1)
+    for exponent in (-126, -100, -90, 0, 110):
+        say("[precision] millions", exponent)
+        c.v_global.fill_(2.0 ** exponent)
+        out, lse = run_attention(c, table, [n], [0, 1], torch.ones((1, 1, 16), dtype=BF), 1, False, out_f32=True, check=False)
+        assert float((lse.double() - math.log(n)).abs().max()) <= (2 ** 16 + 2 ** 8 + 16) * U
+        if exponent >= -84:
+            assert float((out.double() * 2.0 ** -exponent - 1).abs().max()) <= (2 ** 17 + 2 ** 8 + 16) * U + 2.0 ** -22
