@@ -456,7 +456,7 @@ int nvfp4_kv_cache_read_new(const nvfp4_kv_cache *cache, const int64_t *slots, i
  * the sum of two f16 numbers): within 2^-11 (2^-22) of each, and no closer than 2^-30 of the row's largest, whatever the pages'
  * scales are; their sum is that of the unrounded ones.  Pages whose value scale is below 2^-64 of another one's of the same
  * sequence, or below 2^-84, lose digits of their values; the weights of those count in the sum.  Scales are below 2^126 (those
- * that the quantizers choose are below 2^117).
+ * that the quantizers choose are below 2^117), and a row's largest query times softmax_scale log2(e) stays within fp32.
  * Refused (NVFP4_ERR_SHAPE) besides the above: a softmax_scale that is not positive, or not finite times log2(e), more than 2^30
  * pages, pages whose block scales or row means fill 4 GiB, and more rows or sequences than one launch covers (2^32 lanes).
  * workspace: nvfp4_kv_attention_workspace_bytes() bytes, 16-byte aligned (0 bytes: may be NULL): partial results where the

@@ -245,7 +245,7 @@ __global__ __launch_bounds__(64 * WAVES, D == 256 ? 1 : 2) void attention_tiles_
             if constexpr (SMOOTH) sum = sum8(w[c], e, sum);
         }
         sum += __shfl_xor(sum, 32, 64);
-        factor = __builtin_amdgcn_ldexpf(a.scale, -e);
+        factor = fmaxf(__builtin_amdgcn_ldexpf(a.scale, -e), 0x1p-126f);
         sum_q = hi == 0 ? sum : 0.0f;        // (the outer product has two terms, one of them zero)
     }
 
@@ -340,9 +340,11 @@ __global__ __launch_bounds__(64 * WAVES, D == 256 ? 1 : 2) void attention_tiles_
                         const int j = 32 * t + 8 * (e >> 2) + 4 * hi + (e & 3), g = 2 * t + (e >> 3);
                         x[t][e] = (((seen >> g & 1u) != 0u) & sight.of(at + j)) ? x[t][e] : -__builtin_inff();
                     }
-                // (of a page that is not in use anything may stand there)
+                // (of a page that is not in use anything may stand there; and no product of factors is so small that it is zero, which makes
+                // no number of a masked score)
+                const float least = __builtin_amdgcn_rcpf(factor) * 0x1p-126f;
 #pragma unroll
-                for (int g = 0; g < 4; ++g) kg[g] = (seen >> g & 1u) != 0u ? kg[g] : 1.0f;
+                for (int g = 0; g < 4; ++g) kg[g] = (seen >> g & 1u) != 0u ? fmaxf(kg[g], least) : 1.0f;
             }
             // the unit of the pages: it moves in front of the step, and groups whose pages are far from the others' wait for another walk
             const int before = __builtin_amdgcn_readfirstlane(lds.rare.unit[tid >> 6]), pass = __builtin_amdgcn_readfirstlane(lds.rare.pass);

@@ -205,3 +205,18 @@ def test_the_sum_of_millions_of_tokens_on_pages_of_the_least_scales():
         assert float((lse.double() - math.log(n)).abs().max()) <= (2 ** 16 + 2 ** 8 + 16) * U
         if exponent >= -84:
             assert float((out.double() * 2.0 ** -exponent - 1).abs().max()) <= (2 ** 17 + 2 ** 8 + 16) * U + 2.0 ** -22
+
+
+@pytest.mark.parametrize("queries", [1, 40, 150])
+@pytest.mark.parametrize("smooth", [False, True])
+def test_scores_that_are_too_small_for_a_number(queries, smooth):
+    """Queries and key scales whose products vanish: equal weights for what a row sees, masked tokens left out."""
+    for softmax_scale in (0.125, 1e-40):
+        say("[precision] vanishing", queries, smooth, softmax_scale)
+        c, table, starts, q = attention_case(72, [200, 75], [min(queries, 75)] * 2, 4, 2, 64, 16, smooth)
+        c.k_global.fill_(2.0 ** -100)
+        if smooth:
+            c.k_mean.zero_()
+        q = (q.sign() * 2.0 ** -120).to(BF)
+        for causal, window in ((True, 0), (True, 37), (False, 0)):
+            run_attention(c, table, [200, 75], starts, q, queries, causal, window=window, out_f32=True, scale=softmax_scale)
