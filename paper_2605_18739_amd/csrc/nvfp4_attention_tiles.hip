@@ -16,10 +16,13 @@ namespace nvfp4 {
 //    the order in which S^T leaves its tokens: of every sixteen {0-3, 8-11} for lanes 0-31 and {4-7, 12-15} for lanes 32-63.
 // LDS rows are 16-byte chunks, the chunk's place exclusive-or'ed with bits of the row, so that eight neighbouring rows read
 // (or written) at one chunk lie in different banks.
-// Measured (24 heads of 128, 3520 queries over 18480 tokens, smoothed keys): 930 us and 19 to join, 840 TFLOP/s, where a
-// library's product of 8192 x 8192 matrices holds 1170 to 1215: no single pipe is full (the matrix instructions alone take 410 us
-// at 2.14 GHz), and the clock depends on the operands (all zeros: 790 us).  2000 queries over 8192 tokens of
-// 16 heads: d = 64 126 us, 128 157 us, 256 432 us.  Four waves for up to 128 rows, because waves without rows only load.
+// Measured (24 heads of 128, 3520 queries over 18480 tokens, smoothed keys): 945 us and 17 to join, 830 TFLOP/s, where a
+// library's product of 8192 x 8192 matrices holds 1170 to 1215: no single pipe is full (counters: matrix instructions 45 % of the SIMDs'
+// cycles, vector ones 52, LDS 34 of the CUs'), and the clock depends on the operands (all zeros: a fifth less time).
+// 2000 queries over 8192 tokens of 16 heads: d = 64 130 us (matrix 22 %, vector 54: as many exponentials for half of the products),
+// 128 163, with smoothed keys 173, 256 450 (25 and 40: one wave a SIMD, whose waits nothing fills).  The same with pages
+// whose scales are far apart (16 tokens a page, d = 128, with the join 191): one page of zeros 184, every eighth 365, 2^-8 to 2^8 at
+// random 709.  Four waves for up to 128 rows, because waves without rows only load.
 template <int D, int WAVES>
 struct Tiles {
     static constexpr int kThreads = 64 * WAVES;

@@ -8,8 +8,9 @@ namespace nvfp4 {
 
 constexpr int kCacheThreads = 256, kCacheWaves = kCacheThreads / kWave;
 
-// Measured (3520 tokens of 24 heads of 128): writing smoothed keys and searched values 17 us, 3.2 TB/s, bound by the search's vector
-// instructions; reading 13 us, and 18480 tokens 61 us, 4.8 TB/s; 33 tokens of 8 heads 3.3 and 3.5 us, latency.
+// Measured (3520 tokens of 24 heads of 128): writing 10.6 us, 5.2 TB/s, the rate of a copy; with the search 13.7, smoothed keys 12.6, both
+// 16.6, the instructions of the one and the exchange of the other (a row's loads wait for its slot in all four); reading 13 us, and
+// 18480 tokens 61 us, 4.8 TB/s; 33 tokens of 8 heads 2.8 and 3.1 us, latency.
 // A wave works on one token of one tensor (keys or values), so the slot, the page and the page's scale with its tie tests
 // are the same for all its lanes: unit = (token, tensor, part of the token's row of H * d elements).
 struct CacheUnits {
