@@ -33,13 +33,13 @@ def listed():
         # its gradient, joined with that of the residual stream
         {"name": "norm_backward_train", "op": "norm_backward", "T": 17600, "C": 5120, "residual": True, "strided": False},
         # a down projection for five sequences that decode a token each: the weights' bytes
-        {"name": "gemm_decode", "op": "gemm", "M": 5, "N": 4096, "K": 14336, "tiles": True, "f32": False},
+        {"name": "gemm_decode", "op": "gemm", "M": 5, "N": 4096, "K": 14336, "tiles": True, "f32": False, "fast": False},
         # odd sizes: a short prompt through a projection whose width is no multiple of a tile or of a block
-        {"name": "gemm_odd", "op": "gemm", "M": 777, "N": 1111, "K": 2000, "tiles": True, "f32": False},
-        # the down projection of a chunk
-        {"name": "gemm_chunk", "op": "gemm", "M": 3520, "N": 4096, "K": 14336, "tiles": True, "f32": False},
+        {"name": "gemm_odd", "op": "gemm", "M": 777, "N": 1111, "K": 2000, "tiles": True, "f32": False, "fast": False},
+        # the down projection of a chunk, with the sums that the 8-bit matrix instruction makes
+        {"name": "gemm_chunk", "op": "gemm", "M": 3520, "N": 4096, "K": 14336, "tiles": True, "f32": False, "fast": True},
         # a weights' gradient, contracted over the tokens of a training clip (both operands with scales along the tokens)
-        {"name": "gemm_weight_gradient", "op": "gemm", "M": 4096, "N": 2048, "K": 17600, "tiles": False, "f32": True},
+        {"name": "gemm_weight_gradient", "op": "gemm", "M": 4096, "N": 2048, "K": 17600, "tiles": False, "f32": True, "fast": False},
         # gate and up projection for eight sequences that decode a token each
         {"name": "gated_decode", "op": "gated", "M": 8, "F": 14336, "K": 4096, "act": "silu", "train": False},
         # gate and up projection of a training clip's chunk, with what the backward pass needs
@@ -76,7 +76,9 @@ def draw(rng):
         return {"op": op, "M": rng.choice([_log(rng, 1, 64), _log(rng, 1, room)]), "F": F, "K": K, "act": rng.choice(["silu", "silu", "gelu"]), "train": rng.random() < 0.4}
     N = rng.choice([16 * _log(rng, 4, 896), _log(rng, 50, 5000)])
     room = min(8192, int(2.0e11 / (N * K)))
-    return {"op": op, "M": rng.choice([_log(rng, 1, 64), _log(rng, 1, room), _log(rng, 1, room)]), "N": N, "K": K, "tiles": rng.random() < 0.6, "f32": rng.random() < 0.3}
+    f32 = rng.random() < 0.3
+    return {"op": op, "M": rng.choice([_log(rng, 1, 64), _log(rng, 1, room), _log(rng, 1, room)]), "N": N, "K": K, "tiles": rng.random() < 0.6, "f32": f32,
+            "fast": not f32 and rng.random() < 0.5}
 
 
 # ---------------------------------------------------------------------------------------------------------------------
@@ -284,7 +286,7 @@ def _run_own(state):
         state["handles"] = [nv.E4M3Tensor(state[n]["codes"], state[n]["scales"]) for n in ("a", "w")]
     a, w = state["handles"]
     if op == "gemm":
-        return {"y": nv.nvfp4_e4m3_gemm(a, w, out_dtype=nv.OUT_F32 if case["f32"] else nv.OUT_BF16)}
+        return {"y": nv.nvfp4_e4m3_gemm(a, w, out_dtype=nv.OUT_F32 if case["f32"] else nv.OUT_BF16, fast_sums=case["fast"])}
     q, _, gate_up = nv.nvfp4_e4m3_gemm_gated(a, w, act=act, keep_gate_up=case["train"])
     return {"codes": q.codes, "scales": q.scales, "gate_up": gate_up} if case["train"] else {"codes": q.codes, "scales": q.scales}
 
