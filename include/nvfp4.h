@@ -70,7 +70,9 @@ typedef struct nvfp4_tensor {
 enum { NVFP4_OUT_F32 = 0, NVFP4_OUT_BF16 = 1 };
 /* or'ed to the type of nvfp4_kv_attention's output: out, lse hold nothing yet */
 enum { NVFP4_OUT_NEW = 0x100, NVFP4_LSE_NEW = 0x200 };
-enum { NVFP4_ACT_NONE = 0, NVFP4_ACT_GELU_TANH = 1 };
+/* or'ed to the output type of nvfp4_e4m3_gemm or the activation of nvfp4_e4m3_gemm_gated */
+enum { NVFP4_SUMS_FAST = 0x400 };
+enum { NVFP4_ACT_NONE = 0, NVFP4_ACT_GELU_TANH = 1, NVFP4_ACT_SILU = 2 /* gated layers only */ };
 enum { NVFP4_OP_QUANTIZE = 0, NVFP4_OP_KV_QUANT = 1, NVFP4_OP_GEMM_ACT_QUANT = 2, NVFP4_OP_GEMM = 3,
        NVFP4_OP_KV_DEQUANT = 4,
        NVFP4_OP_GEMM_ACT_QUANT_GEMM = 5 /* timing only: the GEMM kernel inside nvfp4_gemm_act_quant */,
@@ -80,7 +82,9 @@ enum { NVFP4_OP_QUANTIZE = 0, NVFP4_OP_KV_QUANT = 1, NVFP4_OP_GEMM_ACT_QUANT = 2
        NVFP4_OP_LORA_DOWN = 13, NVFP4_OP_GEMM_LORA = 14,
        NVFP4_OP_PROBE = 15 /* timing only: nvfp4_probe */, NVFP4_OP_GEMM_SCALE_OUT = 16,
        NVFP4_OP_QK_NORM_ROPE = 17, NVFP4_OP_QK_NORM_ROPE_BACKWARD = 18, NVFP4_OP_KV_CACHE_WRITE = 19,
-       NVFP4_OP_KV_CACHE_READ = 20, NVFP4_OP_KV_ATTENTION = 21 };
+       NVFP4_OP_KV_CACHE_READ = 20, NVFP4_OP_KV_ATTENTION = 21,
+       NVFP4_OP_E4M3_QUANTIZE = 22, NVFP4_OP_E4M3_QUANTIZE_2D = 23, NVFP4_OP_E4M3_GEMM = 24, NVFP4_OP_E4M3_GEMM_GATED = 25,
+       NVFP4_OP_GATED_BACKWARD = 26, NVFP4_OP_RMS_NORM = 27, NVFP4_OP_RMS_NORM_BACKWARD = 28 };
 
 /*
  * Quantizer (Sec. 2.2, Eq. 2; Eq. 12 with target magnitude 6).
@@ -470,6 +474,99 @@ int nvfp4_kv_attention(const void *q_bf16, int64_t ldq, int64_t total_q, int64_t
 /* max_kv = max_pages * page_tokens; 0 where no workspace is needed, and for sizes that the call refuses */
 size_t nvfp4_kv_attention_workspace_bytes(int64_t total_q, int64_t Hq, int64_t H, int64_t d, int64_t max_kv, int64_t B,
                                           int64_t max_q, int64_t window, int64_t sink);
+
+/*
+ * 8-bit tensors, for the layers and gradients that a 4-bit recipe leaves in a higher precision:
+ *   x^ = code * 2^(scale byte - 127)
+ *   codes   [rows, K]  one E4M3 byte (1-4-3, bias 7, max 448; 0x7F and 0xFF are NaN)
+ *   scales  one E8M0 byte (a power of two, 255 is NaN) for 128 consecutive elements along K, the last block of a row may be
+ *           shorter: block_rows 1: [rows, ceil(K / 128)]; block_rows 128: one for 128 x 128, [ceil(rows / 128), ceil(K / 128)]
+ * Scale of a block: the smallest 2^e, e >= -127, with max|x| <= 448 * 2^e (2^-127 for a block of zeros); code: the E4M3 number
+ * nearest to x / 2^e, ties to even.  Nothing saturates, and a block's relative precision is that of E4M3 whatever its scale is.
+ * A block that holds an infinity or NaN gets scale 255 and NaN codes.
+ * K % 16 == 0, K <= 2^22, rows <= 2^30; both arrays contiguous, 16-byte aligned device memory.
+ */
+#define NVFP4_E4M3_BLOCK 128
+typedef struct nvfp4_e4m3_tensor {
+    uint8_t *codes, *scales;
+    int64_t  rows, K;
+    int32_t  block_rows;
+} nvfp4_e4m3_tensor;
+
+/*
+ * x_bf16 [R, C], row stride ld elements (ld >= C, ld % 8 == 0), to 8 bits with block_rows 1.
+ * block_axis 0: blocks run along C (C % 16 == 0); out has rows = R, K = C.
+ * block_axis 1: blocks run along R, out is the transpose (the operand of a product contracted over the rows): rows = C
+ *               (C % 8 == 0), K = R rounded up to a multiple of 16, filled up with zeros.
+ * nvfp4_e4m3_quantize_2d: one scale for each 128 x 128 tile, so that w [R, C] and its transpose hold the same values (weights:
+ *   forward operand and that of the input's gradient).  R % 16 == 0, C % 16 == 0; out: rows = R, K = C, out_t: NULL, or
+ *   rows = C, K = R; both with block_rows 128.
+ */
+int nvfp4_e4m3_quantize(const void *x_bf16, int64_t R, int64_t C, int64_t ld, int block_axis, nvfp4_e4m3_tensor *out, void *stream);
+int nvfp4_e4m3_quantize_2d(const void *w_bf16, int64_t R, int64_t C, int64_t ld, nvfp4_e4m3_tensor *out, nvfp4_e4m3_tensor *out_t, void *stream);
+
+/*
+ * Y[m,n] = sum_k A^[m,k] W^[n,k], accumulated in fp32: A [M, K] with block_rows 1, W [N, K] with block_rows 128 (weights) or 1
+ * (the second operand of a weights' gradient: dW = dY^T X is this product of the two transposes that block_axis 1 gives).
+ * Y: [M, N], row stride ldy >= N elements, fp32 (NVFP4_OUT_F32) or bf16 (NVFP4_OUT_BF16, rounded once); any M, N >= 1 and any
+ * ldy (rows that are whole 16-byte words are stored fastest).  Rows of NaN scales or codes give NaN.  The order of the sums
+ * depends on M, N and K (up to 64 rows take a kernel of their own) and on nothing else.
+ * Products are exact and their sums fp32.  With out_dtype | NVFP4_SUMS_FAST, for more than 64 rows, the 8-bit matrix instruction
+ * makes them at about twice the rate: it aligns eight products that are neighbours along K to the largest of them and drops
+ * what is below 2^-13 of that one (the result is off by at most 2^-10 sum_k |A^ W^|, and 1.5e-5 to 5e-5 relative to it for operands
+ * as layers have them: far below a bf16 result's rounding, not below an fp32 one's).
+ * Operands below 2^-126 or above the bf16 range (code times scale) are outside the contract.
+ */
+int nvfp4_e4m3_gemm(const nvfp4_e4m3_tensor *A, const nvfp4_e4m3_tensor *W, void *Y, int64_t ldy, int out_dtype, void *stream);
+
+/*
+ * Gated projections in one kernel: with W [2F, K], the gate's F rows in front of the up projection's,
+ *   g = A W[0:F]^T,  u = A W[F:2F]^T,  h = act(g) u     (fp32 until h is rounded)
+ * act: NVFP4_ACT_SILU or NVFP4_ACT_GELU_TANH (| NVFP4_SUMS_FAST: sums as in nvfp4_e4m3_gemm).  Results, each of which may be NULL (not all):
+ *   out      h in 8 bits along F (rows = M, K = F, block_rows 1; F % 16 == 0), the operand of the down projection
+ *   h_bf16   h, [M, F], row stride ld_h
+ *   gate_up_bf16  g and u side by side, [M, 2F], row stride ld_gate_up: what nvfp4_gated_backward takes
+ * workspace: nvfp4_workspace_bytes(NVFP4_OP_E4M3_GEMM_GATED, M, F, 0) bytes, 16-byte aligned, may be NULL if that is 0 or
+ * without out.
+ */
+int nvfp4_e4m3_gemm_gated(const nvfp4_e4m3_tensor *A, const nvfp4_e4m3_tensor *W, int act, nvfp4_e4m3_tensor *out, void *h_bf16, int64_t ld_h,
+                          void *gate_up_bf16, int64_t ld_gate_up, void *workspace, size_t workspace_bytes, void *stream);
+
+/*
+ * Backward pass of h = act(g) u.  From dh [T, F] and gate_up = [g | u] [T, 2F] (bf16, row strides multiples of 8),
+ *   dg = dh u act'(g),  du = dh act(g)     (fp32, rounded once)
+ * side by side as [dg | du], and h again:
+ *   out     [T, 2F] along the features (rows = T, K = 2F; F % 128 == 0): dX = out W is nvfp4_e4m3_gemm with the transpose of W
+ *   out_t   along the tokens (rows = 2F, K = T rounded up to 16, zeros behind T): dW = out_t X
+ *   h_t     h along the tokens (rows = F, K likewise), for the down projection's weights; from the bf16 g and u
+ *   d_bf16  [dg | du] in bf16, row stride ld_d a multiple of 8; may be gate_up itself
+ * Each may be NULL (not all); block_rows 1.  F % 8 == 0.  Rounding to 8 bits counts as the identity: the gradients are those
+ * of the unquantized h.
+ */
+int nvfp4_gated_backward(const void *dh_bf16, int64_t ld_dh, const void *gate_up_bf16, int64_t ld_gate_up, int64_t T, int64_t F, int act,
+                         nvfp4_e4m3_tensor *out, nvfp4_e4m3_tensor *out_t, nvfp4_e4m3_tensor *h_t, void *d_bf16, int64_t ld_d, void *stream);
+
+/*
+ * RMS norm of the residual stream, with the residual's addition:
+ *   s = RN_bf16(x + residual) (x itself without a residual),  y = w s / sqrt( mean(s^2) + eps )     (fp32)
+ * x, residual: bf16 [T, C], row strides multiples of 8, C % 16 == 0, C <= 16384; weight bf16 [C].
+ *   sum_bf16  receives s; given exactly when residual is; may be x or residual itself (same stride)
+ *   out       y in 8 bits along C (rows = T, K = C, block_rows 1), or NULL      y_bf16  y in bf16, or NULL (not both)
+ * Magnitudes whose squares leave the fp32 range are outside the contract, as is eps below the normal fp32 numbers
+ * (NVFP4_ERR_SHAPE).
+ */
+int nvfp4_rms_norm(const void *x_bf16, int64_t ld, const void *residual_bf16, int64_t ld_residual, const void *weight_bf16, int64_t T, int64_t C,
+                   float eps, void *sum_bf16, int64_t ld_sum, nvfp4_e4m3_tensor *out, void *y_bf16, int64_t ld_y, void *stream);
+/*
+ * Its backward pass, from dy, the sum s that the forward pass normalised, and (or NULL) dsum, the gradient that the stream
+ * itself brings:  r = 1 / sqrt( mean(s^2) + eps ),  xh = r s,
+ *   dx = dsum + r ( w dy - xh mean(w dy xh) )  (bf16, rounded once; the gradient of x and of the residual alike; may be dy, s
+ *   or dsum itself),   dweight = sum over rows of dy xh (fp32 [C], or NULL; added in a fixed order).
+ * workspace: nvfp4_workspace_bytes(NVFP4_OP_RMS_NORM_BACKWARD, T, C, 0) bytes, 16-byte aligned; may be NULL without dweight.
+ */
+int nvfp4_rms_norm_backward(const void *dy_bf16, int64_t ld_dy, const void *s_bf16, int64_t ld_s, const void *weight_bf16, const void *dsum_bf16,
+                            int64_t ld_dsum, int64_t T, int64_t C, float eps, void *dx_bf16, int64_t ld_dx, float *dweight, void *workspace,
+                            size_t workspace_bytes, void *stream);
 
 /* Workspace size in bytes for `op` (NVFP4_OP_*) at the given sizes; 0 on a bad op. */
 size_t nvfp4_workspace_bytes(int op, int64_t a, int64_t b, int64_t c);

@@ -24,7 +24,7 @@ _lib = None
 _host_module = None
 
 OUT_F32, OUT_BF16 = 0, 1
-ACT_NONE, ACT_GELU_TANH = 0, 1
+ACT_NONE, ACT_GELU_TANH, ACT_SILU = 0, 1, 2
 OP_QUANTIZE, OP_KV_QUANT, OP_GEMM_ACT_QUANT, OP_GEMM, OP_KV_DEQUANT, OP_GEMM_ACT_QUANT_GEMM = 0, 1, 2, 3, 4, 5
 OP_QUANTIZE_4OVER6, OP_KV_QUANT_4OVER6, OP_KV_QUANT_K, OP_KV_DEQUANT_GATHER = 6, 7, 8, 9
 KV_MAX_CHUNKS = 64
@@ -32,7 +32,10 @@ NOALLOC_MAX_ELEMENTS = 1 << 32
 OP_QUANTIZE_2D, OP_QUANTIZE_RHT, OP_QUANTIZE_A2A, OP_LORA_DOWN, OP_GEMM_LORA, OP_PROBE = 10, 11, 12, 13, 14, 15
 OP_GEMM_SCALE_OUT = 16
 OP_QK_NORM_ROPE, OP_QK_NORM_ROPE_BACKWARD, OP_KV_CACHE_WRITE, OP_KV_CACHE_READ, OP_KV_ATTENTION = 17, 18, 19, 20, 21
+OP_E4M3_QUANTIZE, OP_E4M3_QUANTIZE_2D, OP_E4M3_GEMM, OP_E4M3_GEMM_GATED, OP_GATED_BACKWARD, OP_RMS_NORM, OP_RMS_NORM_BACKWARD = 22, 23, 24, 25, 26, 27, 28
 ROPE_MAX_AXES, HEAD_DIM_MAX = 4, 256
+E4M3_BLOCK = 128
+_SUMS_FAST = 0x400
 LORA_RANK = 128
 
 
@@ -64,6 +67,10 @@ class _CKvCache(ctypes.Structure):
     _fields_ = [("k_codes", ctypes.c_void_p), ("k_scales", ctypes.c_void_p), ("k_global", ctypes.c_void_p), ("k_mean", ctypes.c_void_p),
                 ("v_codes", ctypes.c_void_p), ("v_scales", ctypes.c_void_p), ("v_global", ctypes.c_void_p),
                 ("n_pages", ctypes.c_int64), ("page_tokens", ctypes.c_int64), ("H", ctypes.c_int64), ("d", ctypes.c_int64)]
+
+
+class _CE4m3Tensor(ctypes.Structure):
+    _fields_ = [("codes", ctypes.c_void_p), ("scales", ctypes.c_void_p), ("rows", ctypes.c_int64), ("K", ctypes.c_int64), ("block_rows", ctypes.c_int32)]
 
 
 class NVFP4Error(RuntimeError):
@@ -128,6 +135,21 @@ def lib():
                                          vp, i64, c.c_int, vp, vp, sz, vp]
         L.nvfp4_kv_attention_workspace_bytes.restype = sz
         L.nvfp4_kv_attention_workspace_bytes.argtypes = [i64] * 9
+        ep = c.POINTER(_CE4m3Tensor)
+        L.nvfp4_e4m3_quantize.restype = c.c_int
+        L.nvfp4_e4m3_quantize.argtypes = [vp, i64, i64, i64, c.c_int, ep, vp]
+        L.nvfp4_e4m3_quantize_2d.restype = c.c_int
+        L.nvfp4_e4m3_quantize_2d.argtypes = [vp, i64, i64, i64, ep, ep, vp]
+        L.nvfp4_e4m3_gemm.restype = c.c_int
+        L.nvfp4_e4m3_gemm.argtypes = [ep, ep, vp, i64, c.c_int, vp]
+        L.nvfp4_e4m3_gemm_gated.restype = c.c_int
+        L.nvfp4_e4m3_gemm_gated.argtypes = [ep, ep, c.c_int, ep, vp, i64, vp, i64, vp, sz, vp]
+        L.nvfp4_gated_backward.restype = c.c_int
+        L.nvfp4_gated_backward.argtypes = [vp, i64, vp, i64, i64, i64, c.c_int, ep, ep, ep, vp, i64, vp]
+        L.nvfp4_rms_norm.restype = c.c_int
+        L.nvfp4_rms_norm.argtypes = [vp, i64, vp, i64, vp, i64, i64, c.c_float, vp, i64, ep, vp, i64, vp]
+        L.nvfp4_rms_norm_backward.restype = c.c_int
+        L.nvfp4_rms_norm_backward.argtypes = [vp, i64, vp, i64, vp, vp, i64, i64, i64, c.c_float, vp, i64, vp, vp, sz, vp]
         L.nvfp4_workspace_bytes.restype = sz
         L.nvfp4_workspace_bytes.argtypes = [c.c_int, i64, i64, i64]
         L.nvfp4_status_string.restype = c.c_char_p
@@ -202,7 +224,7 @@ def _on(stream, call, *args):
         result = call(*args)
     for new in result if isinstance(result, tuple) else () if isinstance(result, NVFP4KvCache) else (result,):
         if new is not None and not any(new is a for a in args):
-            for t in (new.codes, new.scales, new.global_scale) if isinstance(new, NVFP4Tensor) else (new,):
+            for t in (new.codes, new.scales, new.global_scale) if isinstance(new, NVFP4Tensor) else new._native if isinstance(new, E4M3Tensor) else (new,):
                 t.record_stream(here)
     return result
 
@@ -541,6 +563,121 @@ def nvfp4_kv_attention(q, cache, page_table, kv_lens, q_starts, max_q, softmax_s
                                         1 if causal else 0, window, sink, out_dtype, out, lse, workspace, _stream(stream))
     _check(rc)
     return out, lse
+
+
+class E4M3Tensor:
+    """8-bit tensor (see include/nvfp4.h): codes float8_e4m3fn [rows, K], scales float8_e8m0fnu for 128 elements of a row
+    [rows, ceil(K / 128)] or for 128 x 128 [ceil(rows / 128), ceil(K / 128)]; contiguous (uint8 is taken for either type)."""
+
+    def __init__(self, codes, scales):
+        if codes.dim() != 2:
+            raise _wrong_rank(codes, 2)
+        rows, K = codes.shape
+        assert codes.dtype in (torch.float8_e4m3fn, torch.uint8) and codes.is_contiguous(), "codes: expected a contiguous float8_e4m3fn matrix"
+        assert scales.dtype in (torch.float8_e8m0fnu, torch.uint8) and scales.is_contiguous(), "scales: expected a contiguous float8_e8m0fnu matrix"
+        blocks = -(-K // E4M3_BLOCK)
+        assert tuple(scales.shape) in ((rows, blocks), (-(-rows // E4M3_BLOCK), blocks)), "scales: expected one for 128 elements of a row, or for 128 x 128"
+        self._set(codes, scales)
+
+    def _set(self, codes, scales):
+        self.codes, self.scales = codes, scales
+        self.rows, self.K = codes.shape
+        self.block_rows = 1 if scales.shape[0] == self.rows else E4M3_BLOCK
+        self._native = (codes, scales)
+        return self
+
+    @staticmethod
+    def empty(rows, K, block_rows=1, device="cuda"):
+        """A tensor without contents."""
+        assert block_rows in (1, E4M3_BLOCK), "block_rows: 1 or 128"
+        return E4M3Tensor(torch.empty((rows, K), dtype=torch.float8_e4m3fn, device=device),
+                          torch.empty((-(-rows // block_rows), -(-K // E4M3_BLOCK)), dtype=torch.float8_e8m0fnu, device=device))
+
+    def c(self):
+        return _CE4m3Tensor(self.codes.data_ptr(), self.scales.data_ptr(), self.rows, self.K, self.block_rows)
+
+
+def _native(t):
+    return None if t is None else t._native
+
+
+def _tensor8(given, codes, scales):
+    """The caller's tensor, or the new one of a call (None: neither)."""
+    return given if codes is None else E4M3Tensor.__new__(E4M3Tensor)._set(codes, scales)
+
+
+def nvfp4_e4m3_quantize(x, block_axis=0, out=None, stream=None):
+    """x: bf16 [R, C] device tensor with unit stride along C, to 8 bits with a scale for each 128 elements along C (block_axis 0), or
+    along R and transposed (block_axis 1: [C, R rounded up to 16]).  Returns an E4M3Tensor."""
+    if stream is not None and _elsewhere(stream):
+        return _on(stream, nvfp4_e4m3_quantize, x, block_axis, out)
+    rc, codes, scales = _host().e4m3_quantize(x, block_axis, _native(out), _stream(stream))
+    _check(rc)
+    return _tensor8(out, codes, scales)
+
+
+def nvfp4_e4m3_quantize_2d(w, transposed=True, out=None, out_t=None, stream=None):
+    """w: bf16 [R, C] weights (R, C multiples of 16), one scale per 128 x 128.  Returns (E4M3Tensor [R, C], E4M3Tensor [C, R] or None)."""
+    if stream is not None and _elsewhere(stream):
+        return _on(stream, nvfp4_e4m3_quantize_2d, w, transposed, out, out_t)
+    rc, codes, scales, codes_t, scales_t = _host().e4m3_quantize_2d(w, 1 if transposed else 0, _native(out), _native(out_t), _stream(stream))
+    _check(rc)
+    return _tensor8(out, codes, scales), _tensor8(out_t, codes_t, scales_t)
+
+
+def nvfp4_e4m3_gemm(A, W, out_dtype=OUT_F32, Y=None, fast_sums=False, stream=None):
+    """Y = A W^T of E4M3Tensors A [M, K] (scales by rows) and W [N, K] (by rows or 128 x 128).  Rows of a new Y start on 16-byte boundaries.
+    fast_sums: at about twice the rate, with sums of eight products that keep 13 bits below the largest (see include/nvfp4.h)."""
+    if stream is not None and _elsewhere(stream):
+        return _on(stream, nvfp4_e4m3_gemm, A, W, out_dtype, Y, fast_sums)
+    rc, new = _host().e4m3_gemm(A._native, W._native, out_dtype, Y, 1 if fast_sums else 0, _stream(stream))
+    _check(rc)
+    return Y if new is None else new
+
+
+def nvfp4_e4m3_gemm_gated(A, W, act=ACT_SILU, quantize=True, keep_h=False, keep_gate_up=False, out=None, h=None, gate_up=None, workspace=None,
+                          fast_sums=False, stream=None):
+    """h = act(A Wg^T) * (A Wu^T) with W [2F, K], the gate's rows first.  Returns (out, h, gate_up): h in 8 bits (quantize, or `out` given),
+    in bf16 (keep_h, or given) and [gate | up] in bf16 [M, 2F] (keep_gate_up, or given), None for what is not asked for.
+    fast_sums: as in nvfp4_e4m3_gemm."""
+    if stream is not None and _elsewhere(stream):
+        return _on(stream, nvfp4_e4m3_gemm_gated, A, W, act, quantize, keep_h, keep_gate_up, out, h, gate_up, workspace, fast_sums)
+    rc, codes, scales, new_h, new_gate_up = _host().e4m3_gemm_gated(A._native, W._native, act, 1 if quantize else 0, 1 if keep_h else 0, 1 if keep_gate_up else 0,
+                                                                    _native(out), h, gate_up, workspace, 1 if fast_sums else 0, _stream(stream))
+    _check(rc)
+    return _tensor8(out, codes, scales), h if new_h is None else new_h, gate_up if new_gate_up is None else new_gate_up
+
+
+def nvfp4_gated_backward(dh, gate_up, act=ACT_SILU, quantize=True, recompute_h=False, keep_bf16=False, out=None, out_t=None, h_t=None, d=None, stream=None):
+    """Gradients [dg | du] of the gated activation from dh [T, F] and gate_up [T, 2F] (bf16).  Returns (out, out_t, h_t, d): in 8 bits along the
+    features and, transposed, along the tokens (quantize, or given), h again along the tokens (recompute_h, or given), in bf16 (keep_bf16, or given)."""
+    if stream is not None and _elsewhere(stream):
+        return _on(stream, nvfp4_gated_backward, dh, gate_up, act, quantize, recompute_h, keep_bf16, out, out_t, h_t, d)
+    rc, codes, scales, codes_t, scales_t, h_codes, h_scales, new_d = _host().gated_backward(
+        dh, gate_up, act, 1 if quantize else 0, 1 if recompute_h else 0, 1 if keep_bf16 else 0, _native(out), _native(out_t), _native(h_t), d, _stream(stream))
+    _check(rc)
+    return _tensor8(out, codes, scales), _tensor8(out_t, codes_t, scales_t), _tensor8(h_t, h_codes, h_scales), d if new_d is None else new_d
+
+
+def nvfp4_rms_norm(x, weight, residual=None, eps=1e-6, quantize=True, keep_bf16=False, out=None, y=None, sum=None, stream=None):
+    """RMS norm over the rows of x + residual (bf16 [T, C], any row stride; residual may be None), weight bf16 [C].  Returns (out, y, sum): the
+    result in 8 bits (quantize, or given) and in bf16 (keep_bf16, or given), and x + residual in bf16 (None without a residual; may be
+    given as x or residual itself)."""
+    if stream is not None and _elsewhere(stream):
+        return _on(stream, nvfp4_rms_norm, x, weight, residual, eps, quantize, keep_bf16, out, y, sum)
+    rc, codes, scales, new_y, new_sum = _host().rms_norm(x, weight, residual, eps, 1 if quantize else 0, 1 if keep_bf16 else 0, _native(out), y, sum, _stream(stream))
+    _check(rc)
+    return _tensor8(out, codes, scales), y if new_y is None else new_y, sum if new_sum is None else new_sum
+
+
+def nvfp4_rms_norm_backward(dy, s, weight, dsum=None, eps=1e-6, weight_grad=True, dx=None, dweight=None, workspace=None, stream=None):
+    """Gradients of nvfp4_rms_norm from that of its output, the sum s that it normalised and (or None) the gradient dsum of that sum
+    from elsewhere.  Returns (dx, dweight): bf16 [T, C], for x and the residual alike, and fp32 [C] (None with weight_grad=False)."""
+    if stream is not None and _elsewhere(stream):
+        return _on(stream, nvfp4_rms_norm_backward, dy, s, weight, dsum, eps, weight_grad, dx, dweight, workspace)
+    rc, new_dx, new_dweight = _host().rms_norm_backward(dy, s, weight, dsum, eps, 1 if weight_grad else 0, dx, dweight, workspace, _stream(stream))
+    _check(rc)
+    return dx if new_dx is None else new_dx, dweight if new_dweight is None else new_dweight
 
 
 def nvfp4_gemm_plan(M, N, K):

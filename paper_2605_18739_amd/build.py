@@ -16,7 +16,9 @@ LIB = os.path.join(HERE, "libnvfp4_hip.so")
 HOST = os.path.join(HERE, "_host" + sysconfig.get_config_var("EXT_SUFFIX"))       # (tied to this Python by its name, to this torch by a check)
 SOURCES = ["nvfp4_gemm_tile_256x256.hip", "nvfp4_gemm_tile_256x192.hip", "nvfp4_gemm_tile_128x128.hip",
            "nvfp4_gemm_split.hip", "nvfp4_quantize.hip", "nvfp4_quantize_resident.hip", "nvfp4_gemm.hip", "nvfp4_norm_rope.hip",
-           "nvfp4_kv_cache.hip", "nvfp4_attention_rows16.hip", "nvfp4_attention_tiles.hip", "nvfp4_attention_join.hip", "nvfp4_probe.hip", "nvfp4_api.hip"]
+           "nvfp4_kv_cache.hip", "nvfp4_attention_rows16.hip", "nvfp4_attention_tiles.hip", "nvfp4_attention_join.hip", "nvfp4_probe.hip",
+           "nvfp4_e4m3_gemm_256x256.hip", "nvfp4_e4m3_gemm_256x128.hip", "nvfp4_e4m3_gemm_128x256.hip", "nvfp4_e4m3_gemm_64x256.hip", "nvfp4_e4m3_gemm_128x128.hip",
+           "nvfp4_e4m3_gemm_64x64.hip", "nvfp4_e4m3_gemm.hip", "nvfp4_e4m3_quantize.hip", "nvfp4_gated_backward.hip", "nvfp4_rms_norm.hip", "nvfp4_api.hip"]
 FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC",
          # packed-FP32 instructions are kept out of every kernel
          "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",

@@ -228,6 +228,58 @@ int fill_pages(const nvfp4_kv_cache *c, KvPages *p)
     return NVFP4_OK;
 }
 
+// ---- 8-bit operands ------------------------------------------------------------------------------------------
+static_assert(kRmsNormMaxC == 16384);
+constexpr int64_t kE4m3MaxK = 1ll << 22, kMaxStride = 1ll << 32;
+bool stride_ok(int64_t ld, int64_t cols) { return ld >= cols && ld <= kMaxStride; }
+int64_t up16(int64_t n) { return (n + 15) & ~15ll; }
+int64_t blocks128(int64_t n) { return (n + 127) >> 7; }
+int check_e4m3(const nvfp4_e4m3_tensor *t)
+{
+    if (!t || !t->codes || !t->scales) return NVFP4_ERR_NULL;
+    if (t->rows <= 0 || t->rows > kMaxIndex || t->K <= 0 || t->K > kE4m3MaxK || (t->K & 15) != 0) return NVFP4_ERR_SHAPE;
+    if (t->block_rows != 1 && t->block_rows != NVFP4_E4M3_BLOCK) return NVFP4_ERR_SHAPE;
+    if (!aligned16(t->codes) || !aligned16(t->scales)) return NVFP4_ERR_ALIGN;
+    return NVFP4_OK;
+}
+int check_e4m3_out(const nvfp4_e4m3_tensor *t, int64_t rows, int64_t K, int block_rows)
+{
+    if (int rc = check_e4m3(t)) return rc;
+    return t->rows == rows && t->K == K && t->block_rows == block_rows ? NVFP4_OK : NVFP4_ERR_SHAPE;
+}
+// bf16 [R, C] that kernels read or write in 16-byte words
+int check_matrix(const void *x, int64_t ld, int64_t C)
+{
+    if (!x) return NVFP4_ERR_NULL;
+    if (!stride_ok(ld, C)) return NVFP4_ERR_SHAPE;
+    return aligned16(x) && (ld & 7) == 0 ? NVFP4_OK : NVFP4_ERR_ALIGN;
+}
+int fill_e4m3_gemm(const nvfp4_e4m3_tensor *A, const nvfp4_e4m3_tensor *W, bool gated, E4m3GemmArgs *g)
+{
+    if (int rc = check_e4m3(A)) return rc;
+    if (int rc = check_e4m3(W)) return rc;
+    const int64_t nb = blocks128(A->K), M = A->rows, N = gated ? W->rows / 2 : W->rows;
+    if (A->K != W->K || (A->block_rows != 1 && M > 1) || (gated && (W->rows & 1) != 0)) return NVFP4_ERR_SHAPE;
+    // (a tile's scales are addressed with 32 bits, gated from the gate's first row to the up projection's last)
+    if (gated && W->rows > (1ll << 31) / nb - 1024) return NVFP4_ERR_SHAPE;
+    if ((M + 63) / 64 > (kMaxLanes / 256 - 8) / ((N + 63) / 64) || (M <= 64 && N > (kMaxLanes / 512 - 1) * 16)) return NVFP4_ERR_SHAPE;
+    g->codes_a = A->codes;
+    g->scales_a = A->scales;
+    g->codes_w = W->codes;
+    g->scales_w = W->scales;
+    g->M = M;
+    g->N = N;
+    g->K = A->K;
+    g->w_tiles = W->block_rows != 1;
+    g->scale_words = (nb & 3) == 0;
+    return NVFP4_OK;
+}
+int check_rms_norm(int64_t T, int64_t C, float eps)
+{
+    if (T <= 0 || T > kMaxLanes / 512 || C <= 0 || C > kRmsNormMaxC || (C & 15) != 0) return NVFP4_ERR_SHAPE;
+    return std::isnormal(eps) && eps > 0.0f ? NVFP4_OK : NVFP4_ERR_SHAPE;
+}
+
 // sizes of an attention call that its kernels and its workspace go by
 bool attention_sizes_ok(int64_t total_q, int64_t Hq, int64_t H, int64_t d, int64_t max_kv, int64_t B, int64_t max_q)
 {
@@ -764,6 +816,195 @@ size_t nvfp4_kv_attention_workspace_bytes(int64_t total_q, int64_t Hq, int64_t H
     return attention_grid_ok(plan, Hq, H, B, max_q) ? attention_workspace_bytes(plan, d) : 0;
 }
 
+int nvfp4_e4m3_quantize(const void *x_bf16, int64_t R, int64_t C, int64_t ld, int block_axis, nvfp4_e4m3_tensor *out, void *stream)
+{
+    if (!x_bf16 || !out) return NVFP4_ERR_NULL;
+    if (R <= 0 || C <= 0 || R > kMaxIndex || C > kMaxIndex || (block_axis != 0 && block_axis != 1)) return NVFP4_ERR_SHAPE;
+    if ((C & (block_axis == 0 ? 15 : 7)) != 0) return NVFP4_ERR_SHAPE;
+    if (int rc = check_e4m3_out(out, block_axis == 0 ? R : C, block_axis == 0 ? C : up16(R), 1)) return rc;
+    if (int rc = check_matrix(x_bf16, ld, C)) return rc;
+    const int64_t groups = block_axis == 0 ? R * ((C + 511) / 512) / 16 + 1 : blocks128(R) * blocks128(C);
+    if (groups > kMaxLanes / 256) return NVFP4_ERR_SHAPE;
+    std::lock_guard<std::mutex> lk(g_mu);
+    hipStream_t s = static_cast<hipStream_t>(stream);
+    Timed t(s, NVFP4_OP_E4M3_QUANTIZE);
+    const uint16_t *x = static_cast<const uint16_t *>(x_bf16);
+    hipError_t e = block_axis == 0 ? launch_e4m3_rows(x, R, C, ld, out->codes, out->scales, s) : launch_e4m3_columns(x, R, C, ld, out->codes, out->scales, s);
+    return e == hipSuccess ? NVFP4_OK : NVFP4_ERR_LAUNCH;
+}
+
+int nvfp4_e4m3_quantize_2d(const void *w_bf16, int64_t R, int64_t C, int64_t ld, nvfp4_e4m3_tensor *out, nvfp4_e4m3_tensor *out_t, void *stream)
+{
+    if (!w_bf16 || !out) return NVFP4_ERR_NULL;
+    if (R <= 0 || C <= 0 || (R & 15) != 0 || (C & 15) != 0) return NVFP4_ERR_SHAPE;
+    if (int rc = check_e4m3_out(out, R, C, NVFP4_E4M3_BLOCK)) return rc;
+    if (out_t)
+        if (int rc = check_e4m3_out(out_t, C, R, NVFP4_E4M3_BLOCK)) return rc;
+    if (int rc = check_matrix(w_bf16, ld, C)) return rc;
+    if (blocks128(R) > kMaxLanes / 256 / blocks128(C)) return NVFP4_ERR_SHAPE;
+    std::lock_guard<std::mutex> lk(g_mu);
+    hipStream_t s = static_cast<hipStream_t>(stream);
+    Timed t(s, NVFP4_OP_E4M3_QUANTIZE_2D);
+    hipError_t e = launch_e4m3_tiles(static_cast<const uint16_t *>(w_bf16), R, C, ld, out->codes, out->scales, out_t ? out_t->codes : nullptr,
+                                     out_t ? out_t->scales : nullptr, s);
+    return e == hipSuccess ? NVFP4_OK : NVFP4_ERR_LAUNCH;
+}
+
+int nvfp4_e4m3_gemm(const nvfp4_e4m3_tensor *A, const nvfp4_e4m3_tensor *W, void *Y, int64_t ldy, int out_dtype, void *stream)
+{
+    E4m3GemmArgs g{};
+    if (int rc = fill_e4m3_gemm(A, W, false, &g)) return rc;
+    if (!Y) return NVFP4_ERR_NULL;
+    g.fast = (out_dtype & NVFP4_SUMS_FAST) != 0;
+    out_dtype &= ~NVFP4_SUMS_FAST;
+    if ((out_dtype != NVFP4_OUT_F32 && out_dtype != NVFP4_OUT_BF16) || !stride_ok(ldy, g.N)) return NVFP4_ERR_SHAPE;
+    if (!aligned(Y, out_dtype == NVFP4_OUT_F32 ? 4 : 2)) return NVFP4_ERR_ALIGN;
+    g.y = Y;
+    g.ldy = ldy;
+    std::lock_guard<std::mutex> lk(g_mu);
+    hipStream_t s = static_cast<hipStream_t>(stream);
+    Timed t(s, NVFP4_OP_E4M3_GEMM);
+    return launch_e4m3_gemm(out_dtype == NVFP4_OUT_F32 ? 0 : 1, g, nullptr, s) == hipSuccess ? NVFP4_OK : NVFP4_ERR_LAUNCH;
+}
+
+int nvfp4_e4m3_gemm_gated(const nvfp4_e4m3_tensor *A, const nvfp4_e4m3_tensor *W, int act, nvfp4_e4m3_tensor *out, void *h_bf16, int64_t ld_h,
+                          void *gate_up_bf16, int64_t ld_gate_up, void *workspace, size_t workspace_bytes, void *stream)
+{
+    E4m3GemmArgs g{};
+    if (int rc = fill_e4m3_gemm(A, W, true, &g)) return rc;
+    if (!out && !h_bf16 && !gate_up_bf16) return NVFP4_ERR_NULL;
+    g.fast = (act & NVFP4_SUMS_FAST) != 0;
+    act &= ~NVFP4_SUMS_FAST;
+    if (act != NVFP4_ACT_SILU && act != NVFP4_ACT_GELU_TANH) return NVFP4_ERR_SHAPE;
+    if ((h_bf16 && !stride_ok(ld_h, g.N)) || (gate_up_bf16 && !stride_ok(ld_gate_up, 2 * g.N))) return NVFP4_ERR_SHAPE;
+    if (!aligned(h_bf16, 2) || !aligned(gate_up_bf16, 2)) return NVFP4_ERR_ALIGN;
+    if (out) {
+        if (int rc = check_e4m3_out(out, g.M, g.N, 1)) return rc;
+        g.codes = out->codes;
+        g.scales = out->scales;
+        const size_t need = e4m3_gated_workspace_bytes(g.M, g.N);
+        if (need > 0 && (!workspace || workspace_bytes < need)) return NVFP4_ERR_WORKSPACE;
+        if (need > 0 && !aligned16(workspace)) return NVFP4_ERR_ALIGN;
+    }
+    g.h_bf16 = static_cast<uint16_t *>(h_bf16);
+    g.ld_h = ld_h;
+    g.gate_up = static_cast<uint16_t *>(gate_up_bf16);
+    g.ld_gate_up = ld_gate_up;
+    std::lock_guard<std::mutex> lk(g_mu);
+    hipStream_t s = static_cast<hipStream_t>(stream);
+    Timed t(s, NVFP4_OP_E4M3_GEMM_GATED);
+    return launch_e4m3_gemm(act == NVFP4_ACT_SILU ? 2 : 3, g, workspace, s) == hipSuccess ? NVFP4_OK : NVFP4_ERR_LAUNCH;
+}
+
+int nvfp4_gated_backward(const void *dh_bf16, int64_t ld_dh, const void *gate_up_bf16, int64_t ld_gate_up, int64_t T, int64_t F, int act,
+                         nvfp4_e4m3_tensor *out, nvfp4_e4m3_tensor *out_t, nvfp4_e4m3_tensor *h_t, void *d_bf16, int64_t ld_d, void *stream)
+{
+    if (!out && !out_t && !h_t && !d_bf16) return NVFP4_ERR_NULL;
+    if (T <= 0 || F <= 0 || T > kE4m3MaxK || F > kE4m3MaxK / 2 || (F & 7) != 0 || (out && (F & 127) != 0)) return NVFP4_ERR_SHAPE;
+    if (act != NVFP4_ACT_SILU && act != NVFP4_ACT_GELU_TANH) return NVFP4_ERR_SHAPE;
+    if (int rc = check_matrix(dh_bf16, ld_dh, F)) return rc;
+    if (int rc = check_matrix(gate_up_bf16, ld_gate_up, 2 * F)) return rc;
+    if (out)
+        if (int rc = check_e4m3_out(out, T, 2 * F, 1)) return rc;
+    if (out_t)
+        if (int rc = check_e4m3_out(out_t, 2 * F, up16(T), 1)) return rc;
+    if (h_t)
+        if (int rc = check_e4m3_out(h_t, F, up16(T), 1)) return rc;
+    if (d_bf16)
+        if (int rc = check_matrix(d_bf16, ld_d, 2 * F)) return rc;
+    if (blocks128(T) > kMaxLanes / 512 / blocks128(F)) return NVFP4_ERR_SHAPE;
+    GatedBackwardArgs a{};
+    a.dh = static_cast<const uint16_t *>(dh_bf16);
+    a.ld_dh = ld_dh;
+    a.gate_up = static_cast<const uint16_t *>(gate_up_bf16);
+    a.ld_gate_up = ld_gate_up;
+    a.T = T;
+    a.F = F;
+    a.act = act;
+    a.d_bf16 = static_cast<uint16_t *>(d_bf16);
+    a.ld_d = ld_d;
+    if (out) a.codes = out->codes, a.scales = out->scales;
+    if (out_t) a.codes_t = out_t->codes, a.scales_t = out_t->scales;
+    if (h_t) a.h_codes_t = h_t->codes, a.h_scales_t = h_t->scales;
+    std::lock_guard<std::mutex> lk(g_mu);
+    hipStream_t s = static_cast<hipStream_t>(stream);
+    Timed t(s, NVFP4_OP_GATED_BACKWARD);
+    return launch_gated_backward(a, s) == hipSuccess ? NVFP4_OK : NVFP4_ERR_LAUNCH;
+}
+
+int nvfp4_rms_norm(const void *x_bf16, int64_t ld, const void *residual_bf16, int64_t ld_residual, const void *weight_bf16, int64_t T, int64_t C,
+                   float eps, void *sum_bf16, int64_t ld_sum, nvfp4_e4m3_tensor *out, void *y_bf16, int64_t ld_y, void *stream)
+{
+    if (!weight_bf16 || (!out && !y_bf16)) return NVFP4_ERR_NULL;
+    if (int rc = check_rms_norm(T, C, eps)) return rc;
+    if (int rc = check_matrix(x_bf16, ld, C)) return rc;
+    if ((residual_bf16 != nullptr) != (sum_bf16 != nullptr)) return NVFP4_ERR_NULL;
+    if (residual_bf16) {
+        if (int rc = check_matrix(residual_bf16, ld_residual, C)) return rc;
+        if (int rc = check_matrix(sum_bf16, ld_sum, C)) return rc;
+    }
+    if (y_bf16)
+        if (int rc = check_matrix(y_bf16, ld_y, C)) return rc;
+    if (out)
+        if (int rc = check_e4m3_out(out, T, C, 1)) return rc;
+    if (!aligned16(weight_bf16)) return NVFP4_ERR_ALIGN;
+    RmsNormArgs a{};
+    a.x = static_cast<const uint16_t *>(x_bf16);
+    a.ld = ld;
+    a.residual = static_cast<const uint16_t *>(residual_bf16);
+    a.ld_residual = ld_residual;
+    a.weight = static_cast<const uint16_t *>(weight_bf16);
+    a.T = T;
+    a.C = C;
+    a.sum = static_cast<uint16_t *>(sum_bf16);
+    a.ld_sum = ld_sum;
+    a.y = static_cast<uint16_t *>(y_bf16);
+    a.ld_y = ld_y;
+    if (out) a.codes = out->codes, a.scales = out->scales;
+    a.eps = eps;
+    a.inv_C = 1.0f / (float)C;
+    std::lock_guard<std::mutex> lk(g_mu);
+    hipStream_t s = static_cast<hipStream_t>(stream);
+    Timed t(s, NVFP4_OP_RMS_NORM);
+    return launch_rms_norm(a, s) == hipSuccess ? NVFP4_OK : NVFP4_ERR_LAUNCH;
+}
+
+int nvfp4_rms_norm_backward(const void *dy_bf16, int64_t ld_dy, const void *s_bf16, int64_t ld_s, const void *weight_bf16, const void *dsum_bf16,
+                            int64_t ld_dsum, int64_t T, int64_t C, float eps, void *dx_bf16, int64_t ld_dx, float *dweight, void *workspace,
+                            size_t workspace_bytes, void *stream)
+{
+    if (!weight_bf16) return NVFP4_ERR_NULL;
+    if (int rc = check_rms_norm(T, C, eps)) return rc;
+    if (int rc = check_matrix(dy_bf16, ld_dy, C)) return rc;
+    if (int rc = check_matrix(s_bf16, ld_s, C)) return rc;
+    if (int rc = check_matrix(dx_bf16, ld_dx, C)) return rc;
+    if (dsum_bf16)
+        if (int rc = check_matrix(dsum_bf16, ld_dsum, C)) return rc;
+    if (!aligned16(weight_bf16) || !aligned(dweight, 4)) return NVFP4_ERR_ALIGN;
+    if (dweight) {
+        if (!workspace || workspace_bytes < rms_norm_workspace_bytes(T, C)) return NVFP4_ERR_WORKSPACE;
+        if (!aligned16(workspace)) return NVFP4_ERR_ALIGN;
+    }
+    RmsNormArgs a{};
+    a.x = static_cast<const uint16_t *>(s_bf16);
+    a.ld = ld_s;
+    a.residual = static_cast<const uint16_t *>(dsum_bf16);
+    a.ld_residual = ld_dsum;
+    a.weight = static_cast<const uint16_t *>(weight_bf16);
+    a.dy = static_cast<const uint16_t *>(dy_bf16);
+    a.ld_dy = ld_dy;
+    a.T = T;
+    a.C = C;
+    a.y = static_cast<uint16_t *>(dx_bf16);
+    a.ld_y = ld_dx;
+    a.eps = eps;
+    a.inv_C = 1.0f / (float)C;
+    std::lock_guard<std::mutex> lk(g_mu);
+    hipStream_t s = static_cast<hipStream_t>(stream);
+    Timed t(s, NVFP4_OP_RMS_NORM_BACKWARD);
+    return launch_rms_norm_backward(a, dweight, static_cast<float *>(workspace), s) == hipSuccess ? NVFP4_OK : NVFP4_ERR_LAUNCH;
+}
+
 size_t nvfp4_workspace_bytes(int op, int64_t a, int64_t b, int64_t c)
 {
     switch (op) {
@@ -780,6 +1021,10 @@ size_t nvfp4_workspace_bytes(int op, int64_t a, int64_t b, int64_t c)
         return kPartialBytes + ((a > 0 && b > 0) ? rht_inexact_bytes(a, b) : 0);
     case NVFP4_OP_QK_NORM_ROPE_BACKWARD:   // a = T, b = d
         return a > 0 && b > 0 && b <= NVFP4_HEAD_DIM_MAX ? norm_rope_workspace_bytes(a, b) : 0;
+    case NVFP4_OP_E4M3_GEMM_GATED:         // a = M, b = F
+        return a > 0 && b > 0 && b <= kMaxIndex ? e4m3_gated_workspace_bytes(a, b) : 0;
+    case NVFP4_OP_RMS_NORM_BACKWARD:       // a = T, b = C
+        return a > 0 && b > 0 && b <= kRmsNormMaxC ? rms_norm_workspace_bytes(a, b) : 0;
     case NVFP4_OP_LORA_DOWN:          // a = M, b = K
         if (a <= 0 || b <= 0) return 0;
         return lora_down_workspace_bytes(a, b);

@@ -1,0 +1,109 @@
+// 8-bit operands: E4M3 codes with one E8M0 scale (a power of two) for each 128 elements along the contraction axis.
+#pragma once
+
+#include "nvfp4_device.h"
+
+namespace nvfp4 {
+
+constexpr int kE4m3Block = 128;
+
+typedef int int8v __attribute__((ext_vector_type(8)));
+
+// The scale byte of a block from the bits of its largest magnitude (finite or not): 127 + e for the smallest e >= -127 with
+// amax <= 448 * 2^e.  448 = 1.75 * 2^8, so e is the exponent less 8, and one more where the mantissa is above 1.75: the
+// addition carries exactly then.  A block that holds an infinity or NaN gets 255, the scale that is no number.
+__device__ __forceinline__ uint32_t e8m0_of_amax(uint32_t amax_bits)
+{
+    const int byte = (int)((amax_bits + 0x1FFFFFu) >> 23) - 8;
+    return amax_bits >= 0x7F800000u ? 255u : (uint32_t)max(byte, 0);
+}
+// 2^-(byte - 127), what the block's elements are multiplied by (byte <= 247: a normal number); 255: NaN
+__device__ __forceinline__ float e8m0_inverse(uint32_t byte) { return byte == 255u ? __builtin_nanf("") : __uint_as_float((254u - byte) << 23); }
+
+// four values of at most 448 -> their E4M3 codes, nearest even (NaN: 0x7F with the sign kept)
+__device__ __forceinline__ uint32_t e4m3_pack4(float a, float b, float c, float d)
+{
+    int w = __builtin_amdgcn_cvt_pk_fp8_f32(a, b, 0, false);
+    return (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(c, d, w, true);
+}
+
+__device__ __forceinline__ uint32_t abs_bits(float v) { return __float_as_uint(v) & 0x7FFFFFFFu; }
+
+template <int CTRL>
+__device__ __forceinline__ uint32_t dpp_u32_max(uint32_t v)
+{
+    return max(v, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, CTRL, 0xF, 0xF, true));
+}
+// maximum over the sixteen lanes of a row of lanes; every lane gets it
+__device__ __forceinline__ uint32_t row16_max(uint32_t v)
+{
+    v = dpp_u32_max<0xB1>(v);
+    v = dpp_u32_max<0x4E>(v);
+    v = dpp_u32_max<0x141>(v);
+    return dpp_u32_max<0x140>(v);
+}
+
+__device__ __forceinline__ void unpack8(uint4v v, float (&f)[8])
+{
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        f[2 * i] = bf16lo_to_f32(v[i]);
+        f[2 * i + 1] = bf16hi_to_f32(v[i]);
+    }
+}
+__device__ __forceinline__ uint4v pack8(const float (&f)[8])
+{
+    return uint4v{pack_bf16x2(f[0], f[1]), pack_bf16x2(f[2], f[3]), pack_bf16x2(f[4], f[5]), pack_bf16x2(f[6], f[7])};
+}
+__device__ __forceinline__ uint2v e4m3_pack8(const float (&f)[8], float inv)
+{
+    return uint2v{e4m3_pack4(f[0] * inv, f[1] * inv, f[2] * inv, f[3] * inv), e4m3_pack4(f[4] * inv, f[5] * inv, f[6] * inv, f[7] * inv)};
+}
+// largest magnitude of eight packed bf16, as the bits of an fp32 number
+__device__ __forceinline__ uint32_t absmax8_bits(uint4v v)
+{
+    return pk_hmax_u16(pk_absmax_u16(pk_absmax_u16(pk_absmax_u16(pk_absmax_u16(0u, v.x), v.y), v.z), v.w)) << 16;
+}
+
+// ---- activations of gated layers, in fp32 to about an ulp ---------------------------------------------------------
+constexpr int kActSilu = 2, kActGelu = 1;                       // (NVFP4_ACT_*)
+
+// 1 / (1 + exp(-x)); zero below -87, where it leaves the normal numbers.  The exponent to base two is taken in two parts: one
+// rounded product would cost |x| / 2 ulps.
+__device__ __forceinline__ float sigmoid_f32(float x)
+{
+    constexpr float kLog2e = 1.44269504f, kLog2eLow = 1.92596299e-8f, kLn2 = 0.693147182f;
+    const float y = fminf(-x, 87.0f), t = y * kLog2e, low = __builtin_fmaf(y, kLog2eLow, __builtin_fmaf(y, kLog2e, -t));
+    float e = __builtin_amdgcn_exp2f(t);
+    e = __builtin_fmaf(e * low, kLn2, e);
+    const float d = 1.0f + e, r = __builtin_amdgcn_rcpf(d), s = __builtin_fmaf(r, __builtin_fmaf(-d, r, 1.0f), r);
+    return x < -87.0f ? 0.0f : s;
+}
+// GELU in its tanh form is x sigmoid(z), z = 2 sqrt(2 / pi) (x + 0.044715 x^3).  Beyond 16 the sigmoid is 0 or 1 for good.
+constexpr float kGelu1 = 1.59576912f, kGelu3 = 0.0713548163f;   // z = x (kGelu1 + kGelu3 x^2)
+__device__ __forceinline__ float gelu_within(float x) { return __builtin_amdgcn_fmed3f(x, -16.0f, 16.0f); }
+template <int ACT>
+__device__ __forceinline__ float activation(float x)
+{
+    if constexpr (ACT == kActSilu) return x * sigmoid_f32(x);
+    else {
+        const float c = gelu_within(x);
+        return x * sigmoid_f32(c * __builtin_fmaf(kGelu3, c * c, kGelu1));
+    }
+}
+// act(x), and its derivative: sigmoid + x sigmoid (1 - sigmoid) z'
+template <int ACT>
+__device__ __forceinline__ float activation(float x, float &slope)
+{
+    if constexpr (ACT == kActSilu) {
+        const float s = sigmoid_f32(x);
+        slope = s * __builtin_fmaf(x, 1.0f - s, 1.0f);
+        return x * s;
+    } else {
+        const float c = gelu_within(x), c2 = c * c, s = sigmoid_f32(c * __builtin_fmaf(kGelu3, c2, kGelu1));
+        slope = __builtin_fmaf(c * s, (1.0f - s) * __builtin_fmaf(3.0f * kGelu3, c2, kGelu1), s);
+        return x * s;
+    }
+}
+
+}  // namespace nvfp4

@@ -613,6 +613,250 @@ PyObject *kv_attention(PyObject *const *a)
     });
 }
 
+// ---- 8-bit operands -----------------------------------------------------------------------------------
+// the pair that an E4M3Tensor keeps: codes, scales; or a new one
+struct Bytes8 {
+    nvfp4_e4m3_tensor t{};
+    at::Tensor codes, scales;
+    bool fresh = false;
+    Bytes8() = default;                                               // none
+    Bytes8(const OnDevice &on, PyObject *o)
+    {
+        if (!PyTuple_Check(o) || PyTuple_GET_SIZE(o) != 2) fail(PyExc_TypeError, "expected an E4M3Tensor");
+        codes = on(tensor(PyTuple_GET_ITEM(o, 0)));                   // (shapes, types and strides: checked once, by the E4M3Tensor)
+        scales = on(tensor(PyTuple_GET_ITEM(o, 1)));
+        fill();
+    }
+    // the caller's output, or a new one
+    Bytes8(const OnDevice &on, PyObject *o, int64_t rows, int64_t K, int block_rows)
+    {
+        if (o != Py_None) {
+            *this = Bytes8(on, o);
+            return;
+        }
+        require(rows > 0 && K > 0, "expected a tensor with elements");
+        const auto options = at::TensorOptions().device(on.device);
+        codes = at::empty({rows, K}, options.dtype(at::kFloat8_e4m3fn));
+        scales = at::empty({(rows + block_rows - 1) / block_rows, (K + 127) / 128}, options.dtype(at::kFloat8_e8m0fnu));
+        fresh = true;
+        fill();
+        t.block_rows = block_rows;                                    // (a single row is either)
+    }
+    nvfp4_e4m3_tensor *c() { return t.codes ? &t : nullptr; }
+
+private:
+    void fill()
+    {
+        t.codes = static_cast<uint8_t *>(codes.data_ptr());
+        t.scales = static_cast<uint8_t *>(scales.data_ptr());
+        t.rows = codes.size(0);
+        t.K = codes.size(1);
+        t.block_rows = scales.size(0) == t.rows ? 1 : NVFP4_E4M3_BLOCK;
+    }
+};
+// (status, ...): what is new, None for what is not there or the caller's own
+template <class F>
+PyObject *status_and_new(std::initializer_list<const Bytes8 *> pairs, std::initializer_list<const Output *> outputs, F &&call)
+{
+    PyObject *rc = status(call), *r = rc ? PyTuple_New(1 + 2 * (Py_ssize_t)pairs.size() + (Py_ssize_t)outputs.size()) : nullptr;
+    if (!r) {
+        Py_XDECREF(rc);
+        throw Fail();
+    }
+    PyTuple_SET_ITEM(r, 0, rc);
+    Py_ssize_t i = 1;
+    auto put = [&](const at::Tensor &t, bool fresh) {
+        PyObject *o = Py_None;
+        if (fresh) o = THPVariable_Wrap(t);
+        else Py_INCREF(o);
+        if (!o) throw Fail();
+        PyTuple_SET_ITEM(r, i++, o);
+    };
+    try {
+        for (const Bytes8 *b : pairs) {
+            put(b->codes, b->fresh);
+            put(b->scales, b->fresh);
+        }
+        for (const Output *o : outputs) put(o->t, o->fresh());
+    } catch (...) {
+        Py_DECREF(r);
+        throw;
+    }
+    return r;
+}
+const at::Tensor &matrix_on(const OnDevice &on, PyObject *o) { return on(matrix(o)); }
+int64_t row_stride(const at::Tensor &x) { return x.size(0) > 1 ? x.stride(0) : (x.size(1) + 7) / 8 * 8; }      // (of one row: any)
+// a bf16 output of a call, checked like an input
+void check_output(const Output &o, int64_t rows, int64_t cols)
+{
+    require(o.t.scalar_type() == at::kBFloat16 && o.t.dim() == 2 && o.t.stride(1) == 1 && o.t.size(0) == rows && o.t.size(1) == cols,
+            "expected a bf16 output of the result's shape with unit stride along its rows");
+}
+// (rows of new outputs start on 16-byte boundaries whatever their length: the result is a view of a wider matrix)
+Output wide_output(const OnDevice &on, PyObject *o, int64_t rows, int64_t cols, at::ScalarType type)
+{
+    const int64_t ld = (cols + 7) / 8 * 8;
+    Output r(on, o, {rows, ld}, type);
+    if (r.fresh() && ld != cols) r.t = r.t.slice(1, 0, cols);
+    return r;
+}
+
+PyObject *e4m3_quantize(PyObject *const *a)                         // x, block_axis, out, stream
+{
+    const OnDevice on;
+    const at::Tensor &x = matrix_on(on, a[0]);
+    const int axis = (int)number(a[1]);
+    const int64_t R = x.size(0), C = x.size(1);
+    Bytes8 out(on, a[2], axis == 0 ? R : C, axis == 0 ? C : (R + 15) / 16 * 16, 1);
+    void *s = stream_of(a[3]), *p = x.data_ptr();
+    return status_and_new({&out}, {}, [&] { return nvfp4_e4m3_quantize(p, R, C, row_stride(x), axis, out.c(), s); });
+}
+PyObject *e4m3_quantize_2d(PyObject *const *a)                      // w, transposed, out, out_t, stream
+{
+    const OnDevice on;
+    const at::Tensor &x = matrix_on(on, a[0]);
+    const int64_t R = x.size(0), C = x.size(1);
+    Bytes8 out(on, a[2], R, C, NVFP4_E4M3_BLOCK), out_t;
+    if (number(a[1]) || a[3] != Py_None) out_t = Bytes8(on, a[3], C, R, NVFP4_E4M3_BLOCK);
+    void *s = stream_of(a[4]), *p = x.data_ptr();
+    return status_and_new({&out, &out_t}, {}, [&] { return nvfp4_e4m3_quantize_2d(p, R, C, row_stride(x), out.c(), out_t.c(), s); });
+}
+PyObject *e4m3_gemm(PyObject *const *a)                             // A, W, out_dtype, Y, fast_sums, stream
+{
+    const OnDevice on;
+    Bytes8 A(on, a[0]), W(on, a[1]);
+    const int dtype = (int)number(a[2]);
+    const at::ScalarType type = dtype == NVFP4_OUT_F32 ? at::kFloat : at::kBFloat16;
+    const Output y = wide_output(on, a[3], A.t.rows, W.t.rows, type);
+    require(y.t.scalar_type() == type && y.t.dim() == 2 && y.t.size(0) == A.t.rows && y.t.size(1) == W.t.rows && (y.t.stride(1) == 1 || y.t.size(1) == 1),
+            "expected an output [M, N] of the chosen type with unit stride along its rows");
+    const int sums = number(a[4]) ? NVFP4_SUMS_FAST : 0;
+    void *s = stream_of(a[5]), *p = y.t.data_ptr();
+    return status_and_new({}, {&y}, [&] { return nvfp4_e4m3_gemm(A.c(), W.c(), p, row_stride(y.t), dtype | sums, s); });
+}
+// A, W, act, quantize, keep_h, keep_gate_up, out, h, gate_up, workspace, fast_sums, stream
+PyObject *e4m3_gemm_gated(PyObject *const *a)
+{
+    const OnDevice on;
+    Bytes8 A(on, a[0]), W(on, a[1]), out;
+    const int act = (int)number(a[2]) | (number(a[10]) ? NVFP4_SUMS_FAST : 0);
+    const int64_t M = A.t.rows, F = W.t.rows / 2;
+    if (number(a[3]) || a[6] != Py_None) out = Bytes8(on, a[6], M, F, 1);
+    Output h, gate_up;
+    void *ph = nullptr, *pg = nullptr;
+    int64_t ldh = 0, ldg = 0;
+    if (number(a[4]) || a[7] != Py_None) {
+        h = wide_output(on, a[7], M, F, at::kBFloat16);
+        check_output(h, M, F);
+        ph = h.t.data_ptr();
+        ldh = row_stride(h.t);
+    }
+    if (number(a[5]) || a[8] != Py_None) {
+        gate_up = wide_output(on, a[8], M, 2 * F, at::kBFloat16);
+        check_output(gate_up, M, 2 * F);
+        pg = gate_up.t.data_ptr();
+        ldg = row_stride(gate_up.t);
+    }
+    at::Tensor ws;
+    if (a[9] != Py_None) ws = workspace_of(on, a[9]);
+    else if (out.c())
+        if (const size_t n = nvfp4_workspace_bytes(NVFP4_OP_E4M3_GEMM_GATED, M, F, 0)) ws = bytes_on(on.device, (int64_t)n);
+    void *s = stream_of(a[11]), *w = ws.defined() ? ws.data_ptr() : nullptr;
+    const size_t n = ws.defined() ? (size_t)ws.nbytes() : 0;
+    return status_and_new({&out}, {&h, &gate_up}, [&] { return nvfp4_e4m3_gemm_gated(A.c(), W.c(), act, out.c(), ph, ldh, pg, ldg, w, n, s); });
+}
+// dh, gate_up, act, quantize, recompute_h, keep_bf16, out, out_t, h_t, d, stream
+PyObject *gated_backward(PyObject *const *a)
+{
+    const OnDevice on;
+    const at::Tensor &dh = matrix_on(on, a[0]), &gate_up = matrix_on(on, a[1]);
+    const int act = (int)number(a[2]);
+    const int64_t T = dh.size(0), F = dh.size(1), T16 = (T + 15) / 16 * 16;
+    require(gate_up.size(0) == T && gate_up.size(1) == 2 * F, "expected gate and up values [T, 2F] for gradients [T, F]");
+    Bytes8 out, out_t, h_t;
+    const bool quantize = number(a[3]) != 0;
+    if (quantize || a[6] != Py_None) out = Bytes8(on, a[6], T, 2 * F, 1);
+    if (quantize || a[7] != Py_None) out_t = Bytes8(on, a[7], 2 * F, T16, 1);
+    if (number(a[4]) || a[8] != Py_None) h_t = Bytes8(on, a[8], F, T16, 1);
+    Output d;
+    void *pd = nullptr;
+    int64_t ldd = 0;
+    if (number(a[5]) || a[9] != Py_None) {
+        d = Output(on, a[9], {T, 2 * F}, at::kBFloat16);
+        check_output(d, T, 2 * F);
+        pd = d.t.data_ptr();
+        ldd = row_stride(d.t);
+    }
+    void *s = stream_of(a[10]), *px = dh.data_ptr(), *pg = gate_up.data_ptr();
+    return status_and_new({&out, &out_t, &h_t}, {&d}, [&] {
+        return nvfp4_gated_backward(px, row_stride(dh), pg, row_stride(gate_up), T, F, act, out.c(), out_t.c(), h_t.c(), pd, ldd, s);
+    });
+}
+// x, weight, residual, eps, quantize, keep_bf16, out, y, sum, stream
+PyObject *rms_norm(PyObject *const *a)
+{
+    const OnDevice on;
+    const at::Tensor &x = matrix_on(on, a[0]);
+    const int64_t T = x.size(0), C = x.size(1);
+    const at::Tensor &w = weight_of(on, a[1], C);
+    const float eps = (float)real(a[3]);
+    Bytes8 out;
+    if (number(a[4]) || a[6] != Py_None) out = Bytes8(on, a[6], T, C, 1);
+    Output y, sum;
+    void *py = nullptr, *ps = nullptr, *pr = nullptr;
+    int64_t ldy = 0, lds = 0, ldr = 0;
+    if (number(a[5]) || a[7] != Py_None) {
+        y = Output(on, a[7], {T, C}, at::kBFloat16);
+        check_output(y, T, C);
+        py = y.t.data_ptr();
+        ldy = row_stride(y.t);
+    }
+    if (a[2] != Py_None) {
+        const at::Tensor &r = matrix_on(on, a[2]);
+        require(r.sizes() == x.sizes(), "expected a residual of the input's shape");
+        pr = r.data_ptr();
+        ldr = row_stride(r);
+        sum = Output(on, a[8], {T, C}, at::kBFloat16);
+        check_output(sum, T, C);
+        ps = sum.t.data_ptr();
+        lds = row_stride(sum.t);
+    } else require(a[8] == Py_None, "a sum needs a residual");
+    void *s = stream_of(a[9]), *px = x.data_ptr(), *pw = w.data_ptr();
+    return status_and_new({&out}, {&y, &sum}, [&] { return nvfp4_rms_norm(px, row_stride(x), pr, ldr, pw, T, C, eps, ps, lds, out.c(), py, ldy, s); });
+}
+// dy, s, weight, dsum, eps, weight_grad, dx, dweight, workspace, stream
+PyObject *rms_norm_backward(PyObject *const *a)
+{
+    const OnDevice on;
+    const at::Tensor &dy = matrix_on(on, a[0]), &x = matrix_on(on, a[1]);
+    const int64_t T = dy.size(0), C = dy.size(1);
+    require(x.sizes() == dy.sizes(), "a gradient has its input's shape");
+    const at::Tensor &w = weight_of(on, a[2], C);
+    void *pr = nullptr;
+    int64_t ldr = 0;
+    if (a[3] != Py_None) {
+        const at::Tensor &r = matrix_on(on, a[3]);
+        require(r.sizes() == dy.sizes(), "a gradient has its input's shape");
+        pr = r.data_ptr();
+        ldr = row_stride(r);
+    }
+    const float eps = (float)real(a[4]);
+    Output dx(on, a[6], {T, C}, at::kBFloat16), dweight;
+    check_output(dx, T, C);
+    if (number(a[5]) || a[7] != Py_None) {
+        dweight = Output(on, a[7], {C}, at::kFloat);
+        require(dweight.t.scalar_type() == at::kFloat && dweight.t.dim() == 1 && dweight.t.is_contiguous() && dweight.t.size(0) == C,
+                "expected a contiguous fp32 weight gradient [C]");
+    }
+    at::Tensor ws;
+    if (a[8] != Py_None) ws = workspace_of(on, a[8]);
+    else if (dweight.t.defined()) ws = bytes_on(on.device, std::max<int64_t>(16, (int64_t)nvfp4_workspace_bytes(NVFP4_OP_RMS_NORM_BACKWARD, T, C, 0)));
+    void *s = stream_of(a[9]), *w_ = ws.defined() ? ws.data_ptr() : nullptr, *pd = dy.data_ptr(), *px = x.data_ptr(), *pw = w.data_ptr(), *po = dx.t.data_ptr();
+    float *dw = dweight.t.defined() ? static_cast<float *>(dweight.t.data_ptr()) : nullptr;
+    const size_t n = ws.defined() ? (size_t)ws.nbytes() : 0;
+    return status_and_new({}, {&dx, &dweight}, [&] { return nvfp4_rms_norm_backward(pd, row_stride(dy), px, row_stride(x), pw, pr, ldr, T, C, eps, po, row_stride(dx.t), dw, w_, n, s); });
+}
+
 // one Python function: fixed number of positional arguments, C++ and torch exceptions turned into Python's
 template <PyObject *(*F)(PyObject *const *), int N>
 PyObject *entry(PyObject *, PyObject *const *args, Py_ssize_t n)
@@ -648,7 +892,10 @@ extern "C" PyObject *PyInit__host(void)
         method<gemm_scale_out, 6>("gemm_scale_out"), method<lora_down, 5>("lora_down"), method<gemm_lora, 8>("gemm_lora"),
         method<gemm_act_quant, 8>("gemm_act_quant"), method<qk_norm_rope, 9>("qk_norm_rope"),
         method<qk_norm_rope_backward, 15>("qk_norm_rope_backward"), method<kv_cache_write, 6>("kv_cache_write"),
-        method<kv_cache_read, 5>("kv_cache_read"), method<kv_attention, 15>("kv_attention"), {nullptr, nullptr, 0, nullptr}};
+        method<kv_cache_read, 5>("kv_cache_read"), method<kv_attention, 15>("kv_attention"),
+        method<e4m3_quantize, 4>("e4m3_quantize"), method<e4m3_quantize_2d, 5>("e4m3_quantize_2d"), method<e4m3_gemm, 6>("e4m3_gemm"),
+        method<e4m3_gemm_gated, 12>("e4m3_gemm_gated"), method<gated_backward, 11>("gated_backward"), method<rms_norm, 10>("rms_norm"),
+        method<rms_norm_backward, 10>("rms_norm_backward"), {nullptr, nullptr, 0, nullptr}};
     static PyModuleDef module = {PyModuleDef_HEAD_INIT, "_host", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
     s_codes = PyUnicode_InternFromString("codes");
     s_scales = PyUnicode_InternFromString("scales");

@@ -165,4 +165,54 @@ int gemm_workgroups(int64_t M, int64_t N, int64_t K);
 int gemm_plan_text(int64_t M, int64_t N, int64_t K, char *text, size_t text_bytes);
 bool gemm_is_tiled(int64_t M, int64_t N, int64_t K);   // false: the 64x64 tile alone (no re-quantizing or LoRA epilogue)
 
+// ---- 8-bit operands: E4M3 codes [rows, K], E8M0 scales for 128 elements along K (rows) or for 128 x 128 (tiles)
+hipError_t launch_e4m3_rows(const uint16_t *x, int64_t R, int64_t C, int64_t ld, uint8_t *codes, uint8_t *scales, hipStream_t s);
+// the transpose [C, R rounded up to 16], blocks along R
+hipError_t launch_e4m3_columns(const uint16_t *x, int64_t R, int64_t C, int64_t ld, uint8_t *codes, uint8_t *scales, hipStream_t s);
+// R % 16 == 0; codes_t, scales_t: the transpose, or nullptr
+hipError_t launch_e4m3_tiles(const uint16_t *x, int64_t R, int64_t C, int64_t ld, uint8_t *codes, uint8_t *scales, uint8_t *codes_t, uint8_t *scales_t, hipStream_t s);
+
+struct E4m3GemmArgs {
+    const uint8_t *codes_a, *scales_a, *codes_w, *scales_w;
+    int64_t M, N, K;                       // gated: N columns of the result, W has 2 N rows (gate, then up)
+    bool w_tiles;                          // W: a scale for 128 x 128
+    bool scale_words;                      // rows of scales are whole words
+    bool fast;                             // fast sums (more than 64 rows; fewer are bound by memory and take exact ones)
+    void *y;                               // [M, N] fp32 or bf16 (not gated)
+    int64_t ldy;
+    uint16_t *gate_up, *h_bf16;            // gated: bf16 [M, 2 N] and [M, N], or nullptr
+    int64_t ld_gate_up, ld_h;
+    uint8_t *codes, *scales;               // gated: the result in 8 bits [M, N], or nullptr
+    int tiles_m, tiles_n;                  // filled in by the launchers
+};
+// kind: 0 fp32, 1 bf16; gated: 2 SiLU, 3 GELU.  workspace: gated with few rows, e4m3_gated_workspace_bytes
+hipError_t launch_e4m3_gemm(int kind, const E4m3GemmArgs &g, void *workspace, hipStream_t s);
+size_t e4m3_gated_workspace_bytes(int64_t M, int64_t F);
+
+struct GatedBackwardArgs {
+    const uint16_t *dh, *gate_up;          // [T, F], [T, 2 F]
+    int64_t ld_dh, ld_gate_up, T, F;
+    int act;                               // NVFP4_ACT_*
+    uint16_t *d_bf16;                      // [T, 2 F], or nullptr (each of these)
+    int64_t ld_d;
+    uint8_t *codes, *scales;               // [T, 2 F] along the features
+    uint8_t *codes_t, *scales_t;           // [2 F, T rounded up to 16] along the tokens
+    uint8_t *h_codes_t, *h_scales_t;       // h: [F, T rounded up to 16] along the tokens
+};
+hipError_t launch_gated_backward(const GatedBackwardArgs &a, hipStream_t s);
+
+struct RmsNormArgs {
+    const uint16_t *x, *residual, *weight; // backward: x is the sum, residual the gradient of the sum that comes from elsewhere
+    const uint16_t *dy;                    // backward
+    int64_t ld, ld_residual, ld_dy, T, C;
+    uint16_t *sum, *y;                     // backward: y is dx
+    int64_t ld_sum, ld_y;
+    uint8_t *codes, *scales;
+    float eps, inv_C;
+};
+constexpr int64_t kRmsNormMaxC = 16384;
+hipError_t launch_rms_norm(const RmsNormArgs &a, hipStream_t s);
+size_t rms_norm_workspace_bytes(int64_t T, int64_t C);
+hipError_t launch_rms_norm_backward(const RmsNormArgs &a, float *dweight, float *partial, hipStream_t s);
+
 }  // namespace nvfp4

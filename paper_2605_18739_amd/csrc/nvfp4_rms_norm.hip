@@ -1,0 +1,270 @@
+// RMS norm of the residual stream with the residual's addition and an 8-bit output, and its gradient, for gfx950.
+// Streaming kernels bound by HBM: forward 2 B (with a residual 4 B) read and 1 B (with the sum 3 B, with bf16 2 B more) written
+// per element, backward 4 B (with the stream's gradient 6 B) read and 2 B written.
+#include "nvfp4_e4m3.h"
+
+#include <algorithm>
+#include <type_traits>
+
+#include "nvfp4_kernels.h"
+
+namespace nvfp4 {
+
+// Sums over the workgroup of up to sixteen waves; every lane gets them, added in the same order everywhere.
+template <int WAVES, int N>
+__device__ __forceinline__ void group_sum(float (&v)[N], float (*part)[N])
+{
+    const int wave = threadIdx.x >> 6;
+#pragma unroll
+    for (int k = 0; k < N; ++k) {
+        v[k] += dpp_f32<0xB1>(v[k]);
+        v[k] += dpp_f32<0x4E>(v[k]);
+        v[k] += dpp_f32<0x141>(v[k]);
+        v[k] += dpp_f32<0x140>(v[k]);
+        v[k] += __shfl_xor(v[k], 16, 64);
+        v[k] += __shfl_xor(v[k], 32, 64);
+    }
+    if constexpr (WAVES > 1) {
+        if ((threadIdx.x & 63) == 0) {
+#pragma unroll
+            for (int k = 0; k < N; ++k) part[wave][k] = v[k];
+        }
+        __syncthreads();
+#pragma unroll
+        for (int k = 0; k < N; ++k) {
+            v[k] = part[0][k];
+#pragma unroll
+            for (int w = 1; w < WAVES; ++w) v[k] += part[w][k];
+        }
+    }
+}
+
+// 1 / sqrt(v), the hardware's approximation (1 ulp) and one Newton step: y correct to about half an ulp
+__device__ __forceinline__ float inverse_root(float v)
+{
+    const float y = __builtin_amdgcn_rsqf(v), e = __builtin_fmaf(-v * y, y, 1.0f);
+    return __builtin_fmaf(0.5f * y, e, y);
+}
+
+// A workgroup takes a row, or with one wave a workgroup's worth of waves a row each; lane t of a row's holds elements
+// 8 (t + L j) .. + 7, L the lanes of the row, so that sixteen lanes hold a block of 128.
+template <int WAVES, int CH>
+__global__ __launch_bounds__(WAVES == 1 ? 256 : 64 * WAVES) void rms_norm_kernel(const RmsNormArgs a)
+{
+    constexpr int L = 64 * WAVES;
+    __shared__ float part[WAVES][1];
+    const int t = WAVES == 1 ? threadIdx.x & 63 : threadIdx.x;
+    const int64_t row = WAVES == 1 ? (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6) : blockIdx.x;
+    if (WAVES == 1 && row >= a.T) return;
+    uint4v x[CH], r[CH], w[CH];
+#pragma unroll
+    for (int j = 0; j < CH; ++j) {
+        const int e = 8 * (t + L * j);
+        x[j] = r[j] = w[j] = uint4v{0u, 0u, 0u, 0u};
+        if (e < a.C) {
+            x[j] = *(const uint4v *)(a.x + row * a.ld + e);
+            if (a.residual) r[j] = *(const uint4v *)(a.residual + row * a.ld_residual + e);
+            w[j] = *(const uint4v *)(a.weight + e);
+        }
+    }
+    float s[1] = {0.0f};
+#pragma unroll
+    for (int j = 0; j < CH; ++j) {
+        float f[8];
+        unpack8(x[j], f);
+        if (a.residual) {                                            // the sum is rounded: it is what the later layers read
+            float g[8];
+            unpack8(r[j], g);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) f[i] += g[i];
+            x[j] = pack8(f);
+            const int e = 8 * (t + L * j);
+            if (e < a.C) *(uint4v *)(a.sum + row * a.ld_sum + e) = x[j];
+            unpack8(x[j], f);
+        }
+#pragma unroll
+        for (int i = 0; i < 8; ++i) s[0] = __builtin_fmaf(f[i], f[i], s[0]);
+    }
+    group_sum<WAVES>(s, part);
+    const float rms = inverse_root(__builtin_fmaf(s[0], a.inv_C, a.eps));
+#pragma unroll
+    for (int j = 0; j < CH; ++j) {
+        const int e = 8 * (t + L * j);
+        float f[8], g[8];
+        unpack8(x[j], f);
+        unpack8(w[j], g);
+        uint32_t top = 0u;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            f[i] = f[i] * rms * g[i];
+            top = max(top, abs_bits(f[i]));
+        }
+        if (a.y && e < a.C) *(uint4v *)(a.y + row * a.ld_y + e) = pack8(f);
+        if (a.codes) {
+            const uint32_t byte = e8m0_of_amax(row16_max(top));
+            const uint2v c = e4m3_pack8(f, e8m0_inverse(byte));
+            if (e < a.C) {
+                *(uint2v *)(a.codes + row * a.C + e) = c;
+                if ((t & 15) == 0) a.scales[row * ((a.C + 127) >> 7) + (e >> 7)] = (uint8_t)byte;
+            }
+        }
+    }
+}
+
+// Backward: dx = dsum + r (w dy - xh mean(w dy xh)), xh = r x, and the workgroup's part of dweight = sum over rows of dy xh,
+// which it keeps in registers over all of its rows: partial[workgroup][C].
+// Rows that one wave holds go four to a workgroup, whose waves add up their parts at the end.
+template <int WAVES, int CH>
+__global__ __launch_bounds__(WAVES == 1 ? 256 : 64 * WAVES) void rms_norm_backward_kernel(const RmsNormArgs a, float *__restrict__ partial)
+{
+    constexpr int L = 64 * WAVES, ROWS = WAVES == 1 ? 4 : 1;
+    __shared__ float part[2][WAVES][2];
+    __shared__ float waves_dw[WAVES == 1 ? ROWS : 1][WAVES == 1 ? CH * 512 : 1];
+    const int t = WAVES == 1 ? threadIdx.x & 63 : threadIdx.x, own = WAVES == 1 ? threadIdx.x >> 6 : 0;
+    uint4v w[CH];
+    float dw[CH][8];
+#pragma unroll
+    for (int j = 0; j < CH; ++j) {
+        const int e = 8 * (t + L * j);
+        w[j] = uint4v{0u, 0u, 0u, 0u};
+        if (e < a.C) w[j] = *(const uint4v *)(a.weight + e);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) dw[j][i] = 0.0f;
+    }
+    uint4v x[CH], d[CH], r[CH];
+    auto fetch = [&](int64_t row) {
+#pragma unroll
+        for (int j = 0; j < CH; ++j) {
+            const int e = 8 * (t + L * j);
+            x[j] = d[j] = r[j] = uint4v{0u, 0u, 0u, 0u};
+            if (e < a.C) {
+                x[j] = *(const uint4v *)(a.x + row * a.ld + e);
+                d[j] = *(const uint4v *)(a.dy + row * a.ld_dy + e);
+                if (a.residual) r[j] = *(const uint4v *)(a.residual + row * a.ld_residual + e);
+            }
+        }
+    };
+    int turn = 0;
+    for (int64_t row = (int64_t)blockIdx.x * ROWS + own; row < a.T; row += (int64_t)gridDim.x * ROWS, turn ^= 1) {
+        fetch(row);
+        float s[2] = {0.0f, 0.0f};
+#pragma unroll
+        for (int j = 0; j < CH; ++j) {
+            float f[8], g[8], h[8];
+            unpack8(x[j], f);
+            unpack8(d[j], g);
+            unpack8(w[j], h);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                s[0] = __builtin_fmaf(f[i], f[i], s[0]);
+                s[1] = __builtin_fmaf(g[i] * h[i], f[i], s[1]);
+            }
+        }
+        group_sum<WAVES>(s, part[turn]);                             // (two places in turn: one barrier a row)
+        const float rms = inverse_root(__builtin_fmaf(s[0], a.inv_C, a.eps)), mean = s[1] * a.inv_C * rms * rms;
+#pragma unroll
+        for (int j = 0; j < CH; ++j) {
+            const int e = 8 * (t + L * j);
+            float f[8], g[8], h[8], o[8];
+            unpack8(x[j], f);
+            unpack8(d[j], g);
+            unpack8(w[j], h);
+            unpack8(r[j], o);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                dw[j][i] = __builtin_fmaf(g[i], f[i] * rms, dw[j][i]);
+                o[i] = __builtin_fmaf(rms, __builtin_fmaf(-f[i], mean, g[i] * h[i]), o[i]);
+            }
+            if (e < a.C) *(uint4v *)(a.y + row * a.ld_y + e) = pack8(o);
+        }
+    }
+    if (!partial) return;
+    if constexpr (WAVES == 1) {
+#pragma unroll
+        for (int j = 0; j < CH; ++j)
+#pragma unroll
+            for (int i = 0; i < 8; ++i) waves_dw[own][(j * 8 + i) * 64 + t] = dw[j][i];
+        __syncthreads();
+        if (own > 0) return;
+#pragma unroll
+        for (int j = 0; j < CH; ++j)
+#pragma unroll
+            for (int i = 0; i < 8; ++i)
+#pragma unroll
+                for (int k = 1; k < ROWS; ++k) dw[j][i] += waves_dw[k][(j * 8 + i) * 64 + t];
+    }
+#pragma unroll
+    for (int j = 0; j < CH; ++j) {
+        const int e = 8 * (t + L * j);
+        if (e < a.C) {
+            *(float4v *)(partial + (int64_t)blockIdx.x * a.C + e) = float4v{dw[j][0], dw[j][1], dw[j][2], dw[j][3]};
+            *(float4v *)(partial + (int64_t)blockIdx.x * a.C + e + 4) = float4v{dw[j][4], dw[j][5], dw[j][6], dw[j][7]};
+        }
+    }
+}
+
+// dweight = the partial sums added in a fixed order: sixteen columns a workgroup, 64 strided parts of each
+__global__ __launch_bounds__(1024) void rms_norm_weight_kernel(const float *__restrict__ partial, int n, int C, float *__restrict__ dweight)
+{
+    __shared__ float part[64][17];
+    const int c = blockIdx.x * 16 + (threadIdx.x & 15), row = threadIdx.x >> 4;
+    float v[8];
+#pragma unroll
+    for (int k = 0; k < 8; ++k) v[k] = 0.0f;
+    for (int i = row; i < n; i += 8 * 64)
+#pragma unroll
+        for (int k = 0; k < 8; ++k)
+            if (i + k * 64 < n) v[k] += partial[(int64_t)(i + k * 64) * C + c];
+    part[row][threadIdx.x & 15] = ((v[0] + v[1]) + (v[2] + v[3])) + ((v[4] + v[5]) + (v[6] + v[7]));
+    __syncthreads();
+    if (threadIdx.x < 16) {
+        float sum = 0.0f;
+#pragma unroll
+        for (int i = 0; i < 64; ++i) sum += part[i][threadIdx.x];
+        dweight[c] = sum;
+    }
+}
+
+// --------------------------------------------------------------------------
+constexpr int kBackwardGrid = 1024;
+
+size_t rms_norm_workspace_bytes(int64_t T, int64_t C) { return (size_t)std::min<int64_t>(T, kBackwardGrid) * (size_t)C * sizeof(float); }
+
+// (waves of a row, chunks of eight elements a lane)
+template <class F>
+static void of_row(int64_t C, F &&f)
+{
+    using std::integral_constant;
+    if (C <= 512) f(integral_constant<int, 1>(), integral_constant<int, 1>());
+    else if (C <= 1024) f(integral_constant<int, 1>(), integral_constant<int, 2>());
+    else if (C <= 2048) f(integral_constant<int, 4>(), integral_constant<int, 1>());
+    else if (C <= 4096) f(integral_constant<int, 4>(), integral_constant<int, 2>());
+    else if (C <= 6144) f(integral_constant<int, 4>(), integral_constant<int, 3>());
+    else if (C <= 8192) f(integral_constant<int, 4>(), integral_constant<int, 4>());
+    else f(integral_constant<int, 8>(), integral_constant<int, 4>());
+}
+
+hipError_t launch_rms_norm(const RmsNormArgs &a, hipStream_t s)
+{
+    of_row(a.C, [&](auto waves, auto chunks) {
+        constexpr int W = decltype(waves)::value, CH = decltype(chunks)::value;
+        rms_norm_kernel<W, CH><<<(unsigned)(W == 1 ? (a.T + 3) / 4 : a.T), W == 1 ? 256 : 64 * W, 0, s>>>(a);
+    });
+    return hipGetLastError();
+}
+
+hipError_t launch_rms_norm_backward(const RmsNormArgs &a, float *dweight, float *partial, hipStream_t s)
+{
+    int grid = 0;
+    of_row(a.C, [&](auto waves, auto chunks) {
+        constexpr int W = decltype(waves)::value, CH = decltype(chunks)::value, ROWS = W == 1 ? 4 : 1;
+        grid = (int)std::min<int64_t>((a.T + ROWS - 1) / ROWS, kBackwardGrid);
+        rms_norm_backward_kernel<W, CH><<<(unsigned)grid, W == 1 ? 256 : 64 * W, 0, s>>>(a, dweight ? partial : nullptr);
+    });
+    if (hipError_t e = hipGetLastError()) return e;
+    if (!dweight) return hipSuccess;
+    rms_norm_weight_kernel<<<(unsigned)(a.C / 16), 1024, 0, s>>>(partial, grid, (int)a.C, dweight);
+    return hipGetLastError();
+}
+
+}  // namespace nvfp4
