@@ -267,6 +267,8 @@ int fill_e4m3_gemm(const nvfp4_e4m3_tensor *A, const nvfp4_e4m3_tensor *W, bool 
     g->scales_a = A->scales;
     g->codes_w = W->codes;
     g->scales_w = W->scales;
+    g->scales_a_bytes = M * nb;
+    g->scales_w_bytes = (W->block_rows == 1 ? W->rows : blocks128(W->rows)) * nb;
     g->M = M;
     g->N = N;
     g->K = A->K;

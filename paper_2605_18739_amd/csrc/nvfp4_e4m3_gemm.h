@@ -21,18 +21,19 @@ namespace nvfp4 {
 enum { kE4m3F32 = 0, kE4m3Bf16 = 1, kE4m3Silu = 2, kE4m3Gelu = 3 };
 
 // One tile of BM x BN outputs (gated: BM x BN / 2, the W rows are BN / 2 of the gate and as many of the up projection), four
-// waves of BM / 2 x BN / 2.  A step is 128 k: 128 bytes of every row, in two stages of LDS filled by copies that write LDS
+// waves of BM / 2 x BN / 2.  A step is 128 k: 128 bytes of every row, in STAGES stages of LDS filled by copies that write LDS
 // directly.  LDS: chunk c (16 bytes) of row r stands at 128 r + 16 (c ^ ((r >> 1) & 7)), so that sixteen rows of one chunk,
 // what sixteen lanes read at once, fall on distinct banks; the copies fetch the chunks in that order.
 //
 // Schedule of a step s with fast sums, fragments of its two halves (64 k each) in registers F0 and F1:
-//   first half    multiplies F0, reads F1 from stage s & 1
-//   then          waits for the own copies of step s + 1 and the reads, joins a barrier: stage s & 1 is free, step s + 1 is in
-//   second half   multiplies F1, starts the copies of step s + 2 into stage s & 1, reads F0 of step s + 1
-// One barrier a step; a copy has a whole step to arrive, a read half a step.
+//   first half    multiplies F0, reads F1 from stage s % STAGES
+//   then          waits for the own copies of step s + 1 and the reads, joins a barrier: stage s % STAGES is free, step s + 1 is in
+//   second half   multiplies F1, starts the copies of step s + STAGES into that stage, reads F0 of step s + 1
+// One barrier a step; a copy has STAGES - 1 steps to arrive, a read half a step.
 // With exact sums a step is four phases of two sub-steps (16 k each): a phase reads the next one's codes, a sub-step expands the
 // next one's operands between its matrix instructions, the barrier and the copies stand in front of and in the last phase.
-template <int BM, int BN, int KIND, bool FAST>
+// (Rows of 64 bytes in four slots, with a barrier every 64 k and three half steps for a copy, took 2 to 6 % longer on large products.)
+template <int BM, int BN, int KIND, bool FAST, int STAGES>
 __global__ __launch_bounds__(256) void e4m3_gemm_kernel(const E4m3GemmArgs g)
 {
 #if defined(__HIP_DEVICE_COMPILE__)
@@ -76,9 +77,9 @@ __global__ __launch_bounds__(256) void e4m3_gemm_kernel(const E4m3GemmArgs g)
 #pragma unroll
         for (int p = 0; p < 2; ++p) from[p] = chunk_at[p] < left ? row_at + chunk_at[p] + s * 128 : kPast;
     };
-    auto copy = [&](int to, auto x_c) {
+    auto copy = [&](int s, auto x_c) {
         constexpr int x = decltype(x_c)::value;
-        uint8_t *stage = lds + to;
+        uint8_t *stage = lds + s % STAGES * STAGE;
         if constexpr (x < UA) {
             const int u = wave * UA + x;
             __builtin_amdgcn_raw_ptr_buffer_load_lds(ra, (lds_ptr_t)(stage + u * 1024), 16, from[x & 1] + u * 8 * K, 0, 0, 0);
@@ -104,7 +105,7 @@ __global__ __launch_bounds__(256) void e4m3_gemm_kernel(const E4m3GemmArgs g)
     int frag_at[4];                                        // 16-byte chunks 2 c + half of the lane's row
 #pragma unroll
     for (int c = 0; c < 4; ++c) frag_at[c] = lrow * 128 + (((2 * c + lhalf) ^ ((lrow >> 1) & 7)) << 4);
-    auto read_chunk = [&](int from_stage, int c, int f) { return *(const uint4v *)(lds + from_stage + frag_row0(f) * 128 + frag_at[c]); };
+    auto read_chunk = [&](int s, int c, int f) { return *(const uint4v *)(lds + s % STAGES * STAGE + frag_row0(f) * 128 + frag_at[c]); };
 
     // ---- scales: a word holds those of four steps of a fragment's row
     const int nb = S;
@@ -124,16 +125,23 @@ __global__ __launch_bounds__(256) void e4m3_gemm_kernel(const E4m3GemmArgs g)
             scale_at[f] = (int)((g.w_tiles ? n >> 7 : n) - w_first) * nb;
         }
     }
-    auto load_scales = [&](int group) {                    // of steps 4 group .. + 3
+    auto load_scales = [&](int group) {                    // of steps 4 group .. + 3; bytes behind the row's last become 0
+        const uint32_t mine = 4 * group + 4 > nb ? (1u << 8 * (nb - 4 * group)) - 1u : 0xFFFFFFFFu;
 #pragma unroll
         for (int f = 0; f < NF; ++f) {
             const uint8_t *p = (f < TM ? scales_a : scales_w) + scale_at[f];
             if (g.scale_words) next_scale[f] = *(const uint32_t *)(p + 4 * group);
-            else {
-                uint32_t w = 0u;
-#pragma unroll
-                for (int b = 0; b < 4; ++b) w |= (uint32_t)p[min(4 * group + b, nb - 1)] << 8 * b;
-                next_scale[f] = w;
+            else {                                         // at any address; one that would end behind the array is moved back to its last word
+                typedef uint32_t any_word __attribute__((aligned(1)));
+                const int64_t bytes = f < TM ? g.scales_a_bytes : g.scales_w_bytes, left = bytes - (p - (f < TM ? g.scales_a : g.scales_w));
+                if (bytes >= 4) {
+                    const int at = (int)min((int64_t)(4 * group), left - 4);
+                    next_scale[f] = *(const any_word *)(p + at) >> 8 * (4 * group - at) & mine;
+                } else {                                   // (a single group)
+                    uint32_t w = 0u;
+                    for (int b = 0; b < nb; ++b) w |= (uint32_t)p[b] << 8 * b;
+                    next_scale[f] = w;
+                }
             }
         }
     };
@@ -146,33 +154,30 @@ __global__ __launch_bounds__(256) void e4m3_gemm_kernel(const E4m3GemmArgs g)
 #pragma unroll
             for (int r = 0; r < 16; ++r) acc[i][j][r] = 0.0f;
 
-    auto wait_and_join = [&] {
+    // all but the last N copies have arrived, all reads are back
+    auto wait_and_join = [&](auto n_c) {
+        constexpr int n = decltype(n_c)::value;
+        static_assert(n < 64, "vmcnt");
         NVFP4_COMPILER_FENCE();
-        __builtin_amdgcn_s_waitcnt(0x0070);                // vmcnt(0), lgkmcnt(0)
+        __builtin_amdgcn_s_waitcnt(0x0070 | (n & 15) | (n >> 4) << 14);
         __builtin_amdgcn_s_barrier();
         NVFP4_COMPILER_FENCE();
     };
+    using InFlight = std::integral_constant<int, (STAGES - 2) * (UA + UW)>;      // at a step's barrier: the copies behind the next step's
 
-#pragma unroll
-    for (int f = 0; f < NF; ++f) next_scale[f] = 0u;
     load_scales(0);
-    start_step(0);
-    static_for<0, UA + UW>([&](auto x) { copy(0, x); });
-    wait_and_join();
     uint32_t word[NF];
 #pragma unroll
     for (int f = 0; f < NF; ++f) word[f] = next_scale[f];
-    start_step(1);
-    static_for<0, UA + UW>([&](auto x) { copy(STAGE, x); });
-    auto next_words = [&](int s) {                         // (selected: see below)
-        const bool last = (s & 3) == 3;
-#pragma unroll
-        for (int f = 0; f < NF; ++f) word[f] = last ? next_scale[f] : word[f] >> 8;
-    };
+    static_for<0, STAGES>([&](auto s) {
+        start_step(s);
+        static_for<0, UA + UW>([&](auto x) { copy(s, x); });
+    });
+    wait_and_join(std::integral_constant<int, (STAGES - 1) * (UA + UW)>());
 
-    // A step is one basic block: a branch between its matrix instructions would let the compiler move them behind it, out of
-    // the shadow of what they are placed around.  So copies past the end of K go out with offsets past the range, and the next
-    // step's scales (made where everything that was asked for has arrived, so that no wait stands in front of them) by selection.
+    // Four steps (a word of scales) are one basic block: a branch between matrix instructions would let the compiler move them
+    // behind it, out of the shadow of what they are placed around.  So copies past the end of K go out with offsets past the
+    // range, and the steps that fill up the last four multiply the zeros that these leave.
     if constexpr (FAST) {
         union Frag {
             uint4v q[2];
@@ -180,46 +185,39 @@ __global__ __launch_bounds__(256) void e4m3_gemm_kernel(const E4m3GemmArgs g)
         };
         Frag frag[2][NF];
         uint32_t scale[NF];
-        auto multiply = [&](auto h_c, auto t_c) {
-            constexpr int h = decltype(h_c)::value, i = decltype(t_c)::value / TM, j = decltype(t_c)::value % TM;
-            acc[i][j] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(frag[h][TM + i].v, frag[h][j].v, acc[i][j], 0, 0, 0, (int)scale[TM + i], 0, (int)scale[j]);
-            __builtin_amdgcn_sched_barrier(0);
-        };
-        using Half0 = std::integral_constant<int, 0>;
-        using Half1 = std::integral_constant<int, 1>;
-        // the 2 NF reads of a half go behind the first MFMAs of the half before, two to an MFMA: they are back when it ends
-        auto reads_behind = [&](int stage, auto h_c, auto t_c) {
-            constexpr int h = decltype(h_c)::value, t = decltype(t_c)::value, kEach = (2 * NF + NMF - 1) / NMF > 2 ? (2 * NF + NMF - 1) / NMF : 2;
-            static_for<0, 2 * NF>([&](auto pc) {
-                if constexpr (pc / kEach == t) frag[h][pc / 2].q[pc % 2] = read_chunk(stage, 2 * h + pc % 2, pc / 2);
-            });
-        };
         static_for<0, NF>([&](auto f) {
             frag[0][f].q[0] = read_chunk(0, 0, f);
             frag[0][f].q[1] = read_chunk(0, 1, f);
             scale[f] = word[f];
         });
-        for (int s = 0; s < S; ++s) {
-            const int here = (s & 1) * STAGE, there = STAGE - here;
-            if ((s & 3) == 1) load_scales(min((s >> 2) + 1, (S - 1) >> 2));
-            static_for<0, NMF>([&](auto t) {
-                multiply(Half0(), t);
-                reads_behind(here, Half1(), t);
-                __builtin_amdgcn_sched_barrier(0);
-            });
-            wait_and_join();
-            next_words(s);
-            start_step(s + 2);
-            static_for<0, NMF>([&](auto t) {
-                multiply(Half1(), t);
-                reads_behind(there, Half0(), t);
-                static_for<0, UA + UW>([&](auto x) {
-                    if constexpr (x * NMF / (UA + UW) == decltype(t)::value) copy(here, x);
+        for (int s0 = 0; s0 < S; s0 += 4) {
+            load_scales(min((s0 >> 2) + 1, (S - 1) >> 2));
+            static_for<0, 8>([&](auto half_c) {
+                constexpr int q = decltype(half_c)::value / 2, h = decltype(half_c)::value % 2;
+                if constexpr (h == 1) {
+                    wait_and_join(InFlight());
+                    start_step(s0 + q + STAGES);
+                }
+                static_for<0, NMF>([&](auto t_c) {
+                    constexpr int t = decltype(t_c)::value, i = t / TM, j = t % TM;
+                    acc[i][j] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(frag[h][TM + i].v, frag[h][j].v, acc[i][j], 0, 0, 0, (int)scale[TM + i], 0, (int)scale[j]);
+                    __builtin_amdgcn_sched_barrier(0);
+                    // the 2 NF reads of a half go behind the first matrix instructions, two to one: they are back when it ends
+                    constexpr int kEach = (2 * NF + NMF - 1) / NMF > 2 ? (2 * NF + NMF - 1) / NMF : 2;
+                    static_for<0, 2 * NF>([&](auto pc) {
+                        if constexpr (pc / kEach == t) frag[1 - h][pc / 2].q[pc % 2] = read_chunk(q + h, 2 * (1 - h) + pc % 2, pc / 2);
+                    });
+                    if constexpr (h == 1)
+                        static_for<0, UA + UW>([&](auto x) {
+                            if constexpr (x * NMF / (UA + UW) == t) copy(q, x);
+                        });
+                    __builtin_amdgcn_sched_barrier(0);
                 });
-                __builtin_amdgcn_sched_barrier(0);
-            });
+                if constexpr (h == 1) {
 #pragma unroll
-            for (int f = 0; f < NF; ++f) scale[f] = word[f];
+                    for (int f = 0; f < NF; ++f) scale[f] = q == 3 ? next_scale[f] : scale[f] >> 8;
+                }
+            });
         }
     } else {
         typedef __bf16 bf16x8v __attribute__((ext_vector_type(8)));
@@ -234,24 +232,28 @@ __global__ __launch_bounds__(256) void e4m3_gemm_kernel(const E4m3GemmArgs g)
             frag[j][f][d] = x;
         };
         // an E8M0 byte is the exponent of an fp32 number; the conversion takes nothing else of its scale (0 is 2^-127, 255 NaN)
-        auto take_scales = [&] {
+        auto take_scales = [&](int q) {
 #pragma unroll
-            for (int f = 0; f < NF; ++f) scale[f] = __uint_as_float((word[f] & 255u) << 23);
+            for (int f = 0; f < NF; ++f) scale[f] = __uint_as_float((word[f] >> 8 * q & 255u) << 23);
         };
         static_for<0, NF>([&](auto f) { codes[0][f] = read_chunk(0, 0, f); });
-        take_scales();
+        take_scales(0);
         static_for<0, 4 * NF>([&](auto pc) { expand(0, 0, pc / 4, pc % 4); });
-        for (int s = 0; s < S; ++s) {
-            const int here = (s & 1) * STAGE, there = STAGE - here;
-            if ((s & 3) == 1) load_scales(min((s >> 2) + 1, (S - 1) >> 2));
-            static_for<0, 8>([&](auto sub_c) {
-                constexpr int c = decltype(sub_c)::value / 2, j = decltype(sub_c)::value % 2, set = c & 1;
+        for (int s0 = 0; s0 < S; s0 += 4) {
+            load_scales(min((s0 >> 2) + 1, (S - 1) >> 2));
+            static_for<0, 32>([&](auto sub_c) {
+                constexpr int q = decltype(sub_c)::value / 8, c = decltype(sub_c)::value / 2 % 4, j = decltype(sub_c)::value % 2, set = c & 1;
                 if constexpr (c == 3 && j == 0) {
-                    wait_and_join();
-                    next_words(s);
-                    start_step(s + 2);
+                    wait_and_join(InFlight());
+                    start_step(s0 + q + STAGES);
                 }
-                if constexpr (c == 3 && j == 1) take_scales();
+                if constexpr (c == 3 && j == 1) {
+                    if constexpr (q == 3) {
+#pragma unroll
+                        for (int f = 0; f < NF; ++f) word[f] = next_scale[f];
+                    }
+                    take_scales((q + 1) & 3);
+                }
                 static_for<0, NMF>([&](auto t_c) {
                     constexpr int t = decltype(t_c)::value, i = t / TM, jj = t % TM;
                     acc[i][jj] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8v, frag[j][TM + i]), __builtin_bit_cast(bf16x8v, frag[j][jj]), acc[i][jj], 0, 0, 0);
@@ -260,18 +262,18 @@ __global__ __launch_bounds__(256) void e4m3_gemm_kernel(const E4m3GemmArgs g)
                         if constexpr (pc * NMF / (4 * NF) == t) expand(j == 0 ? set : set ^ 1, 1 - j, pc / 4, pc % 4);
                     });
                     static_for<0, NF>([&](auto f) {
-                        if constexpr (j == 0 && frag_slot<NMF, NF>(f) == t) codes[set ^ 1][f] = read_chunk(c == 3 ? there : here, (c + 1) & 3, f);
+                        if constexpr (j == 0 && frag_slot<NMF, NF>(f) == t) codes[set ^ 1][f] = read_chunk(c == 3 ? q + 1 : q, (c + 1) & 3, f);
                     });
                     if constexpr (c == 3)
                         static_for<0, UA + UW>([&](auto x) {
-                            if constexpr (x * 2 * NMF / (UA + UW) == j * NMF + t) copy(here, x);
+                            if constexpr (x * 2 * NMF / (UA + UW) == j * NMF + t) copy(q, x);
                         });
                     __builtin_amdgcn_sched_barrier(0);
                 });
             });
         }
     }
-    wait_and_join();                                       // (reads and copies past the end: the epilogue takes LDS over)
+    wait_and_join(std::integral_constant<int, 0>());       // (reads and copies past the end: the epilogue takes LDS over)
 
     // ---- epilogue.  A wave turns 32 rows at a time in LDS of its own and stores whole rows of its tile.
     const int64_t wave_m = m0 + wm * WM, wave_n = n0 + wn * WF;
@@ -387,11 +389,11 @@ __global__ __launch_bounds__(256) void e4m3_gemm_kernel(const E4m3GemmArgs g)
 #endif
 }
 
-template <int BM, int BN, int KIND, bool FAST>
-static hipError_t launch_e4m3_shape(E4m3GemmArgs g, hipStream_t s)
+template <int BM, int BN, int KIND, bool FAST, int STAGES>
+static hipError_t launch_e4m3_stages(const E4m3GemmArgs &g, hipStream_t s)
 {
     constexpr bool GATED = KIND >= kE4m3Silu;
-    constexpr int BF = GATED ? BN / 2 : BN, main = 2 * (BM + BN) * 128, turn = 4 * 32 * (BF / 2 * 4 + 16) + (GATED ? BM * (8 + 144) : 0);
+    constexpr int BF = GATED ? BN / 2 : BN, main = STAGES * (BM + BN) * 128, turn = 4 * 32 * (BF / 2 * 4 + 16) + (GATED ? BM * (8 + 144) : 0);
     constexpr int smem = main > turn ? main : turn;
     static_assert(smem <= 160 * 1024, "LDS");
     // the dynamic LDS limit is raised once per kernel variant and device
@@ -399,14 +401,27 @@ static hipError_t launch_e4m3_shape(E4m3GemmArgs g, hipStream_t s)
     int dev = 0;
     if (hipError_t e = hipGetDevice(&dev); e != hipSuccess) return e;
     if (((attr_set >> (dev & 63)) & 1u) == 0) {
-        if (hipError_t e = hipFuncSetAttribute((const void *)e4m3_gemm_kernel<BM, BN, KIND, FAST>, hipFuncAttributeMaxDynamicSharedMemorySize, smem)) return e;
+        if (hipError_t e = hipFuncSetAttribute((const void *)e4m3_gemm_kernel<BM, BN, KIND, FAST, STAGES>, hipFuncAttributeMaxDynamicSharedMemorySize, smem)) return e;
         attr_set |= 1ull << (dev & 63);
     }
+    const unsigned per_xcd = (unsigned)((g.tiles_m * (int64_t)g.tiles_n + 7) / 8);
+    e4m3_gemm_kernel<BM, BN, KIND, FAST, STAGES><<<8 * per_xcd, 256, smem, s>>>(g);
+    return hipGetLastError();
+}
+
+template <int BM, int BN, int KIND, bool FAST>
+static hipError_t launch_e4m3_shape(E4m3GemmArgs g, hipStream_t s)
+{
+    constexpr int BF = KIND >= kE4m3Silu ? BN / 2 : BN;
     g.tiles_m = (int)((g.M + BM - 1) / BM);
     g.tiles_n = (int)((g.N + BF - 1) / BF);
-    const unsigned per_xcd = (unsigned)((g.tiles_m * (int64_t)g.tiles_n + 7) / 8);
-    e4m3_gemm_kernel<BM, BN, KIND, FAST><<<8 * per_xcd, 256, smem, s>>>(g);
-    return hipGetLastError();
+    if constexpr (BM + BN <= 128) return launch_e4m3_stages<BM, BN, KIND, FAST, 4>(g, s);
+    else if constexpr (BM + BN <= 320) {
+        // a tile to a compute unit: its own copies have to hide the way to memory, so four stages; with more tiles two of them
+        // share a compute unit and its LDS, and hide each other's waits
+        if (g.tiles_m * (int64_t)g.tiles_n <= 256) return launch_e4m3_stages<BM, BN, KIND, FAST, 4>(g, s);
+        return launch_e4m3_stages<BM, BN, KIND, FAST, 2>(g, s);
+    } else return launch_e4m3_stages<BM, BN, KIND, FAST, 2>(g, s);
 }
 
 template <int BM, int BN, bool FAST>

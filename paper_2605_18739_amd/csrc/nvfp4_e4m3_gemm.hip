@@ -180,24 +180,22 @@ hipError_t launch_e4m3_gemm(int kind, const E4m3GemmArgs &g, void *workspace, hi
 {
     if (g.M <= kFewRows) return launch_few_rows(kind, g, g.codes ? static_cast<float *>(workspace) : nullptr, s);
     const bool gated = kind >= kE4m3Silu;
-    // the shape whose rounds of workgroups over the 256 compute units take least: cycles of a step (128 k) by the tile's
-    // matrix instructions and what comes with them
+    // The shape whose rounds of tiles over the 256 compute units take least, by the time of a step (128 k) of a full round, ns:
+    // 4096^3 takes exact 103 / 116 / 105 / 112 / 116 / 165 us with the shapes in this order, fast 56 / 73 / 70 / 69 / 77 / 109.
     struct Shape {
-        int bm, bn;
-        double step;
+        int bm, bn, exact, fast;
         hipError_t (*launch)(int, const E4m3GemmArgs &, hipStream_t);
     };
-    static const Shape kPlain[] = {{256, 256, 2300, launch_e4m3_256x256}, {256, 128, 1250, launch_e4m3_256x128}, {128, 128, 750, launch_e4m3_128x128}, {64, 64, 300, launch_e4m3_64x64}};
-    static const Shape kGated[] = {{256, 256, 2300, launch_e4m3_256x256}, {128, 256, 1250, launch_e4m3_128x256}, {64, 256, 800, launch_e4m3_64x256}};
+    static const Shape kShapes[] = {{256, 256, 3150, 1750, launch_e4m3_256x256}, {256, 128, 1800, 1140, launch_e4m3_256x128}, {128, 256, 1640, 1090, launch_e4m3_128x256},
+                                    {128, 128, 880, 540, launch_e4m3_128x128}, {64, 256, 910, 600, launch_e4m3_64x256}, {64, 64, 330, 215, launch_e4m3_64x64}};
     const Shape *best = nullptr;
-    double least = 0.0;
-    auto consider = [&](const Shape &c) {
-        const int64_t tiles = ((g.M + c.bm - 1) / c.bm) * ((g.N + c.bn / (gated ? 2 : 1) - 1) / (c.bn / (gated ? 2 : 1)));
-        const double cost = (double)((tiles + 255) / 256) * c.step;
+    int64_t least = 0;
+    for (const Shape &c : kShapes) {
+        if (gated && c.bn != 256) continue;
+        const int64_t bf = gated ? c.bn / 2 : c.bn, tiles = ((g.M + c.bm - 1) / c.bm) * ((g.N + bf - 1) / bf);
+        const int64_t cost = (tiles + 255) / 256 * (g.fast ? c.fast : c.exact);
         if (!best || cost < least) best = &c, least = cost;
-    };
-    if (gated) for (const Shape &c : kGated) consider(c);
-    else for (const Shape &c : kPlain) consider(c);
+    }
     return best->launch(kind, g, s);
 }
 

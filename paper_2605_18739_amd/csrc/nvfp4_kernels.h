@@ -175,6 +175,7 @@ hipError_t launch_e4m3_tiles(const uint16_t *x, int64_t R, int64_t C, int64_t ld
 struct E4m3GemmArgs {
     const uint8_t *codes_a, *scales_a, *codes_w, *scales_w;
     int64_t M, N, K;                       // gated: N columns of the result, W has 2 N rows (gate, then up)
+    int64_t scales_a_bytes, scales_w_bytes;
     bool w_tiles;                          // W: a scale for 128 x 128
     bool scale_words;                      // rows of scales are whole words
     bool fast;                             // fast sums (more than 64 rows; fewer are bound by memory and take exact ones)
