@@ -533,7 +533,7 @@ int nvfp4_e4m3_gemm_gated(const nvfp4_e4m3_tensor *A, const nvfp4_e4m3_tensor *W
                           void *gate_up_bf16, int64_t ld_gate_up, void *workspace, size_t workspace_bytes, void *stream);
 
 /*
- * Backward pass of h = act(g) u.  From dh [T, F] and gate_up = [g | u] [T, 2F] (bf16, row strides multiples of 8),
+ * Backward pass of h = act(g) u.  From dh [T, F] and gate_up = [g | u] [T, 2F] (bf16, row strides multiples of 8, at most 2^22),
  *   dg = dh u act'(g),  du = dh act(g)     (fp32, rounded once)
  * side by side as [dg | du], and h again:
  *   out     [T, 2F] along the features (rows = T, K = 2F; F % 128 == 0): dX = out W is nvfp4_e4m3_gemm with the transpose of W

@@ -914,7 +914,7 @@ int nvfp4_gated_backward(const void *dh_bf16, int64_t ld_dh, const void *gate_up
         if (int rc = check_e4m3_out(h_t, F, up16(T), 1)) return rc;
     if (d_bf16)
         if (int rc = check_matrix(d_bf16, ld_d, 2 * F)) return rc;
-    if (blocks128(T) > kMaxLanes / 512 / blocks128(F)) return NVFP4_ERR_SHAPE;
+    if (ld_dh > kE4m3MaxK || ld_gate_up > kE4m3MaxK || (d_bf16 && ld_d > kE4m3MaxK)) return NVFP4_ERR_SHAPE;       // (a tile's rows are addressed with 32 bits)
     GatedBackwardArgs a{};
     a.dh = static_cast<const uint16_t *>(dh_bf16);
     a.ld_dh = ld_dh;

@@ -17,16 +17,51 @@ __device__ __forceinline__ uint32_t e8m0_of_amax(uint32_t amax_bits)
     const int byte = (int)((amax_bits + 0x1FFFFFu) >> 23) - 8;
     return amax_bits >= 0x7F800000u ? 255u : (uint32_t)max(byte, 0);
 }
-// 2^-(byte - 127), what the block's elements are multiplied by (byte <= 247: a normal number); 255: NaN
-__device__ __forceinline__ float e8m0_inverse(uint32_t byte) { return byte == 255u ? __builtin_nanf("") : __uint_as_float((254u - byte) << 23); }
+// 2^(byte - 127) as the conversions below take it: the byte is the exponent of an fp32 number, and they look at nothing else of it
+// (0 is 2^-127, 255 makes every code NaN)
+__device__ __forceinline__ float e8m0_scale(uint32_t byte) { return __uint_as_float(byte << 23); }
 
-// four values of at most 448 -> their E4M3 codes, nearest even (NaN: 0x7F with the sign kept)
-__device__ __forceinline__ uint32_t e4m3_pack4(float a, float b, float c, float d)
+// Values that are at most 448 times the scale -> their E4M3 codes, nearest even (NaN: 0x7F with the sign kept).  (Compared with
+// scaling by an exact power of two and v_cvt_pk_fp8_f32 on all codes, all midpoints and their neighbours at every scale: the same.)
+typedef short short2v __attribute__((ext_vector_type(2)));
+__device__ __forceinline__ short2v any_pair()          // (both halves get written; a zero would cost a move)
 {
-    int w = __builtin_amdgcn_cvt_pk_fp8_f32(a, b, 0, false);
-    return (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(c, d, w, true);
+    uint32_t w;
+#if defined(__HIP_DEVICE_COMPILE__)
+    asm("" : "=v"(w));
+#else
+    w = 0;
+#endif
+    return __builtin_bit_cast(short2v, w);
+}
+__device__ __forceinline__ uint32_t e4m3_pack4(float a, float b, float c, float d, float scale)
+{
+    const short2v w = __builtin_amdgcn_cvt_scalef32_pk_fp8_f32(any_pair(), a, b, scale, false);
+    return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_fp8_f32(w, c, d, scale, true));
+}
+// two codes in the lower half of a word whose upper half is anything
+__device__ __forceinline__ uint32_t e4m3_pack2(float a, float b, float scale)
+{
+    return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_fp8_f32(any_pair(), a, b, scale, false));
+}
+// two pairs of bf16
+__device__ __forceinline__ uint32_t e4m3_pack4(uint32_t ab, uint32_t cd, float scale)
+{
+    typedef __bf16 bf16x2v __attribute__((ext_vector_type(2)));
+    const short2v w = __builtin_amdgcn_cvt_scalef32_pk_fp8_bf16(any_pair(), __builtin_bit_cast(bf16x2v, ab), scale, false);
+    return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_fp8_bf16(w, __builtin_bit_cast(bf16x2v, cd), scale, true));
 }
 
+// the larger of m and |v|; NaN if either is (v_maximum3_f32: the older maxima drop it)
+__device__ __forceinline__ float abs_max(float m, float v)
+{
+#if defined(__HIP_DEVICE_COMPILE__)
+    return __builtin_elementwise_maximum(m, __builtin_fabsf(v));
+#else
+    return m + v;
+#endif
+}
+// ... as bits that order like unsigned numbers, NaN above all
 __device__ __forceinline__ uint32_t abs_bits(float v) { return __float_as_uint(v) & 0x7FFFFFFFu; }
 
 template <int CTRL>
@@ -55,10 +90,11 @@ __device__ __forceinline__ uint4v pack8(const float (&f)[8])
 {
     return uint4v{pack_bf16x2(f[0], f[1]), pack_bf16x2(f[2], f[3]), pack_bf16x2(f[4], f[5]), pack_bf16x2(f[6], f[7])};
 }
-__device__ __forceinline__ uint2v e4m3_pack8(const float (&f)[8], float inv)
+__device__ __forceinline__ uint2v e4m3_pack8(const float (&f)[8], float scale)
 {
-    return uint2v{e4m3_pack4(f[0] * inv, f[1] * inv, f[2] * inv, f[3] * inv), e4m3_pack4(f[4] * inv, f[5] * inv, f[6] * inv, f[7] * inv)};
+    return uint2v{e4m3_pack4(f[0], f[1], f[2], f[3], scale), e4m3_pack4(f[4], f[5], f[6], f[7], scale)};
 }
+__device__ __forceinline__ uint2v e4m3_pack8(uint4v v, float scale) { return uint2v{e4m3_pack4(v.x, v.y, scale), e4m3_pack4(v.z, v.w, scale)}; }
 // largest magnitude of eight packed bf16, as the bits of an fp32 number
 __device__ __forceinline__ uint32_t absmax8_bits(uint4v v)
 {

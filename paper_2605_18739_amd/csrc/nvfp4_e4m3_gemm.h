@@ -350,14 +350,15 @@ __global__ __launch_bounds__(256) void e4m3_gemm_kernel(const E4m3GemmArgs g)
                 store_bf16(j_c, std::integral_constant<int, 0>(), g.gate_up, g.ld_gate_up, 0, g.N);
                 store_bf16(j_c, std::integral_constant<int, TF>(), g.gate_up, g.ld_gate_up, g.N, g.N);
             }
-            uint32_t m = 0u;
+            float most = 0.0f;
 #pragma unroll
             for (int i = 0; i < TF; ++i)
 #pragma unroll
                 for (int e = 0; e < 16; ++e) {
                     acc[i][j][e] = activation<KIND == kE4m3Silu ? kActSilu : kActGelu>(acc[i][j][e]) * acc[i + TF][j][e];
-                    m = max(m, abs_bits(acc[i][j][e]));
+                    most = abs_max(most, acc[i][j][e]);
                 }
+            uint32_t m = abs_bits(most);
             m = max(m, (uint32_t)__shfl_xor((int)m, 32, 64));
             if (lhalf == 0) top[(wm * WM + j * 32 + lrow) * 2 + wn] = m;
             if (g.h_bf16) store_bf16(j_c, std::integral_constant<int, 0>(), g.h_bf16, g.ld_h, 0, g.N);
@@ -368,14 +369,14 @@ __global__ __launch_bounds__(256) void e4m3_gemm_kernel(const E4m3GemmArgs g)
             constexpr int j = decltype(j_c)::value;
             const int r = wm * WM + j * 32 + lrow;
             const uint32_t byte = e8m0_of_amax(max(top[2 * r], top[2 * r + 1]));
-            const float inv = e8m0_inverse(byte);
+            const float scale = e8m0_scale(byte);
             if (wn == 0 && lhalf == 0 && m0 + r < g.M) g.scales[(m0 + r) * ((g.N + 127) >> 7) + tile_n] = (uint8_t)byte;
 #pragma unroll
             for (int i = 0; i < TF; ++i)
 #pragma unroll
                 for (int q = 0; q < 4; ++q)
                     *(uint32_t *)(rows + r * kRow + wn * WF + i * 32 + 8 * q + 4 * lhalf) =
-                        e4m3_pack4(acc[i][j][4 * q] * inv, acc[i][j][4 * q + 1] * inv, acc[i][j][4 * q + 2] * inv, acc[i][j][4 * q + 3] * inv);
+                        e4m3_pack4(acc[i][j][4 * q], acc[i][j][4 * q + 1], acc[i][j][4 * q + 2], acc[i][j][4 * q + 3], scale);
         });
         __syncthreads();
 #pragma unroll

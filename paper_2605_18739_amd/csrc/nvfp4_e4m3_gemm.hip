@@ -146,12 +146,12 @@ __global__ __launch_bounds__(256) void e4m3_rows_f32_kernel(const float *__restr
 #pragma unroll
         for (int i = 0; i < 4; ++i) f[i] = lo[i], f[4 + i] = hi[i];
     }
-    uint32_t top = 0u;
+    float top = 0.0f;
 #pragma unroll
-    for (int i = 0; i < 8; ++i) top = max(top, abs_bits(f[i]));
-    const uint32_t byte = e8m0_of_amax(row16_max(top));
+    for (int i = 0; i < 8; ++i) top = abs_max(top, f[i]);
+    const uint32_t byte = e8m0_of_amax(row16_max(abs_bits(top)));
     if (col < F) {
-        *(uint2v *)(codes + m * F + col) = e4m3_pack8(f, e8m0_inverse(byte));
+        *(uint2v *)(codes + m * F + col) = e4m3_pack8(f, e8m0_scale(byte));
         if ((threadIdx.x & 15) == 0) scales[block] = (uint8_t)byte;
     }
 }

@@ -31,9 +31,7 @@ __global__ __launch_bounds__(256) void e4m3_rows_kernel(const uint16_t *__restri
 #pragma unroll
     for (int i = 0; i < kRowPieces; ++i) {
         const uint32_t byte = e8m0_of_amax(row16_max(absmax8_bits(v[i])));
-        float f[8];
-        unpack8(v[i], f);
-        const uint2v c = e4m3_pack8(f, e8m0_inverse(byte));
+        const uint2v c = e4m3_pack8(v[i], e8m0_scale(byte));
         if (first + i < pieces && col[i] < C) {
             *(uint2v *)(codes + row[i] * C + col[i]) = c;
             if ((lane & 15) == 0) scales[row[i] * nb + (col[i] >> 7)] = (uint8_t)byte;
@@ -47,7 +45,7 @@ __global__ __launch_bounds__(256) void e4m3_rows_kernel(const uint16_t *__restri
 // whole rows of 128 bytes.
 // TILES: one scale for the tile, the codes also leave in the order of x.
 template <bool TILES>
-__global__ __launch_bounds__(256) void e4m3_tile_kernel(const uint16_t *__restrict__ x, int64_t ld, int64_t R, int64_t C, int64_t tiles_c, int64_t K_t,
+__global__ __launch_bounds__(256, 4) void e4m3_tile_kernel(const uint16_t *__restrict__ x, int64_t ld, int64_t R, int64_t C, int64_t tiles_c, int64_t K_t,
                                                         uint8_t *__restrict__ codes, uint8_t *__restrict__ scales, uint8_t *__restrict__ codes_t,
                                                         uint8_t *__restrict__ scales_t)
 {
@@ -77,15 +75,15 @@ __global__ __launch_bounds__(256) void e4m3_tile_kernel(const uint16_t *__restri
     }
     __syncthreads();
     uint32_t byte[8];
-    float inv[8];
+    float scale[8];
     if constexpr (TILES) {
         uint32_t all = 0u;
 #pragma unroll
         for (int w = 0; w < 4; ++w) all = pk_absmax_u16(all, top[w][lane >> 2][lane & 3]);
         byte[0] = e8m0_of_amax(wave_max_u32(pk_hmax_u16(all)) << 16);
-        inv[0] = e8m0_inverse(byte[0]);
+        scale[0] = e8m0_scale(byte[0]);
 #pragma unroll
-        for (int k = 1; k < 8; ++k) inv[k] = inv[0];
+        for (int k = 1; k < 8; ++k) scale[k] = scale[0];
     } else {
 #pragma unroll
         for (int k = 0; k < 4; ++k) {
@@ -94,17 +92,15 @@ __global__ __launch_bounds__(256) void e4m3_tile_kernel(const uint16_t *__restri
             for (int w = 1; w < 4; ++w) all = pk_absmax_u16(all, top[w][cg][k]);
             byte[2 * k] = e8m0_of_amax(all << 16);
             byte[2 * k + 1] = e8m0_of_amax(all & 0xFFFF0000u);
-            inv[2 * k] = e8m0_inverse(byte[2 * k]);
-            inv[2 * k + 1] = e8m0_inverse(byte[2 * k + 1]);
+            scale[2 * k] = e8m0_scale(byte[2 * k]);
+            scale[2 * k + 1] = e8m0_scale(byte[2 * k + 1]);
         }
     }
     uint32_t c[8][2];                                       // TILES: of a row; otherwise of a column
     if constexpr (TILES) {
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
-            float f[8];
-            unpack8(v[i], f);
-            const uint2v w = e4m3_pack8(f, inv[0]);
+            const uint2v w = e4m3_pack8(v[i], scale[0]);
             c[i][0] = w.x, c[i][1] = w.y;
             if (r0 + i < R && c0 < C) *(uint2v *)(codes + (r0 + i) * C + c0) = w;
         }
@@ -135,11 +131,11 @@ __global__ __launch_bounds__(256) void e4m3_tile_kernel(const uint16_t *__restri
         }
 #pragma unroll
         for (int k = 0; k < 8; ++k) {
-            float f[8];
+            uint32_t pair[4];                               // rows 2 i, 2 i + 1 of column k
 #pragma unroll
-            for (int i = 0; i < 8; ++i) f[i] = k & 1 ? bf16hi_to_f32(v[i][k >> 1]) : bf16lo_to_f32(v[i][k >> 1]);
-            const uint2v w = e4m3_pack8(f, inv[k]);
-            c[k][0] = w.x, c[k][1] = w.y;
+            for (int i = 0; i < 4; ++i) pair[i] = __builtin_amdgcn_perm(v[2 * i + 1][k >> 1], v[2 * i][k >> 1], k & 1 ? 0x07060302u : 0x05040100u);
+            c[k][0] = e4m3_pack4(pair[0], pair[1], scale[k]);
+            c[k][1] = e4m3_pack4(pair[2], pair[3], scale[k]);
         }
     }
 #pragma unroll

@@ -10,11 +10,13 @@
 
 namespace nvfp4 {
 
-// Sums over the workgroup of up to sixteen waves; every lane gets them, added in the same order everywhere.
-template <int WAVES, int N>
+// Sums over a wave (ONE) or the workgroup of up to sixteen waves; every lane gets them, added in the same order everywhere.
+constexpr int kNormMaxWaves = 16;
+
+template <bool ONE, int N>
 __device__ __forceinline__ void group_sum(float (&v)[N], float (*part)[N])
 {
-    const int wave = threadIdx.x >> 6;
+    const int wave = threadIdx.x >> 6, waves = blockDim.x >> 6;
 #pragma unroll
     for (int k = 0; k < N; ++k) {
         v[k] += dpp_f32<0xB1>(v[k]);
@@ -24,7 +26,7 @@ __device__ __forceinline__ void group_sum(float (&v)[N], float (*part)[N])
         v[k] += __shfl_xor(v[k], 16, 64);
         v[k] += __shfl_xor(v[k], 32, 64);
     }
-    if constexpr (WAVES > 1) {
+    if constexpr (!ONE) {
         if ((threadIdx.x & 63) == 0) {
 #pragma unroll
             for (int k = 0; k < N; ++k) part[wave][k] = v[k];
@@ -33,8 +35,7 @@ __device__ __forceinline__ void group_sum(float (&v)[N], float (*part)[N])
 #pragma unroll
         for (int k = 0; k < N; ++k) {
             v[k] = part[0][k];
-#pragma unroll
-            for (int w = 1; w < WAVES; ++w) v[k] += part[w][k];
+            for (int w = 1; w < waves; ++w) v[k] += part[w][k];
         }
     }
 }
@@ -46,16 +47,16 @@ __device__ __forceinline__ float inverse_root(float v)
     return __builtin_fmaf(0.5f * y, e, y);
 }
 
-// A workgroup takes a row, or with one wave a workgroup's worth of waves a row each; lane t of a row's holds elements
-// 8 (t + L j) .. + 7, L the lanes of the row, so that sixteen lanes hold a block of 128.
-template <int WAVES, int CH>
-__global__ __launch_bounds__(WAVES == 1 ? 256 : 64 * WAVES) void rms_norm_kernel(const RmsNormArgs a)
+// A workgroup takes a row, with as many waves as 1024 elements each ask for; rows of up to 1024 elements go a wave each (ONE),
+// four to a workgroup.  Lane t of the row's L holds elements 8 (t + L j) .. + 7, so that sixteen lanes hold a block of 128.
+template <bool ONE, int CH>
+__global__ __launch_bounds__(ONE ? 256 : 64 * kNormMaxWaves) void rms_norm_kernel(const RmsNormArgs a)
 {
-    constexpr int L = 64 * WAVES;
-    __shared__ float part[WAVES][1];
-    const int t = WAVES == 1 ? threadIdx.x & 63 : threadIdx.x;
-    const int64_t row = WAVES == 1 ? (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6) : blockIdx.x;
-    if (WAVES == 1 && row >= a.T) return;
+    const int L = ONE ? 64 : blockDim.x;
+    __shared__ float part[kNormMaxWaves][1];
+    const int t = ONE ? threadIdx.x & 63 : threadIdx.x;
+    const int64_t row = ONE ? (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6) : blockIdx.x;
+    if (ONE && row >= a.T) return;
     uint4v x[CH], r[CH], w[CH];
 #pragma unroll
     for (int j = 0; j < CH; ++j) {
@@ -85,7 +86,7 @@ __global__ __launch_bounds__(WAVES == 1 ? 256 : 64 * WAVES) void rms_norm_kernel
 #pragma unroll
         for (int i = 0; i < 8; ++i) s[0] = __builtin_fmaf(f[i], f[i], s[0]);
     }
-    group_sum<WAVES>(s, part);
+    group_sum<ONE>(s, part);
     const float rms = inverse_root(__builtin_fmaf(s[0], a.inv_C, a.eps));
 #pragma unroll
     for (int j = 0; j < CH; ++j) {
@@ -93,16 +94,16 @@ __global__ __launch_bounds__(WAVES == 1 ? 256 : 64 * WAVES) void rms_norm_kernel
         float f[8], g[8];
         unpack8(x[j], f);
         unpack8(w[j], g);
-        uint32_t top = 0u;
+        float top = 0.0f;
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
             f[i] = f[i] * rms * g[i];
-            top = max(top, abs_bits(f[i]));
+            top = abs_max(top, f[i]);
         }
         if (a.y && e < a.C) *(uint4v *)(a.y + row * a.ld_y + e) = pack8(f);
         if (a.codes) {
-            const uint32_t byte = e8m0_of_amax(row16_max(top));
-            const uint2v c = e4m3_pack8(f, e8m0_inverse(byte));
+            const uint32_t byte = e8m0_of_amax(row16_max(abs_bits(top)));
+            const uint2v c = e4m3_pack8(f, e8m0_scale(byte));
             if (e < a.C) {
                 *(uint2v *)(a.codes + row * a.C + e) = c;
                 if ((t & 15) == 0) a.scales[row * ((a.C + 127) >> 7) + (e >> 7)] = (uint8_t)byte;
@@ -114,13 +115,14 @@ __global__ __launch_bounds__(WAVES == 1 ? 256 : 64 * WAVES) void rms_norm_kernel
 // Backward: dx = dsum + r (w dy - xh mean(w dy xh)), xh = r x, and the workgroup's part of dweight = sum over rows of dy xh,
 // which it keeps in registers over all of its rows: partial[workgroup][C].
 // Rows that one wave holds go four to a workgroup, whose waves add up their parts at the end.
-template <int WAVES, int CH>
-__global__ __launch_bounds__(WAVES == 1 ? 256 : 64 * WAVES) void rms_norm_backward_kernel(const RmsNormArgs a, float *__restrict__ partial)
+template <bool ONE, int CH>
+__global__ __launch_bounds__(ONE ? 256 : 64 * kNormMaxWaves) void rms_norm_backward_kernel(const RmsNormArgs a, float *__restrict__ partial)
 {
-    constexpr int L = 64 * WAVES, ROWS = WAVES == 1 ? 4 : 1;
-    __shared__ float part[2][WAVES][2];
-    __shared__ float waves_dw[WAVES == 1 ? ROWS : 1][WAVES == 1 ? CH * 512 : 1];
-    const int t = WAVES == 1 ? threadIdx.x & 63 : threadIdx.x, own = WAVES == 1 ? threadIdx.x >> 6 : 0;
+    constexpr int ROWS = ONE ? 4 : 1;
+    const int L = ONE ? 64 : blockDim.x;
+    __shared__ float part[2][kNormMaxWaves][2];
+    __shared__ float waves_dw[ONE ? ROWS : 1][ONE ? CH * 512 : 1];
+    const int t = ONE ? threadIdx.x & 63 : threadIdx.x, own = ONE ? threadIdx.x >> 6 : 0;
     uint4v w[CH];
     float dw[CH][8];
 #pragma unroll
@@ -160,7 +162,7 @@ __global__ __launch_bounds__(WAVES == 1 ? 256 : 64 * WAVES) void rms_norm_backwa
                 s[1] = __builtin_fmaf(g[i] * h[i], f[i], s[1]);
             }
         }
-        group_sum<WAVES>(s, part[turn]);                             // (two places in turn: one barrier a row)
+        group_sum<ONE>(s, part[turn]);                             // (two places in turn: one barrier a row)
         const float rms = inverse_root(__builtin_fmaf(s[0], a.inv_C, a.eps)), mean = s[1] * a.inv_C * rms * rms;
 #pragma unroll
         for (int j = 0; j < CH; ++j) {
@@ -179,7 +181,7 @@ __global__ __launch_bounds__(WAVES == 1 ? 256 : 64 * WAVES) void rms_norm_backwa
         }
     }
     if (!partial) return;
-    if constexpr (WAVES == 1) {
+    if constexpr (ONE) {
 #pragma unroll
         for (int j = 0; j < CH; ++j)
 #pragma unroll
@@ -226,29 +228,26 @@ __global__ __launch_bounds__(1024) void rms_norm_weight_kernel(const float *__re
 }
 
 // --------------------------------------------------------------------------
-constexpr int kBackwardGrid = 1024;
+constexpr int kBackwardGrid = 1024;                    // workgroups of the backward pass at most, each with one partial sum
 
 size_t rms_norm_workspace_bytes(int64_t T, int64_t C) { return (size_t)std::min<int64_t>(T, kBackwardGrid) * (size_t)C * sizeof(float); }
 
-// (waves of a row, chunks of eight elements a lane)
+// f(a wave holds a row, chunks of eight elements a lane), waves of a workgroup
 template <class F>
 static void of_row(int64_t C, F &&f)
 {
     using std::integral_constant;
-    if (C <= 512) f(integral_constant<int, 1>(), integral_constant<int, 1>());
-    else if (C <= 1024) f(integral_constant<int, 1>(), integral_constant<int, 2>());
-    else if (C <= 2048) f(integral_constant<int, 4>(), integral_constant<int, 1>());
-    else if (C <= 4096) f(integral_constant<int, 4>(), integral_constant<int, 2>());
-    else if (C <= 6144) f(integral_constant<int, 4>(), integral_constant<int, 3>());
-    else if (C <= 8192) f(integral_constant<int, 4>(), integral_constant<int, 4>());
-    else f(integral_constant<int, 8>(), integral_constant<int, 4>());
+    if (C <= 512) f(std::true_type(), integral_constant<int, 1>(), 4);
+    else if (C <= 1024) f(std::true_type(), integral_constant<int, 2>(), 4);
+    else f(std::false_type(), integral_constant<int, 2>(), (int)((C + 1023) / 1024));
 }
 
 hipError_t launch_rms_norm(const RmsNormArgs &a, hipStream_t s)
 {
-    of_row(a.C, [&](auto waves, auto chunks) {
-        constexpr int W = decltype(waves)::value, CH = decltype(chunks)::value;
-        rms_norm_kernel<W, CH><<<(unsigned)(W == 1 ? (a.T + 3) / 4 : a.T), W == 1 ? 256 : 64 * W, 0, s>>>(a);
+    of_row(a.C, [&](auto one, auto chunks, int waves) {
+        constexpr bool ONE = decltype(one)::value;
+        constexpr int CH = decltype(chunks)::value;
+        rms_norm_kernel<ONE, CH><<<(unsigned)(ONE ? (a.T + 3) / 4 : a.T), 64 * waves, 0, s>>>(a);
     });
     return hipGetLastError();
 }
@@ -256,10 +255,12 @@ hipError_t launch_rms_norm(const RmsNormArgs &a, hipStream_t s)
 hipError_t launch_rms_norm_backward(const RmsNormArgs &a, float *dweight, float *partial, hipStream_t s)
 {
     int grid = 0;
-    of_row(a.C, [&](auto waves, auto chunks) {
-        constexpr int W = decltype(waves)::value, CH = decltype(chunks)::value, ROWS = W == 1 ? 4 : 1;
-        grid = (int)std::min<int64_t>((a.T + ROWS - 1) / ROWS, kBackwardGrid);
-        rms_norm_backward_kernel<W, CH><<<(unsigned)grid, W == 1 ? 256 : 64 * W, 0, s>>>(a, dweight ? partial : nullptr);
+    of_row(a.C, [&](auto one, auto chunks, int waves) {
+        constexpr bool ONE = decltype(one)::value;
+        constexpr int CH = decltype(chunks)::value;
+        // as many workgroups as the chip holds at once (sixteen waves to a compute unit): more would be a second, emptier round
+        grid = (int)std::min<int64_t>(ONE ? (a.T + 3) / 4 : a.T, 256 * std::min(16 / waves, 4));
+        rms_norm_backward_kernel<ONE, CH><<<(unsigned)grid, 64 * waves, 0, s>>>(a, dweight ? partial : nullptr);
     });
     if (hipError_t e = hipGetLastError()) return e;
     if (!dweight) return hipSuccess;
