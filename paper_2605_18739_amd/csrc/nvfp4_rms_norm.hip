@@ -140,9 +140,9 @@ __global__ __launch_bounds__(ONE ? 256 : 64 * kNormMaxWaves) void rms_norm_backw
             const int e = 8 * (t + L * j);
             x[j] = d[j] = r[j] = uint4v{0u, 0u, 0u, 0u};
             if (e < a.C) {
-                x[j] = *(const uint4v *)(a.x + row * a.ld + e);
-                d[j] = *(const uint4v *)(a.dy + row * a.ld_dy + e);
-                if (a.residual) r[j] = *(const uint4v *)(a.residual + row * a.ld_residual + e);
+                x[j] = __builtin_nontemporal_load((const uint4v *)(a.x + row * a.ld + e));
+                d[j] = __builtin_nontemporal_load((const uint4v *)(a.dy + row * a.ld_dy + e));
+                if (a.residual) r[j] = __builtin_nontemporal_load((const uint4v *)(a.residual + row * a.ld_residual + e));
             }
         }
     };
@@ -177,7 +177,7 @@ __global__ __launch_bounds__(ONE ? 256 : 64 * kNormMaxWaves) void rms_norm_backw
                 dw[j][i] = __builtin_fmaf(g[i], f[i] * rms, dw[j][i]);
                 o[i] = __builtin_fmaf(rms, __builtin_fmaf(-f[i], mean, g[i] * h[i]), o[i]);
             }
-            if (e < a.C) *(uint4v *)(a.y + row * a.ld_y + e) = pack8(o);
+            if (e < a.C) __builtin_nontemporal_store(pack8(o), (uint4v *)(a.y + row * a.ld_y + e));
         }
     }
     if (!partial) return;
