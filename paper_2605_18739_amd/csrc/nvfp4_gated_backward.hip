@@ -34,6 +34,7 @@ __device__ __forceinline__ void columns_max(uint32_t (&m)[8])
 
 // Addresses are 32-bit offsets from the tile's first element, checked against a range, so that rows behind T need no branches
 // (loaded: zeros, stored: dropped).
+constexpr int kStream = 2;                                       // (the loads' streaming bit: nothing finds the inputs cached)
 constexpr uint32_t kRange = 1u << 30, kPast = 1u << 30;         // (a tile: at most 128 rows 2^22 elements apart, or 2^22 bytes)
 
 __device__ __forceinline__ __amdgpu_buffer_rsrc_t range_at(const void *p)
@@ -66,9 +67,9 @@ __global__ __launch_bounds__(64 * kGatedWaves) void gated_backward_kernel(const 
             const bool in = 2 * rg + i < rows && 8 * cg < cols;
             const uint32_t at = in ? (uint32_t)(2 * rg + i) * (uint32_t)(2 * a.ld_gate_up) + 16 * cg : kPast;
             const uint32_t at_d = in ? (uint32_t)(2 * rg + i) * (uint32_t)(2 * a.ld_dh) + 16 * cg : kPast;
-            g[i] = __builtin_bit_cast(uint4v, __builtin_amdgcn_raw_buffer_load_b128(rg_, at, 0, 0));
-            u[i] = __builtin_bit_cast(uint4v, __builtin_amdgcn_raw_buffer_load_b128(ru, at, 0, 0));
-            d[i] = __builtin_bit_cast(uint4v, __builtin_amdgcn_raw_buffer_load_b128(rd, at_d, 0, 0));
+            g[i] = __builtin_bit_cast(uint4v, __builtin_amdgcn_raw_buffer_load_b128(rg_, at, 0, kStream));
+            u[i] = __builtin_bit_cast(uint4v, __builtin_amdgcn_raw_buffer_load_b128(ru, at, 0, kStream));
+            d[i] = __builtin_bit_cast(uint4v, __builtin_amdgcn_raw_buffer_load_b128(rd, at_d, 0, kStream));
         }
     };
     fetch(blockIdx.x);
