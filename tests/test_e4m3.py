@@ -275,8 +275,8 @@ def test_gemm_into_columns(M, N, ld, first, dtype):
     assert (whole[:, :first] == 7).all() and (whole[:, first + N :] == 7).all()
 
 
-@pytest.mark.parametrize("M", [3, 200])
-def test_gemm_scales(M):
+@pytest.mark.parametrize("M,fast", [(3, False), (200, False), (200, True)])
+def test_gemm_scales(M, fast):
     """Scales over the whole range; a NaN scale and a NaN code reach their own row or columns and no others."""
     g = gen(5)
     A, W = small_integers(g, M, 512, False), small_integers(g, 256, 512, True)
@@ -285,16 +285,16 @@ def test_gemm_scales(M):
     W = nv.E4M3Tensor(W.codes, torch.tensor([[67] * 4, [187] * 4], dtype=torch.uint8).view(E8M0).cuda())
     want = A.codes.cpu().float() @ W.codes.cpu().float().T                      # integers, then one power of two for each result
     want = want.double() * torch.exp2(e.double()) * torch.exp2(torch.tensor([-60.0] * 128 + [60.0] * 128, dtype=F64))
-    assert torch.equal(nv.nvfp4_e4m3_gemm(A, W).cpu().double(), want)
+    assert torch.equal(nv.nvfp4_e4m3_gemm(A, W, fast_sums=fast).cpu().double(), want)
     s = A.scales.view(torch.uint8).clone()
     s[1, 3] = 255
-    bad = nv.nvfp4_e4m3_gemm(nv.E4M3Tensor(A.codes, s), W).cpu().double()
+    bad = nv.nvfp4_e4m3_gemm(nv.E4M3Tensor(A.codes, s), W, fast_sums=fast).cpu().double()
     assert torch.isnan(bad[1]).all()
     keep = torch.arange(M) != 1
     assert torch.equal(bad[keep], want[keep])
     c = W.codes.view(torch.uint8).clone()
     c[130, 511] = 0x7F
-    bad = nv.nvfp4_e4m3_gemm(A, nv.E4M3Tensor(c, W.scales)).cpu().double()
+    bad = nv.nvfp4_e4m3_gemm(A, nv.E4M3Tensor(c, W.scales), fast_sums=fast).cpu().double()
     keep = torch.arange(256) != 130
     assert torch.isnan(bad[:, 130]).all() and torch.equal(bad[:, keep], want[:, keep])
 
@@ -360,6 +360,28 @@ def test_gated(M, F, K, tile, act):
     assert no_codes is None and torch.equal(h_alone, h_bf16)
 
 
+@pytest.mark.parametrize("M,F", [(3, 37), (70, 37), (130, 1), (20, 129), (300, 263)])
+def test_gated_of_odd_widths(M, F):
+    """Without an 8-bit result F may be anything: the gate's and the up projection's rows meet inside a block of scales."""
+    g = gen(M + F)
+    A, W = small_integers(g, M, 400, False), small_integers(g, 2 * F, 400, True)
+    y = values(A) @ values(W).T
+    none, h, gu = nv.nvfp4_e4m3_gemm_gated(A, W, quantize=False, keep_h=True, keep_gate_up=True)
+    assert none is None and torch.equal(gu.cpu(), y.float().to(BF))
+    want = act_ref(nv.ACT_SILU, y[:, :F])[0] * y[:, F:]                         # (exact sums; the activation within 8 u (|g| + 1))
+    E = 8 * U * (y[:, :F].abs() + 1) * want.abs() + 4 * U * want.abs() + 1e-36
+    assert ((h.cpu().double() - want).abs() <= E + 2.0 ** -8 * (want.abs() + E)).all()
+
+
+def test_gated_fast_sums():
+    """The 8-bit instruction's sums in the gated form: exact for small integers, and so the same bytes."""
+    g = gen(21)
+    A, W = small_integers(g, 200, 512, False), small_integers(g, 2 * 272, 512, True)
+    W = nv.E4M3Tensor(W.codes, (W.scales.view(torch.uint8) - 9).view(E8M0))
+    exact, fast = (nv.nvfp4_e4m3_gemm_gated(A, W, keep_h=True, keep_gate_up=True, fast_sums=f) for f in (False, True))
+    assert all(torch.equal(x, y) for x, y in zip(raw(exact[0]), raw(fast[0]))) and torch.equal(exact[1], fast[1]) and torch.equal(exact[2], fast[2])
+
+
 def test_gated_of_large_gates():
     """Gates far outside of what the exponentials take: h goes to zero or to g u, and stays finite."""
     K, F = 16, 16
@@ -410,6 +432,32 @@ def test_gated_backward(T, F, pad, act):
     in_place = gu.cuda()
     assert nv.nvfp4_gated_backward(dh.cuda(), in_place, act=act, quantize=False, d=in_place)[3] is in_place
     assert torch.equal(in_place, got[3])
+
+
+@pytest.mark.parametrize("T,F", [(40, 8), (130, 136), (257, 264)])
+def test_gated_backward_of_odd_widths(T, F):
+    """Along the tokens F may be any multiple of eight; one result alone is what it is beside the others."""
+    g = gen(T + F)
+    dh, gu = randn(g, T, F).to(BF), (1.5 * randn(g, T, 2 * F)).to(BF)
+    gate, up, d = gu[:, :F].double(), gu[:, F:].double(), dh.double()
+    a, slope = act_ref(nv.ACT_SILU, gate)
+    T16 = 16 * ceil(T, 16)
+
+    def turned(x):
+        t = torch.zeros((x.shape[1], T16), dtype=F64)
+        t[:, :T] = x.T
+        return t
+    want, E = torch.cat([d * up * slope, d * a], 1), 32 * U * torch.cat([(d * up).abs(), (d * a).abs()], 1) * (1 + gate.abs()).repeat(1, 2) + 1e-38
+    (o_t, i1), (h_t, i2) = poisoned(2 * F, T16), poisoned(F, T16)
+    nv.nvfp4_gated_backward(dh.cuda(), gu.cuda(), quantize=False, out_t=o_t, h_t=h_t)
+    assert_codes(o_t, turned(want), turned(E), "along the tokens")
+    assert_codes(h_t, turned(a * up), turned(32 * U * (a * up).abs() * (1 + gate.abs()) + 1e-38), "h")
+    i1(), i2()
+    for kind in ("out_t", "h_t"):
+        t, intact = poisoned(2 * F if kind == "out_t" else F, T16)
+        nv.nvfp4_gated_backward(dh.cuda(), gu.cuda(), quantize=False, **{kind: t})
+        assert all(torch.equal(x, y) for x, y in zip(raw(t), raw(o_t if kind == "out_t" else h_t)))
+        intact()
 
 
 def test_gated_backward_against_differences():
