@@ -964,7 +964,7 @@ int nvfp4_rms_norm(const void *x_bf16, int64_t ld, const void *residual_bf16, in
     a.ld_y = ld_y;
     if (out) a.codes = out->codes, a.scales = out->scales;
     a.eps = eps;
-    a.inv_C = 1.0f / (float)C;
+    a.inv_C = 1.0 / (double)C;
     std::lock_guard<std::mutex> lk(g_mu);
     hipStream_t s = static_cast<hipStream_t>(stream);
     Timed t(s, NVFP4_OP_RMS_NORM);
@@ -1000,7 +1000,7 @@ int nvfp4_rms_norm_backward(const void *dy_bf16, int64_t ld_dy, const void *s_bf
     a.y = static_cast<uint16_t *>(dx_bf16);
     a.ld_y = ld_dx;
     a.eps = eps;
-    a.inv_C = 1.0f / (float)C;
+    a.inv_C = 1.0 / (double)C;
     std::lock_guard<std::mutex> lk(g_mu);
     hipStream_t s = static_cast<hipStream_t>(stream);
     Timed t(s, NVFP4_OP_RMS_NORM_BACKWARD);

@@ -209,7 +209,8 @@ struct RmsNormArgs {
     uint16_t *sum, *y;                     // backward: y is dx
     int64_t ld_sum, ld_y;
     uint8_t *codes, *scales;
-    float eps, inv_C;
+    float eps;
+    double inv_C;
 };
 constexpr int64_t kRmsNormMaxC = 16384;
 hipError_t launch_rms_norm(const RmsNormArgs &a, hipStream_t s);

@@ -11,18 +11,29 @@
 namespace nvfp4 {
 
 // Sums over a wave (ONE) or the workgroup of up to sixteen waves; every lane gets them, added in the same order everywhere.
+// The lanes' sums (sixteen elements each) are fp32, they are added in fp64: ten more fp32 roundings in a row would be as large as
+// all others of a result together, and each halves a share of the codes that lie next to a border.
 constexpr int kNormMaxWaves = 16;
 
+template <int CTRL>
+__device__ __forceinline__ double dpp_add(double v)
+{
+    const uint64_t b = __builtin_bit_cast(uint64_t, v);
+    const uint32_t lo = (uint32_t)__builtin_amdgcn_update_dpp(0, (int)(uint32_t)b, CTRL, 0xF, 0xF, true);
+    const uint32_t hi = (uint32_t)__builtin_amdgcn_update_dpp(0, (int)(uint32_t)(b >> 32), CTRL, 0xF, 0xF, true);
+    return v + __builtin_bit_cast(double, (uint64_t)hi << 32 | lo);
+}
+
 template <bool ONE, int N>
-__device__ __forceinline__ void group_sum(float (&v)[N], float (*part)[N])
+__device__ __forceinline__ void group_sum(const float (&lane_sum)[N], double (&v)[N], double (*part)[N])
 {
     const int wave = threadIdx.x >> 6, waves = blockDim.x >> 6;
 #pragma unroll
     for (int k = 0; k < N; ++k) {
-        v[k] += dpp_f32<0xB1>(v[k]);
-        v[k] += dpp_f32<0x4E>(v[k]);
-        v[k] += dpp_f32<0x141>(v[k]);
-        v[k] += dpp_f32<0x140>(v[k]);
+        v[k] = dpp_add<0xB1>((double)lane_sum[k]);
+        v[k] = dpp_add<0x4E>(v[k]);
+        v[k] = dpp_add<0x141>(v[k]);
+        v[k] = dpp_add<0x140>(v[k]);
         v[k] += __shfl_xor(v[k], 16, 64);
         v[k] += __shfl_xor(v[k], 32, 64);
     }
@@ -53,7 +64,7 @@ template <bool ONE, int CH>
 __global__ __launch_bounds__(ONE ? 256 : 64 * kNormMaxWaves) void rms_norm_kernel(const RmsNormArgs a)
 {
     const int L = ONE ? 64 : blockDim.x;
-    __shared__ float part[kNormMaxWaves][1];
+    __shared__ double part[kNormMaxWaves][1];
     const int t = ONE ? threadIdx.x & 63 : threadIdx.x;
     const int64_t row = ONE ? (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6) : blockIdx.x;
     if (ONE && row >= a.T) return;
@@ -86,8 +97,9 @@ __global__ __launch_bounds__(ONE ? 256 : 64 * kNormMaxWaves) void rms_norm_kerne
 #pragma unroll
         for (int i = 0; i < 8; ++i) s[0] = __builtin_fmaf(f[i], f[i], s[0]);
     }
-    group_sum<ONE>(s, part);
-    const float rms = inverse_root(__builtin_fmaf(s[0], a.inv_C, a.eps));
+    double sum[1];
+    group_sum<ONE>(s, sum, part);
+    const float rms = inverse_root((float)(sum[0] * a.inv_C + (double)a.eps));
 #pragma unroll
     for (int j = 0; j < CH; ++j) {
         const int e = 8 * (t + L * j);
@@ -97,7 +109,8 @@ __global__ __launch_bounds__(ONE ? 256 : 64 * kNormMaxWaves) void rms_norm_kerne
         float top = 0.0f;
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
-            f[i] = f[i] * rms * g[i];
+            const float xh = f[i] * rms, low = __builtin_fmaf(f[i], rms, -xh);      // (what the product's rounding dropped comes back in the next one)
+            f[i] = __builtin_fmaf(xh, g[i], low * g[i]);
             top = abs_max(top, f[i]);
         }
         if (a.y && e < a.C) *(uint4v *)(a.y + row * a.ld_y + e) = pack8(f);
@@ -120,7 +133,7 @@ __global__ __launch_bounds__(ONE ? 256 : 64 * kNormMaxWaves) void rms_norm_backw
 {
     constexpr int ROWS = ONE ? 4 : 1;
     const int L = ONE ? 64 : blockDim.x;
-    __shared__ float part[2][kNormMaxWaves][2];
+    __shared__ double part[2][kNormMaxWaves][2];
     __shared__ float waves_dw[ONE ? ROWS : 1][ONE ? CH * 512 : 1];
     const int t = ONE ? threadIdx.x & 63 : threadIdx.x, own = ONE ? threadIdx.x >> 6 : 0;
     uint4v w[CH];
@@ -162,8 +175,9 @@ __global__ __launch_bounds__(ONE ? 256 : 64 * kNormMaxWaves) void rms_norm_backw
                 s[1] = __builtin_fmaf(g[i] * h[i], f[i], s[1]);
             }
         }
-        group_sum<ONE>(s, part[turn]);                             // (two places in turn: one barrier a row)
-        const float rms = inverse_root(__builtin_fmaf(s[0], a.inv_C, a.eps)), mean = s[1] * a.inv_C * rms * rms;
+        double sum[2];
+        group_sum<ONE>(s, sum, part[turn]);                        // (two places in turn: one barrier a row)
+        const float rms = inverse_root((float)(sum[0] * a.inv_C + (double)a.eps)), mean = (float)(sum[1] * a.inv_C) * rms * rms;
 #pragma unroll
         for (int j = 0; j < CH; ++j) {
             const int e = 8 * (t + L * j);
