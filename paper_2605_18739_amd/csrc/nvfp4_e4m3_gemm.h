@@ -71,6 +71,18 @@ __global__ __launch_bounds__(256) void e4m3_gemm_kernel(const E4m3GemmArgs g)
     const int row_at = (lane >> 3) * K;
     // copy x of step s: rows 8 u .. 8 u + 7, u = the wave's first copy + x (even for x even: a wave's counts are even)
     static_assert(UA % 2 == 0 && (GATED ? UW / 2 : UW) % 2 == 0, "copies of a wave");
+    int place[STAGES];                                     // of the stages of steps s0, s0 + 1, ...: they change places where four steps are no whole turns
+#pragma unroll
+    for (int i = 0; i < STAGES; ++i) place[i] = i * STAGE;
+    auto next_turn = [&] {
+        if constexpr (4 % STAGES != 0) {
+            int moved[STAGES];
+#pragma unroll
+            for (int i = 0; i < STAGES; ++i) moved[i] = place[(i + 4) % STAGES];
+#pragma unroll
+            for (int i = 0; i < STAGES; ++i) place[i] = moved[i];
+        }
+    };
     int from[2];                                           // lane offsets of the step being copied
     auto start_step = [&](int s) {
         const int left = K - s * 128;
@@ -79,7 +91,7 @@ __global__ __launch_bounds__(256) void e4m3_gemm_kernel(const E4m3GemmArgs g)
     };
     auto copy = [&](int s, auto x_c) {
         constexpr int x = decltype(x_c)::value;
-        uint8_t *stage = lds + s % STAGES * STAGE;
+        uint8_t *stage = lds + place[s % STAGES];
         if constexpr (x < UA) {
             const int u = wave * UA + x;
             __builtin_amdgcn_raw_ptr_buffer_load_lds(ra, (lds_ptr_t)(stage + u * 1024), 16, from[x & 1] + u * 8 * K, 0, 0, 0);
@@ -105,7 +117,7 @@ __global__ __launch_bounds__(256) void e4m3_gemm_kernel(const E4m3GemmArgs g)
     int frag_at[4];                                        // 16-byte chunks 2 c + half of the lane's row
 #pragma unroll
     for (int c = 0; c < 4; ++c) frag_at[c] = lrow * 128 + (((2 * c + lhalf) ^ ((lrow >> 1) & 7)) << 4);
-    auto read_chunk = [&](int s, int c, int f) { return *(const uint4v *)(lds + s % STAGES * STAGE + frag_row0(f) * 128 + frag_at[c]); };
+    auto read_chunk = [&](int s, int c, int f) { return *(const uint4v *)(lds + place[s % STAGES] + frag_row0(f) * 128 + frag_at[c]); };
 
     // ---- scales: a word holds those of four steps of a fragment's row
     const int nb = S;
@@ -218,6 +230,7 @@ __global__ __launch_bounds__(256) void e4m3_gemm_kernel(const E4m3GemmArgs g)
                     for (int f = 0; f < NF; ++f) scale[f] = q == 3 ? next_scale[f] : scale[f] >> 8;
                 }
             });
+            next_turn();
         }
     } else {
         typedef __bf16 bf16x8v __attribute__((ext_vector_type(8)));
@@ -271,6 +284,7 @@ __global__ __launch_bounds__(256) void e4m3_gemm_kernel(const E4m3GemmArgs g)
                     __builtin_amdgcn_sched_barrier(0);
                 });
             });
+            next_turn();
         }
     }
     wait_and_join(std::integral_constant<int, 0>());       // (reads and copies past the end: the epilogue takes LDS over)
@@ -422,7 +436,8 @@ static hipError_t launch_e4m3_shape(E4m3GemmArgs g, hipStream_t s)
         // share a compute unit and its LDS, and hide each other's waits
         if (g.tiles_m * (int64_t)g.tiles_n <= 256) return launch_e4m3_stages<BM, BN, KIND, FAST, 4>(g, s);
         return launch_e4m3_stages<BM, BN, KIND, FAST, 2>(g, s);
-    } else return launch_e4m3_stages<BM, BN, KIND, FAST, 2>(g, s);
+    } else if constexpr (FAST && BM + BN <= 384) return launch_e4m3_stages<BM, BN, KIND, FAST, 3>(g, s);     // (4096^3 64 us, with two 70; exact sums: even)
+    else return launch_e4m3_stages<BM, BN, KIND, FAST, 2>(g, s);
 }
 
 template <int BM, int BN, bool FAST>

@@ -267,12 +267,12 @@ hipError_t launch_e4m3_gemm(int kind, const E4m3GemmArgs &g, void *workspace, hi
     if (g.M <= kFewRows) return launch_few_rows(kind, g, g.codes ? static_cast<float *>(workspace) : nullptr, s);
     const bool gated = kind >= kE4m3Silu;
     // The shape whose rounds of tiles over the 256 compute units take least, by the time of a step (128 k) of a full round, ns:
-    // 4096^3 takes exact 103 / 116 / 105 / 112 / 116 / 163 us with the shapes in this order, fast 56 / 73 / 70 / 69 / 77 / 109.
+    // 4096^3 takes exact 105 / 117 / 106 / 112 / 118 / 160 us with the shapes in this order, fast 56 / 65 / 64 / 69 / 76 / 110.
     struct Shape {
         int bm, bn, exact, fast;
         hipError_t (*launch)(int, const E4m3GemmArgs &, hipStream_t);
     };
-    static const Shape kShapes[] = {{256, 256, 3150, 1750, launch_e4m3_256x256}, {256, 128, 1800, 1140, launch_e4m3_256x128}, {128, 256, 1640, 1090, launch_e4m3_128x256},
+    static const Shape kShapes[] = {{256, 256, 3150, 1750, launch_e4m3_256x256}, {256, 128, 1800, 1000, launch_e4m3_256x128}, {128, 256, 1640, 980, launch_e4m3_128x256},
                                     {128, 128, 880, 540, launch_e4m3_128x128}, {64, 256, 910, 600, launch_e4m3_64x256}, {64, 64, 300, 215, launch_e4m3_64x64}};
     const Shape *best = nullptr;
     int64_t least = 0;
