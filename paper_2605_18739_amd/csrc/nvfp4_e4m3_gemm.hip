@@ -20,9 +20,10 @@ __device__ __forceinline__ float gated_value(const E4m3GemmArgs &g, int kind, in
 // Up to 16 MT rows of A: bound by the bytes of W.  A workgroup takes 16 rows of W (GATED: 16 of the gate and the 16 of the up
 // projection that belong to them), its waves cut the blocks of 128 k between them and add their sums in LDS in a fixed order.
 // A wave's blocks go through a ring of DEPTH slots in LDS of its own, filled by copies that write LDS directly (eight rows of 128
-// bytes each, whole lines), so waves wait for their own copies only and there is no barrier on the way.  (Loads straight into the
-// instruction's operands, where neighbouring lanes hold different rows, take a cycle of the address unit for each lane: 42 us
-// for 8 x 2*14336 x 4096 where this takes 26.)
+// bytes each, whole lines), so waves wait for their own copies only and there is no barrier on the way.  5 x 4096 x 14336 takes 12.6 us
+// (4.7 TB/s), 64 rows of it 20; 8 x 2*14336 x 4096 gated 26 with the launch behind it (20 at 5.9 TB/s, and 4.8), 64 rows 43.  (Loads
+// straight into the instruction's operands, where neighbouring lanes hold different rows, take a cycle of the address unit for each
+// lane: 14, 43, 33 and 119 us.  Gated columns by the 128 to a workgroup, which would need no second launch: 41 to 49 us for 8 rows.)
 //   v_mfma_f32_16x16x32_bf16 on expanded codes, W as the row operand: lane (r = lane & 15, q = lane >> 4) holds chunks q and q + 4
 //   (16 bytes each) of row r for four instructions.  Chunk c of row r stands at 128 r + 16 (c ^ (r >> 1)): no bank conflicts.
 //   The lane ends up with row m = r of A and columns 4 q .. 4 q + 3.
@@ -195,7 +196,7 @@ __global__ __launch_bounds__(64 * WAVES) void e4m3_few_rows_kernel(const E4m3Gem
 #endif
 }
 
-// fp32 [M, F] (F % 16 == 0) -> 8 bits along F: sixteen lanes a block
+// fp32 [M, F] (F % 16 == 0) -> 8 bits along F: sixteen lanes a block (8 x 14336: 4.8 us, a trip to memory and a launch)
 __global__ __launch_bounds__(256) void e4m3_rows_f32_kernel(const float *__restrict__ h, int64_t F, int64_t nb, int64_t blocks, uint8_t *__restrict__ codes, uint8_t *__restrict__ scales)
 {
     const int64_t block = (int64_t)blockIdx.x * 16 + (threadIdx.x >> 4);

@@ -60,6 +60,8 @@ __device__ __forceinline__ float inverse_root(float v)
 
 // A workgroup takes a row, with as many waves as 1024 elements each ask for; rows of up to 1024 elements go a wave each (ONE),
 // four to a workgroup.  Lane t of the row's L holds elements 8 (t + L j) .. + 7, so that sixteen lanes hold a block of 128.
+// 17600 x 5120 takes 102 us with a residual and its sum (6.2 TB/s), 139 with a bf16 result as well (5.8), 53 without either (5.1);
+// 8 x 4096 takes 3.6, a trip to memory and a launch.
 template <bool ONE, int CH>
 __global__ __launch_bounds__(ONE ? 256 : 64 * kNormMaxWaves) void rms_norm_kernel(const RmsNormArgs a)
 {
@@ -128,6 +130,8 @@ __global__ __launch_bounds__(ONE ? 256 : 64 * kNormMaxWaves) void rms_norm_kerne
 // Backward: dx = dsum + r (w dy - xh mean(w dy xh)), xh = r x, and the workgroup's part of dweight = sum over rows of dy xh,
 // which it keeps in registers over all of its rows: partial[workgroup][C].
 // Rows that one wave holds go four to a workgroup, whose waves add up their parts at the end.
+// 17600 x 5120 with the sum's gradient: 142 us, 5.1 TB/s; waves wait for memory in 70 % of their cycles.  (With loads and stores that
+// keep the lines cached 155; with the next row's loads ahead of this one's sums the same 142.)
 template <bool ONE, int CH>
 __global__ __launch_bounds__(ONE ? 256 : 64 * kNormMaxWaves) void rms_norm_backward_kernel(const RmsNormArgs a, float *__restrict__ partial)
 {
@@ -219,7 +223,7 @@ __global__ __launch_bounds__(ONE ? 256 : 64 * kNormMaxWaves) void rms_norm_backw
     }
 }
 
-// dweight = the partial sums added in a fixed order: sixteen columns a workgroup, 64 strided parts of each
+// dweight = the partial sums added in a fixed order: sixteen columns a workgroup, 64 strided parts of each (768 parts of 5120: 7 us)
 __global__ __launch_bounds__(1024) void rms_norm_weight_kernel(const float *__restrict__ partial, int n, int C, float *__restrict__ dweight)
 {
     __shared__ float part[64][17];
