@@ -384,6 +384,28 @@ def test_gated_fast_sums():
     assert all(torch.equal(x, y) for x, y in zip(raw(exact[0]), raw(fast[0]))) and torch.equal(exact[1], fast[1]) and torch.equal(exact[2], fast[2])
 
 
+@pytest.mark.parametrize("M,N,K", [(4097, 1030, 2032), (4097, 1030, 1680), (4352, 1900, 1808), (4352, 1900, 1152), (300, 700, 1984), (300, 700, 1424)])
+def test_products_over_several_turns(M, N, K):
+    """Stages of LDS change places from turn to turn (four steps of 128 k): whole turns and parts of one, tiles of each kind."""
+    g = gen(M + K)
+    A, W = small_integers(g, M, K, False), small_integers(g, N, K, True)
+    want = values(A).float() @ values(W).float().T                  # (exact: integers below 2^24)
+    say(M, N, K)
+    for fast in (False, True):
+        assert torch.equal(nv.nvfp4_e4m3_gemm(A, W, fast_sums=fast).cpu(), want), fast
+
+
+@pytest.mark.parametrize("K", [512, 1424, 2032])
+def test_gated_fast_sums_over_several_turns(K):
+    """As test_gated_fast_sums, at sizes that take tiles of 128 x 256."""
+    g = gen(K)
+    A, W = small_integers(g, 1100, K, False), small_integers(g, 2 * 2700, K, True)
+    W = nv.E4M3Tensor(W.codes, (W.scales.view(torch.uint8) - 9).view(E8M0))
+    say(K)
+    exact, fast = (nv.nvfp4_e4m3_gemm_gated(A, W, quantize=False, keep_h=True, keep_gate_up=True, fast_sums=f) for f in (False, True))
+    assert torch.equal(exact[1], fast[1]) and torch.equal(exact[2], fast[2])
+
+
 def test_gated_of_large_gates():
     """Gates far outside of what the exponentials take: h goes to zero or to g u, and stays finite."""
     K, F = 16, 16
