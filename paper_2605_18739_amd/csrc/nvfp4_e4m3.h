@@ -115,9 +115,18 @@ __device__ __forceinline__ float sigmoid_f32(float x)
     const float d = 1.0f + e, r = __builtin_amdgcn_rcpf(d), s = __builtin_fmaf(r, __builtin_fmaf(-d, r, 1.0f), r);
     return x < -87.0f ? 0.0f : s;
 }
+// v between two bounds; NaN where v is (v_med3_f32 and the older minima and maxima would give a bound)
+__device__ __forceinline__ float clamped(float v, float lo, float hi)
+{
+#if defined(__HIP_DEVICE_COMPILE__)
+    return __builtin_elementwise_minimum(__builtin_elementwise_maximum(v, lo), hi);
+#else
+    return v + lo + hi;
+#endif
+}
 // GELU in its tanh form is x sigmoid(z), z = 2 sqrt(2 / pi) (x + 0.044715 x^3).  Beyond 16 the sigmoid is 0 or 1 for good.
 constexpr float kGelu1 = 1.59576912f, kGelu3 = 0.0713548163f;   // z = x (kGelu1 + kGelu3 x^2)
-__device__ __forceinline__ float gelu_within(float x) { return __builtin_amdgcn_fmed3f(x, -16.0f, 16.0f); }
+__device__ __forceinline__ float gelu_within(float x) { return clamped(x, -16.0f, 16.0f); }
 template <int ACT>
 __device__ __forceinline__ float activation(float x)
 {

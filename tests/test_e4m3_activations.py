@@ -1,0 +1,66 @@
+"""The activations of gated layers where they can go wrong: gates that are no numbers, gates far outside of what the exponentials
+take, and gates whose activation is tiny.  Against plain evaluations in 64 bits.
+"""
+import math
+
+import pytest
+import torch
+
+import paper_2605_18739_amd as nv
+from tests.test_e4m3 import BF, E8M0, E4M3, F32, F64, U, act_ref, gen, randn, raw, say, values
+
+pytestmark = pytest.mark.gpu
+
+ACTS = [nv.ACT_SILU, nv.ACT_GELU_TANH]
+
+
+@pytest.mark.parametrize("where", ["dh", "gate", "up"])
+@pytest.mark.parametrize("act", ACTS)
+def test_nan_in_the_backward_pass(act, where):
+    """dg = dh u act'(g), du = dh act(g) and h = act(g) u are NaN where a factor is: in bf16, and with scale 255 in the blocks along
+    both axes.  All other blocks are what they are without it."""
+    g = gen(12)
+    T, F, t, f = 300, 256, 130, 5
+    dh, gu = randn(g, T, F).to(BF), randn(g, T, 2 * F).to(BF)
+    clean = nv.nvfp4_gated_backward(dh.cuda(), gu.cuda(), act=act, recompute_h=True, keep_bf16=True)
+    (dh if where == "dh" else gu)[t, f + (F if where == "up" else 0)] = math.nan
+    bad = nv.nvfp4_gated_backward(dh.cuda(), gu.cuda(), act=act, recompute_h=True, keep_bf16=True)
+    in_dg, in_du, in_h = True, where != "up", where != "dh"
+    say(act, where)
+    places = {f: in_dg, F + f: in_du}
+    nan = torch.zeros((T, 2 * F), dtype=torch.bool)
+    for column, is_nan in places.items():
+        nan[t, column] = is_nan
+    d, d_clean = bad[3].cpu(), clean[3].cpu()
+    assert torch.equal(torch.isnan(d), nan) and torch.equal(d[~nan], d_clean[~nan])
+    for q, c, blocks in ((bad[0], clean[0], [(t, column // 128) for column, n in places.items() if n]),
+                         (bad[1], clean[1], [(column, t // 128) for column, n in places.items() if n]),
+                         (bad[2], clean[2], [(f, t // 128)] if in_h else [])):
+        want = raw(c)[1].clone()
+        for at in blocks:
+            want[at] = 255
+        assert torch.equal(raw(q)[1], want), "scales"
+        spread = (want == 255).repeat_interleave(128, 1)[:, : q.K]
+        assert torch.isnan(values(q)[spread]).all() and torch.equal(raw(q)[0][~spread], raw(c)[0][~spread])
+
+
+@pytest.mark.parametrize("M", [3, 80])
+@pytest.mark.parametrize("act", ACTS)
+@pytest.mark.parametrize("half", ["gate", "up"])
+def test_nan_in_the_forward_pass(act, half, M):
+    """A NaN code of one row of W makes that column of the gate (or the up projection) NaN, and with it h; its block's scales are 255."""
+    g = gen(M)
+    F, K, f = 256, 272, 133
+    A = nv.nvfp4_e4m3_quantize(randn(g, M, K).to(BF).cuda())
+    W = nv.nvfp4_e4m3_quantize_2d(randn(g, 2 * F, K).to(BF).cuda(), transposed=False)[0]
+    clean = nv.nvfp4_e4m3_gemm_gated(A, W, act=act, keep_h=True, keep_gate_up=True)
+    codes = W.codes.view(torch.uint8).clone()
+    codes[f + (F if half == "up" else 0), 7] = 0x7F
+    q, h, gu = nv.nvfp4_e4m3_gemm_gated(A, nv.E4M3Tensor(codes, W.scales), act=act, keep_h=True, keep_gate_up=True)
+    say(act, half, M)
+    keep, keep2 = torch.arange(F) != f, torch.arange(2 * F) != f + (F if half == "up" else 0)
+    assert torch.isnan(h[:, f]).all() and torch.equal(h.cpu()[:, keep], clean[1].cpu()[:, keep])
+    assert torch.isnan(gu.cpu()[:, ~keep2]).all() and torch.equal(gu.cpu()[:, keep2], clean[2].cpu()[:, keep2])
+    s, want = raw(q)[1], raw(clean[0])[1].clone()
+    want[:, f // 128] = 255
+    assert torch.equal(s, want) and torch.isnan(values(q)[:, 128:]).all() and torch.equal(raw(q)[0][:, :128], raw(clean[0])[0][:, :128])
