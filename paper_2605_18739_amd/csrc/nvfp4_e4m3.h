@@ -104,17 +104,6 @@ __device__ __forceinline__ uint32_t absmax8_bits(uint4v v)
 // ---- activations of gated layers, in fp32 to about an ulp ---------------------------------------------------------
 constexpr int kActSilu = 2, kActGelu = 1;                       // (NVFP4_ACT_*)
 
-// 1 / (1 + exp(-x)); zero below -87, where it leaves the normal numbers.  The exponent to base two is taken in two parts: one
-// rounded product would cost |x| / 2 ulps.
-__device__ __forceinline__ float sigmoid_f32(float x)
-{
-    constexpr float kLog2e = 1.44269504f, kLog2eLow = 1.92596299e-8f, kLn2 = 0.693147182f;
-    const float y = fminf(-x, 87.0f), t = y * kLog2e, low = __builtin_fmaf(y, kLog2eLow, __builtin_fmaf(y, kLog2e, -t));
-    float e = __builtin_amdgcn_exp2f(t);
-    e = __builtin_fmaf(e * low, kLn2, e);
-    const float d = 1.0f + e, r = __builtin_amdgcn_rcpf(d), s = __builtin_fmaf(r, __builtin_fmaf(-d, r, 1.0f), r);
-    return x < -87.0f ? 0.0f : s;
-}
 // v between two bounds; NaN where v is (v_med3_f32 and the older minima and maxima would give a bound)
 __device__ __forceinline__ float clamped(float v, float lo, float hi)
 {
@@ -124,6 +113,21 @@ __device__ __forceinline__ float clamped(float v, float lo, float hi)
     return v + lo + hi;
 #endif
 }
+// Where the sigmoid is no constant in fp32: it is zero below -87, where it leaves the normal numbers, and one above 104.  (Of a number
+// far outside the exponent to base two overflows, and what its rounding drops is infinite.)
+__device__ __forceinline__ float sigmoid_within(float x) { return clamped(x, -87.0f, 104.0f); }
+// 1 / (1 + exp(-x)), `within` being sigmoid_within(x).  The exponent to base two is taken in two parts: one rounded product would
+// cost |x| / 2 ulps.
+__device__ __forceinline__ float sigmoid_f32(float x, float within)
+{
+    constexpr float kLog2e = 1.44269504f, kLog2eLow = 1.92596299e-8f, kLn2 = 0.693147182f;
+    const float y = -within, t = y * kLog2e, low = __builtin_fmaf(y, kLog2eLow, __builtin_fmaf(y, kLog2e, -t));
+    float e = __builtin_amdgcn_exp2f(t);
+    e = __builtin_fmaf(e * low, kLn2, e);
+    const float d = 1.0f + e, r = __builtin_amdgcn_rcpf(d), s = __builtin_fmaf(r, __builtin_fmaf(-d, r, 1.0f), r);
+    return x < -87.0f ? 0.0f : s;
+}
+__device__ __forceinline__ float sigmoid_f32(float x) { return sigmoid_f32(x, sigmoid_within(x)); }
 // GELU in its tanh form is x sigmoid(z), z = 2 sqrt(2 / pi) (x + 0.044715 x^3).  Beyond 16 the sigmoid is 0 or 1 for good.
 constexpr float kGelu1 = 1.59576912f, kGelu3 = 0.0713548163f;   // z = x (kGelu1 + kGelu3 x^2)
 __device__ __forceinline__ float gelu_within(float x) { return clamped(x, -16.0f, 16.0f); }
@@ -136,13 +140,14 @@ __device__ __forceinline__ float activation(float x)
         return x * sigmoid_f32(c * __builtin_fmaf(kGelu3, c * c, kGelu1));
     }
 }
-// act(x), and its derivative: sigmoid + x sigmoid (1 - sigmoid) z'
+// act(x), and its derivative: sigmoid + x sigmoid (1 - sigmoid) z'.  (At an infinity the derivative is its limit; act(-infinity) is
+// NaN, as -infinity times zero is.)
 template <int ACT>
 __device__ __forceinline__ float activation(float x, float &slope)
 {
     if constexpr (ACT == kActSilu) {
-        const float s = sigmoid_f32(x);
-        slope = s * __builtin_fmaf(x, 1.0f - s, 1.0f);
+        const float c = sigmoid_within(x), s = sigmoid_f32(x, c);
+        slope = s * __builtin_fmaf(c, 1.0f - s, 1.0f);
         return x * s;
     } else {
         const float c = gelu_within(x), c2 = c * c, s = sigmoid_f32(c * __builtin_fmaf(kGelu3, c2, kGelu1));

@@ -64,3 +64,45 @@ def test_nan_in_the_forward_pass(act, half, M):
     s, want = raw(q)[1], raw(clean[0])[1].clone()
     want[:, f // 128] = 255
     assert torch.equal(s, want) and torch.isnan(values(q)[:, 128:]).all() and torch.equal(raw(q)[0][:, :128], raw(clean[0])[0][:, :128])
+
+
+@pytest.mark.parametrize("M", [2, 70])
+@pytest.mark.parametrize("act", ACTS)
+def test_gates_at_the_end_of_the_range(act, M):
+    """Gates of +-1.75 * 2^127 and +-infinity times a small up value: a finite gate gives h = g u or zero, +infinity infinity; -infinity
+    is NaN, as it is times the sigmoid's zero."""
+    F, K = 16, 16
+    v = torch.zeros((2 * F, K))
+    v[:F, 0] = torch.where(torch.arange(F) % 2 == 0, 1.75, -1.75)
+    v[F:, 0] = 1.0
+    e = torch.tensor([67] * F + [-120] * F)                                     # gate rows times 2^67, up rows times 2^-120
+    W = nv.E4M3Tensor(v.to(E4M3).cuda(), (e + 127).to(torch.uint8).view(2 * F, 1).view(E8M0).cuda())
+    A = nv.E4M3Tensor(torch.nn.functional.pad(torch.ones((M, 1)), (0, K - 1)).to(E4M3).cuda(),
+                      (torch.where(torch.arange(M) % 2 == 0, 60, 64) + 127).to(torch.uint8).view(M, 1).view(E8M0).cuda())
+    y = values(A) @ values(W).T
+    gate = y[:, :F].float().double()                                            # (2^131 is infinite in 32 bits)
+    assert torch.isinf(gate[1::2]).all() and (gate[::2].abs() == 1.75 * 2.0 ** 127).all()
+    q, h, _ = nv.nvfp4_e4m3_gemm_gated(A, W, act=act, keep_h=True)
+    h, want = h.cpu(), act_ref(act, gate)[0] * y[:, F:]
+    say(act, M)
+    assert torch.equal(torch.isnan(h), torch.isnan(want))
+    assert torch.equal(h[0::2].double(), want[0::2]) and torch.isposinf(h[1::2, 0::2]).all() and torch.isnan(h[1::2, 1::2]).all()      # (seven bits: exact)
+    assert (raw(q)[1][1::2] == 255).all() and torch.equal(values(q)[0::2], want[0::2])
+
+
+@pytest.mark.parametrize("act", ACTS)
+def test_gradients_at_the_end_of_the_range(act):
+    """act' is one above and zero below what the exponentials take, up to the infinities, and act is g or zero."""
+    gates = torch.tensor([2.0 ** 127, 3.2e38, 2.4e38, 2.2e38, 1e30, 500.0, 105.0, 104.0, math.inf, -math.inf, -3.2e38, -2.2e38, -1e30, -500.0, -105.0, -88.0]).to(BF)
+    T, F = 5, 16
+    g = gen(3)
+    dh, up = (1e-3 * (1 + torch.rand((T, F), generator=g))).to(BF), randn(g, T, F).to(BF)
+    d = nv.nvfp4_gated_backward(dh.cuda(), torch.cat([gates.expand(T, F), up], 1).contiguous().cuda(), act=act, quantize=False, keep_bf16=True)[3].cpu().double()
+    positive = gates.double() > 0
+    slope, a = positive.double(), torch.where(positive, gates.double(), 0.0)
+    a[9] = math.nan                                                             # -infinity times zero
+    want = torch.cat([dh.double() * up.double() * slope, dh.double() * a], 1)
+    # two products in 32 bits (2^-23 in all) and one rounding to bf16; below -87 the activation is taken as zero (at most 1.44e-36)
+    assert torch.equal(torch.isnan(d), torch.isnan(want))
+    same = torch.isinf(want) & (d == want) | torch.isnan(want)
+    assert (same | ((d - want).abs() <= (2.0 ** -8 + 2.0 ** -22) * want.abs() + 1.5e-36)).all()
