@@ -101,10 +101,15 @@ __device__ __forceinline__ uint32_t absmax8_bits(uint4v v)
     return pk_hmax_u16(pk_absmax_u16(pk_absmax_u16(pk_absmax_u16(pk_absmax_u16(0u, v.x), v.y), v.z), v.w)) << 16;
 }
 
-// ---- activations of gated layers, in fp32 to about an ulp ---------------------------------------------------------
+// ---- activations of gated layers ------------------------------------------------------------------------------------
+// In fp32, u = 2^-24 (these steps with correctly rounded exponentials and reciprocals, over 10^6 gates): act within 4 u of itself, down
+// to where its sigmoid leaves the normal numbers (about e^-87) and is taken as zero; the derivative within 4 u (GELU) and 16 u (SiLU: around
+// 16, where 1 - s is the difference of nearly equal numbers).
 constexpr int kActSilu = 2, kActGelu = 1;                       // (NVFP4_ACT_*)
 
-// v between two bounds; NaN where v is (v_med3_f32 and the older minima and maxima would give a bound)
+// v between two bounds; a bound where v is NaN
+__device__ __forceinline__ float bounded(float v, float lo, float hi) { return __builtin_amdgcn_fmed3f(v, lo, hi); }
+// ... and NaN there, at one instruction more
 __device__ __forceinline__ float clamped(float v, float lo, float hi)
 {
 #if defined(__HIP_DEVICE_COMPILE__)
@@ -113,31 +118,42 @@ __device__ __forceinline__ float clamped(float v, float lo, float hi)
     return v + lo + hi;
 #endif
 }
-// Where the sigmoid is no constant in fp32: it is zero below -87, where it leaves the normal numbers, and one above 104.  (Of a number
-// far outside the exponent to base two overflows, and what its rounding drops is infinite.)
-__device__ __forceinline__ float sigmoid_within(float x) { return clamped(x, -87.0f, 104.0f); }
-// 1 / (1 + exp(-x)), `within` being sigmoid_within(x).  The exponent to base two is taken in two parts: one rounded product would
-// cost |x| / 2 ulps.
+// 1 / (1 + exp(-x)), `within` being x between these: the sigmoid is zero below, where it leaves the normal numbers, and one above.  (Of a
+// number far outside the exponent to base two overflows, and what its rounding drops is infinite.)  The exponent comes in two parts:
+// one rounded product x log2(e) would cost |x| / 2 ulps.
+constexpr float kSigmoidLow = -87.0f, kSigmoidHigh = 104.0f, kLn2 = 0.693147182f;
 __device__ __forceinline__ float sigmoid_f32(float x, float within)
 {
-    constexpr float kLog2e = 1.44269504f, kLog2eLow = 1.92596299e-8f, kLn2 = 0.693147182f;
+    constexpr float kLog2e = 1.44269504f, kLog2eLow = 1.92596299e-8f;
     const float y = -within, t = y * kLog2e, low = __builtin_fmaf(y, kLog2eLow, __builtin_fmaf(y, kLog2e, -t));
     float e = __builtin_amdgcn_exp2f(t);
     e = __builtin_fmaf(e * low, kLn2, e);
     const float d = 1.0f + e, r = __builtin_amdgcn_rcpf(d), s = __builtin_fmaf(r, __builtin_fmaf(-d, r, 1.0f), r);
-    return x < -87.0f ? 0.0f : s;
+    return x < kSigmoidLow ? 0.0f : s;
 }
-__device__ __forceinline__ float sigmoid_f32(float x) { return sigmoid_f32(x, sigmoid_within(x)); }
-// GELU in its tanh form is x sigmoid(z), z = 2 sqrt(2 / pi) (x + 0.044715 x^3).  Beyond 16 the sigmoid is 0 or 1 for good.
-constexpr float kGelu1 = 1.59576912f, kGelu3 = 0.0713548163f;   // z = x (kGelu1 + kGelu3 x^2)
-__device__ __forceinline__ float gelu_within(float x) { return clamped(x, -16.0f, 16.0f); }
+// GELU in its tanh form is x sigmoid(z), z = 2 sqrt(2 / pi) (x + 0.044715 x^3) = x (kGelu1 + kGelu3 x^2).  Beyond kGeluEnd the sigmoid is
+// 0 or 1 for good.  For negative z it is about e^z, which turns z's relative error into |z| times as much (an fp32 z: 80 u at -7, 200 u
+// at -10).  So the exponent to base two, -z log2(e) = -c p, p = K1 + K3 c^2, carries what each step drops: c^2's remainder, p's (the upper
+// part of K1 has twelve bits: p - K1 is exact, whichever of the two terms is larger) and the product's.
+constexpr float kGelu1 = 1.59576912f, kGelu3 = 0.0713548163f, kGeluEnd = 16.0f;
+// sigmoid(z) at c (within kGeluEnd), c2 = c^2; e = e^-z, which may be infinite: the reciprocal is zero then (a step after it would be NaN)
+__device__ __forceinline__ float gelu_sigmoid(float c, float c2, float &e)
+{
+    constexpr float kUp1 = 2.30224609375f, kLow1 = -3.7895606510574e-05f, kUp3 = 0.10294324159622192f, kLow3 = -2.016198319410023e-09f;     // 2 sqrt(2 / pi) log2(e), and 0.044715 of it
+    const float p = __builtin_fmaf(kUp3, c2, kUp1), p_low = __builtin_fmaf(kUp3, c2, kUp1 - p) + __builtin_fmaf(kLow3, c2, kLow1);
+    const float rest = __builtin_fmaf(kUp3, __builtin_fmaf(c, c, -c2), p_low), t = -c * p, minus_low = __builtin_fmaf(c, rest, __builtin_fmaf(c, p, t));
+    e = __builtin_amdgcn_exp2f(t) * __builtin_fmaf(minus_low, -kLn2, 1.0f);
+    return __builtin_amdgcn_rcpf(1.0f + e);
+}
+// act(x).  (A NaN that the bounds take away comes back with the factor x.)
 template <int ACT>
 __device__ __forceinline__ float activation(float x)
 {
-    if constexpr (ACT == kActSilu) return x * sigmoid_f32(x);
+    if constexpr (ACT == kActSilu) return x * sigmoid_f32(x, bounded(x, kSigmoidLow, kSigmoidHigh));
     else {
-        const float c = gelu_within(x);
-        return x * sigmoid_f32(c * __builtin_fmaf(kGelu3, c * c, kGelu1));
+        float e;
+        const float c = bounded(x, -kGeluEnd, kGeluEnd);
+        return x * gelu_sigmoid(c, c * c, e);
     }
 }
 // act(x), and its derivative: sigmoid + x sigmoid (1 - sigmoid) z'.  (At an infinity the derivative is its limit; act(-infinity) is
@@ -146,12 +162,13 @@ template <int ACT>
 __device__ __forceinline__ float activation(float x, float &slope)
 {
     if constexpr (ACT == kActSilu) {
-        const float c = sigmoid_within(x), s = sigmoid_f32(x, c);
+        const float c = clamped(x, kSigmoidLow, kSigmoidHigh), s = sigmoid_f32(x, c);
         slope = s * __builtin_fmaf(c, 1.0f - s, 1.0f);
         return x * s;
     } else {
-        const float c = gelu_within(x), c2 = c * c, s = sigmoid_f32(c * __builtin_fmaf(kGelu3, c2, kGelu1));
-        slope = __builtin_fmaf(c * s, (1.0f - s) * __builtin_fmaf(3.0f * kGelu3, c2, kGelu1), s);
+        float e;
+        const float c = clamped(x, -kGeluEnd, kGeluEnd), c2 = c * c, s = gelu_sigmoid(c, c2, e);
+        slope = __builtin_fmaf(c * s, fminf(e, 1e38f) * s * __builtin_fmaf(3.0f * kGelu3, c2, kGelu1), s);      // (1 - s = e s; s is zero where e is infinite)
         return x * s;
     }
 }

@@ -363,6 +363,14 @@ __global__ __launch_bounds__(256) void e4m3_gemm_kernel(const E4m3GemmArgs g)
         constexpr int kRow = 144;
         static_for<0, TM>([&](auto j_c) {
             constexpr int j = decltype(j_c)::value;
+            // Of 256 accumulators those of the bands behind this one stay where the matrix instructions left them: taken over all at once,
+            // 32 of them went to scratch memory and came back one by one, each a wait behind the stores (3 to 5 us a tile).
+            if constexpr (NMF * 16 >= 256) {
+#pragma unroll
+                for (int jj = j + 1; jj < TM; ++jj)
+#pragma unroll
+                    for (int i = 0; i < TN; ++i) asm volatile("" : "+a"(acc[i][jj]));
+            }
             if (g.gate_up) {
                 store_bf16(j_c, std::integral_constant<int, 0>(), g.gate_up, g.ld_gate_up, 0, g.N);
                 store_bf16(j_c, std::integral_constant<int, TF>(), g.gate_up, g.ld_gate_up, g.N, g.N);

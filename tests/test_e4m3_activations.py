@@ -106,3 +106,59 @@ def test_gradients_at_the_end_of_the_range(act):
     assert torch.equal(torch.isnan(d), torch.isnan(want))
     same = torch.isinf(want) & (d == want) | torch.isnan(want)
     assert (same | ((d - want).abs() <= (2.0 ** -8 + 2.0 ** -22) * want.abs() + 1.5e-36)).all()
+
+
+def assert_rounded(got, want, err, what):
+    """Every bf16 number is the rounding of something within err of want: off by a rounding elsewhere does not hide what is off here."""
+    low, high = (want - err).float().to(BF).double(), (want + err).float().to(BF).double()
+    out = (got < low) | (got > high)
+    assert not out.any(), f"{what}: {int(out.sum())} of {out.numel()} numbers round to something else, the first at {out.nonzero()[0].tolist()}"
+
+
+def negative_gates(g, M, F):
+    """Operands whose gates are sums of exact products, all over (-10, 0), and whose up values are one."""
+    K, terms = 16, 6
+    a, w = torch.zeros((M, K)), torch.zeros((2 * F, K))
+    a[:, 0] = -torch.randint(8, 16, (M,), generator=g) / 8 * torch.exp2(torch.randint(-2, 3, (M,), generator=g).float())
+    w[:F, 0] = torch.randint(8, 16, (F,), generator=g) / 8
+    a[:, 1 : 1 + terms] = torch.randint(8, 16, (M, terms), generator=g) / 512
+    w[:F, 1 : 1 + terms] = torch.randint(-15, 16, (F, terms), generator=g) / 32
+    a[:, 15] = w[F:, 15] = 1.0
+    one = lambda v: nv.E4M3Tensor(v.to(E4M3).cuda(), torch.full((v.shape[0], 1), 127, dtype=torch.uint8).view(E8M0).cuda())
+    assert (a.to(E4M3).float() == a).all() and (w.to(E4M3).float() == w).all()
+    return one(a), one(w)
+
+
+@pytest.mark.parametrize("M", [50, 900])
+@pytest.mark.parametrize("act", ACTS)
+def test_small_activations(act, M):
+    """The activation of negative gates, which is about g e^z, relative to itself.  An error of z counts |z| times there, so z may not be
+    a rounded number: e^z within 2 u of the hardware's and 2 u of its exponent's parts and the product with them, a sum, a reciprocal
+    and a product 4 u, and the roundings of this test's bounds to fp32: 9 u."""
+    A, W = negative_gates(gen(M), M, 384)
+    y = values(A) @ values(W).T
+    assert (y.float().double() == y).all() and (y[:, 384:] == 1).all()
+    gate = y[:, :384]
+    h = nv.nvfp4_e4m3_gemm_gated(A, W, act=act, quantize=False, keep_h=True)[1].cpu().double()
+    want = act_ref(act, gate)[0]
+    say(act, M, "gates", float(gate.min()), float(gate.max()), "below -3:", int((gate < -3).sum()))
+    inside = gate > -9.8                                                        # (further down the sigmoid of GELU leaves the normal numbers)
+    assert_rounded(h[inside], want[inside], 9 * U * want[inside].abs(), "act")
+
+
+@pytest.mark.parametrize("act", ACTS)
+def test_gradients_of_small_activations(act):
+    """As above for du = dh act(g): one product more, 10 u; and dg = dh u act'(g), act' = s + g s (1 - s) z': s and 1 - s within 6 u of
+    themselves (SiLU: 1 - s within 6 u of s), z' 2 u, six products and a sum: 16 u of the sum of its terms' magnitudes."""
+    g = gen(7)
+    T, F = 700, 384
+    gate = (-9.8 * torch.rand((T, F), generator=g)).to(BF)
+    dh, up = randn(g, T, F).to(BF), randn(g, T, F).to(BF)
+    d = nv.nvfp4_gated_backward(dh.cuda(), torch.cat([gate, up], 1).cuda(), act=act, quantize=False, keep_bf16=True)[3].cpu().double()
+    gate, dh, up = gate.double(), dh.double(), up.double()
+    a, slope = act_ref(act, gate)
+    s = torch.sigmoid(gate if act == nv.ACT_SILU else math.sqrt(8 / math.pi) * (gate + 0.044715 * gate ** 3))
+    inner = 1.0 if act == nv.ACT_SILU else math.sqrt(8 / math.pi) * (1 + 0.134145 * gate ** 2)
+    say(act)
+    assert_rounded(d[:, F:], dh * a, 10 * U * (dh * a).abs(), "du")
+    assert_rounded(d[:, :F], dh * up * slope, 16 * U * (dh * up).abs() * s * (1 + gate.abs() * inner), "dg")
