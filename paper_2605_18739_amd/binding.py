@@ -224,7 +224,7 @@ def _on(stream, call, *args):
         result = call(*args)
     for new in result if isinstance(result, tuple) else () if isinstance(result, NVFP4KvCache) else (result,):
         if new is not None and not any(new is a for a in args):
-            for t in (new.codes, new.scales, new.global_scale) if isinstance(new, NVFP4Tensor) else new._native if isinstance(new, E4M3Tensor) else (new,):
+            for t in (new.codes, new.scales, new.global_scale) if isinstance(new, NVFP4Tensor) else (new.codes, new.scales) if isinstance(new, E4M3Tensor) else (new,):
                 t.record_stream(here)
     return result
 
@@ -567,7 +567,8 @@ def nvfp4_kv_attention(q, cache, page_table, kv_lens, q_starts, max_q, softmax_s
 
 class E4M3Tensor:
     """8-bit tensor (see include/nvfp4.h): codes float8_e4m3fn [rows, K], scales float8_e8m0fnu for 128 elements of a row
-    [rows, ceil(K / 128)] or for 128 x 128 [ceil(rows / 128), ceil(K / 128)]; contiguous (uint8 is taken for either type)."""
+    [rows, ceil(K / 128)] or for 128 x 128 [ceil(rows / 128), ceil(K / 128)]; contiguous (uint8 is taken for either type).
+    Both may be assigned; a call takes and checks what they are then."""
 
     def __init__(self, codes, scales):
         if codes.dim() != 2:
@@ -577,14 +578,11 @@ class E4M3Tensor:
         assert scales.dtype in (torch.float8_e8m0fnu, torch.uint8) and scales.is_contiguous(), "scales: expected a contiguous float8_e8m0fnu matrix"
         blocks = -(-K // E4M3_BLOCK)
         assert tuple(scales.shape) in ((rows, blocks), (-(-rows // E4M3_BLOCK), blocks)), "scales: expected one for 128 elements of a row, or for 128 x 128"
-        self._set(codes, scales)
-
-    def _set(self, codes, scales):
         self.codes, self.scales = codes, scales
-        self.rows, self.K = codes.shape
-        self.block_rows = 1 if scales.shape[0] == self.rows else E4M3_BLOCK
-        self._native = (codes, scales)
-        return self
+
+    rows = property(lambda self: self.codes.shape[0])
+    K = property(lambda self: self.codes.shape[1])
+    block_rows = property(lambda self: 1 if self.scales.shape[0] == self.codes.shape[0] else E4M3_BLOCK)
 
     @staticmethod
     def empty(rows, K, block_rows=1, device="cuda"):
@@ -597,13 +595,13 @@ class E4M3Tensor:
         return _CE4m3Tensor(self.codes.data_ptr(), self.scales.data_ptr(), self.rows, self.K, self.block_rows)
 
 
-def _native(t):
-    return None if t is None else t._native
-
-
 def _tensor8(given, codes, scales):
     """The caller's tensor, or the new one of a call (None: neither)."""
-    return given if codes is None else E4M3Tensor.__new__(E4M3Tensor)._set(codes, scales)
+    if codes is None:
+        return given
+    t = E4M3Tensor.__new__(E4M3Tensor)
+    t.codes, t.scales = codes, scales
+    return t
 
 
 def nvfp4_e4m3_quantize(x, block_axis=0, out=None, stream=None):
@@ -611,7 +609,7 @@ def nvfp4_e4m3_quantize(x, block_axis=0, out=None, stream=None):
     along R and transposed (block_axis 1: [C, R rounded up to 16]).  Returns an E4M3Tensor."""
     if stream is not None and _elsewhere(stream):
         return _on(stream, nvfp4_e4m3_quantize, x, block_axis, out)
-    rc, codes, scales = _host().e4m3_quantize(x, block_axis, _native(out), _stream(stream))
+    rc, codes, scales = _host().e4m3_quantize(x, block_axis, out, _stream(stream))
     _check(rc)
     return _tensor8(out, codes, scales)
 
@@ -620,7 +618,7 @@ def nvfp4_e4m3_quantize_2d(w, transposed=True, out=None, out_t=None, stream=None
     """w: bf16 [R, C] weights (R, C multiples of 16), one scale per 128 x 128.  Returns (E4M3Tensor [R, C], E4M3Tensor [C, R] or None)."""
     if stream is not None and _elsewhere(stream):
         return _on(stream, nvfp4_e4m3_quantize_2d, w, transposed, out, out_t)
-    rc, codes, scales, codes_t, scales_t = _host().e4m3_quantize_2d(w, 1 if transposed else 0, _native(out), _native(out_t), _stream(stream))
+    rc, codes, scales, codes_t, scales_t = _host().e4m3_quantize_2d(w, 1 if transposed else 0, out, out_t, _stream(stream))
     _check(rc)
     return _tensor8(out, codes, scales), _tensor8(out_t, codes_t, scales_t)
 
@@ -630,7 +628,7 @@ def nvfp4_e4m3_gemm(A, W, out_dtype=OUT_F32, Y=None, fast_sums=False, stream=Non
     fast_sums: at about twice the rate, with sums of eight products that keep 13 bits below the largest (see include/nvfp4.h)."""
     if stream is not None and _elsewhere(stream):
         return _on(stream, nvfp4_e4m3_gemm, A, W, out_dtype, Y, fast_sums)
-    rc, new = _host().e4m3_gemm(A._native, W._native, out_dtype, Y, 1 if fast_sums else 0, _stream(stream))
+    rc, new = _host().e4m3_gemm(A, W, out_dtype, Y, 1 if fast_sums else 0, _stream(stream))
     _check(rc)
     return Y if new is None else new
 
@@ -642,8 +640,8 @@ def nvfp4_e4m3_gemm_gated(A, W, act=ACT_SILU, quantize=True, keep_h=False, keep_
     fast_sums: as in nvfp4_e4m3_gemm."""
     if stream is not None and _elsewhere(stream):
         return _on(stream, nvfp4_e4m3_gemm_gated, A, W, act, quantize, keep_h, keep_gate_up, out, h, gate_up, workspace, fast_sums)
-    rc, codes, scales, new_h, new_gate_up = _host().e4m3_gemm_gated(A._native, W._native, act, 1 if quantize else 0, 1 if keep_h else 0, 1 if keep_gate_up else 0,
-                                                                    _native(out), h, gate_up, workspace, 1 if fast_sums else 0, _stream(stream))
+    rc, codes, scales, new_h, new_gate_up = _host().e4m3_gemm_gated(A, W, act, 1 if quantize else 0, 1 if keep_h else 0, 1 if keep_gate_up else 0,
+                                                                    out, h, gate_up, workspace, 1 if fast_sums else 0, _stream(stream))
     _check(rc)
     return _tensor8(out, codes, scales), h if new_h is None else new_h, gate_up if new_gate_up is None else new_gate_up
 
@@ -654,7 +652,7 @@ def nvfp4_gated_backward(dh, gate_up, act=ACT_SILU, quantize=True, recompute_h=F
     if stream is not None and _elsewhere(stream):
         return _on(stream, nvfp4_gated_backward, dh, gate_up, act, quantize, recompute_h, keep_bf16, out, out_t, h_t, d)
     rc, codes, scales, codes_t, scales_t, h_codes, h_scales, new_d = _host().gated_backward(
-        dh, gate_up, act, 1 if quantize else 0, 1 if recompute_h else 0, 1 if keep_bf16 else 0, _native(out), _native(out_t), _native(h_t), d, _stream(stream))
+        dh, gate_up, act, 1 if quantize else 0, 1 if recompute_h else 0, 1 if keep_bf16 else 0, out, out_t, h_t, d, _stream(stream))
     _check(rc)
     return _tensor8(out, codes, scales), _tensor8(out_t, codes_t, scales_t), _tensor8(h_t, h_codes, h_scales), d if new_d is None else new_d
 
@@ -665,7 +663,7 @@ def nvfp4_rms_norm(x, weight, residual=None, eps=1e-6, quantize=True, keep_bf16=
     given as x or residual itself)."""
     if stream is not None and _elsewhere(stream):
         return _on(stream, nvfp4_rms_norm, x, weight, residual, eps, quantize, keep_bf16, out, y, sum)
-    rc, codes, scales, new_y, new_sum = _host().rms_norm(x, weight, residual, eps, 1 if quantize else 0, 1 if keep_bf16 else 0, _native(out), y, sum, _stream(stream))
+    rc, codes, scales, new_y, new_sum = _host().rms_norm(x, weight, residual, eps, 1 if quantize else 0, 1 if keep_bf16 else 0, out, y, sum, _stream(stream))
     _check(rc)
     return _tensor8(out, codes, scales), y if new_y is None else new_y, sum if new_sum is None else new_sum
 

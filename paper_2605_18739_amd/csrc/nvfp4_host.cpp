@@ -614,7 +614,8 @@ PyObject *kv_attention(PyObject *const *a)
 }
 
 // ---- 8-bit operands -----------------------------------------------------------------------------------
-// the pair that an E4M3Tensor keeps: codes, scales; or a new one
+// an E4M3Tensor as it is at the time of the call, or a new one.  (Its tensors may have been assigned or changed in place since it was
+// made, so what it checked then is checked here: the kernels go by the shapes.)
 struct Bytes8 {
     nvfp4_e4m3_tensor t{};
     at::Tensor codes, scales;
@@ -622,9 +623,16 @@ struct Bytes8 {
     Bytes8() = default;                                               // none
     Bytes8(const OnDevice &on, PyObject *o)
     {
-        if (!PyTuple_Check(o) || PyTuple_GET_SIZE(o) != 2) fail(PyExc_TypeError, "expected an E4M3Tensor");
-        codes = on(tensor(PyTuple_GET_ITEM(o, 0)));                   // (shapes, types and strides: checked once, by the E4M3Tensor)
-        scales = on(tensor(PyTuple_GET_ITEM(o, 1)));
+        buffer(o, s_codes, codes);
+        buffer(o, s_scales, scales);
+        on(codes), on(scales);
+        require((codes.scalar_type() == at::kFloat8_e4m3fn || codes.scalar_type() == at::kByte) && codes.dim() == 2 && codes.is_contiguous(),
+                "codes: expected a contiguous float8_e4m3fn matrix");
+        require((scales.scalar_type() == at::kFloat8_e8m0fnu || scales.scalar_type() == at::kByte) && scales.dim() == 2 && scales.is_contiguous(),
+                "scales: expected a contiguous float8_e8m0fnu matrix");
+        const int64_t rows = codes.size(0), n = scales.size(0);
+        require((n == rows || n == (rows + NVFP4_E4M3_BLOCK - 1) / NVFP4_E4M3_BLOCK) && scales.size(1) == (codes.size(1) + NVFP4_E4M3_BLOCK - 1) / NVFP4_E4M3_BLOCK,
+                "scales: expected one for 128 elements of a row, or for 128 x 128");
         fill();
     }
     // the caller's output, or a new one
@@ -645,6 +653,14 @@ struct Bytes8 {
     nvfp4_e4m3_tensor *c() { return t.codes ? &t : nullptr; }
 
 private:
+    static void buffer(PyObject *o, PyObject *name, at::Tensor &keep)
+    {
+        PyObject *a = attribute(o, name);
+        const bool is = THPVariable_Check(a);
+        if (is) keep = THPVariable_Unpack(a);
+        Py_DECREF(a);
+        if (!is) fail(PyExc_TypeError, "expected an E4M3Tensor");
+    }
     void fill()
     {
         t.codes = static_cast<uint8_t *>(codes.data_ptr());
