@@ -522,6 +522,7 @@ int nvfp4_e4m3_gemm(const nvfp4_e4m3_tensor *A, const nvfp4_e4m3_tensor *W, void
 /*
  * Gated projections in one kernel: with W [2F, K], the gate's F rows in front of the up projection's,
  *   g = A W[0:F]^T,  u = A W[F:2F]^T,  h = act(g) u     (fp32 until h is rounded)
+ * A sigmoid below about e^-87 counts as zero (h is off by at most 1.5e-36 |u| there).  A NaN in g or u makes h NaN, as g = -infinity does.
  * act: NVFP4_ACT_SILU or NVFP4_ACT_GELU_TANH (| NVFP4_SUMS_FAST: sums as in nvfp4_e4m3_gemm).  Results, each of which may be NULL (not all):
  *   out      h in 8 bits along F (rows = M, K = F, block_rows 1; F % 16 == 0), the operand of the down projection
  *   h_bf16   h, [M, F], row stride ld_h
@@ -541,7 +542,8 @@ int nvfp4_e4m3_gemm_gated(const nvfp4_e4m3_tensor *A, const nvfp4_e4m3_tensor *W
  *   h_t     h along the tokens (rows = F, K likewise), for the down projection's weights; from the bf16 g and u
  *   d_bf16  [dg | du] in bf16, row stride ld_d a multiple of 8; may be gate_up itself
  * Each may be NULL (not all); block_rows 1.  F % 8 == 0.  Rounding to 8 bits counts as the identity: the gradients are those
- * of the unquantized h.
+ * of the unquantized h.  act and a NaN are as in nvfp4_e4m3_gemm_gated; act' at an infinity is its limit.  dh u is formed first: pairs
+ * whose product leaves the fp32 range are outside the contract.
  */
 int nvfp4_gated_backward(const void *dh_bf16, int64_t ld_dh, const void *gate_up_bf16, int64_t ld_gate_up, int64_t T, int64_t F, int act,
                          nvfp4_e4m3_tensor *out, nvfp4_e4m3_tensor *out_t, nvfp4_e4m3_tensor *h_t, void *d_bf16, int64_t ld_d, void *stream);
@@ -562,6 +564,7 @@ int nvfp4_rms_norm(const void *x_bf16, int64_t ld, const void *residual_bf16, in
  * itself brings:  r = 1 / sqrt( mean(s^2) + eps ),  xh = r s,
  *   dx = dsum + r ( w dy - xh mean(w dy xh) )  (bf16, rounded once; the gradient of x and of the residual alike; may be dy, s
  *   or dsum itself),   dweight = sum over rows of dy xh (fp32 [C], or NULL; added in a fixed order).
+ * Products w dy s that leave the fp32 range are outside the contract, as squares of s are.
  * workspace: nvfp4_workspace_bytes(NVFP4_OP_RMS_NORM_BACKWARD, T, C, 0) bytes, 16-byte aligned; may be NULL without dweight.
  */
 int nvfp4_rms_norm_backward(const void *dy_bf16, int64_t ld_dy, const void *s_bf16, int64_t ld_s, const void *weight_bf16, const void *dsum_bf16,
