@@ -555,7 +555,7 @@ int nvfp4_gated_backward(const void *dh_bf16, int64_t ld_dh, const void *gate_up
  *   sum_bf16  receives s; given exactly when residual is; may be x or residual itself (same stride)
  *   out       y in 8 bits along C (rows = T, K = C, block_rows 1), or NULL      y_bf16  y in bf16, or NULL (not both)
  * Magnitudes whose squares leave the fp32 range are outside the contract, as is eps below the normal fp32 numbers
- * (NVFP4_ERR_SHAPE).
+ * (NVFP4_ERR_SHAPE).  T <= 2^23 - 1, and above C = 8192 T ceil(C / 1024) <= 2^26 - 1: the rows of one launch.
  */
 int nvfp4_rms_norm(const void *x_bf16, int64_t ld, const void *residual_bf16, int64_t ld_residual, const void *weight_bf16, int64_t T, int64_t C,
                    float eps, void *sum_bf16, int64_t ld_sum, nvfp4_e4m3_tensor *out, void *y_bf16, int64_t ld_y, void *stream);

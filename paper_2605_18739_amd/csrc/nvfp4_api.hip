@@ -276,6 +276,8 @@ int fill_e4m3_gemm(const nvfp4_e4m3_tensor *A, const nvfp4_e4m3_tensor *W, bool 
     g->scale_words = (nb & 3) == 0;
     return NVFP4_OK;
 }
+// (the forward pass launches a workgroup for each row, 64 lanes for 1024 elements; the backward pass goes over the rows)
+bool rms_norm_rows_ok(int64_t T, int64_t C) { return T <= kMaxLanes / (64 * ((C + 1023) / 1024)); }
 int check_rms_norm(int64_t T, int64_t C, float eps)
 {
     if (T <= 0 || T > kMaxLanes / 512 || C <= 0 || C > kRmsNormMaxC || (C & 15) != 0) return NVFP4_ERR_SHAPE;
@@ -939,6 +941,7 @@ int nvfp4_rms_norm(const void *x_bf16, int64_t ld, const void *residual_bf16, in
 {
     if (!weight_bf16 || (!out && !y_bf16)) return NVFP4_ERR_NULL;
     if (int rc = check_rms_norm(T, C, eps)) return rc;
+    if (!rms_norm_rows_ok(T, C)) return NVFP4_ERR_SHAPE;
     if (int rc = check_matrix(x_bf16, ld, C)) return rc;
     if ((residual_bf16 != nullptr) != (sum_bf16 != nullptr)) return NVFP4_ERR_NULL;
     if (residual_bf16) {
