@@ -13,6 +13,7 @@
 #pragma once
 
 #include "nvfp4_e4m3.h"
+#include "nvfp4_e4m3_plan.h"
 #include "nvfp4_gemm_tile.h"
 
 namespace nvfp4 {
@@ -441,14 +442,10 @@ static hipError_t launch_e4m3_shape(E4m3GemmArgs g, hipStream_t s)
     constexpr int BF = KIND >= kE4m3Silu ? BN / 2 : BN;
     g.tiles_m = (int)((g.M + BM - 1) / BM);
     g.tiles_n = (int)((g.N + BF - 1) / BF);
-    if constexpr (BM + BN <= 128) return launch_e4m3_stages<BM, BN, KIND, FAST, 4>(g, s);
-    else if constexpr (BM + BN <= 320) {
-        // a tile to a compute unit: its own copies have to hide the way to memory, so four stages; with more tiles two of them
-        // share a compute unit and its LDS, and hide each other's waits
-        if (g.tiles_m * (int64_t)g.tiles_n <= 256) return launch_e4m3_stages<BM, BN, KIND, FAST, 4>(g, s);
-        return launch_e4m3_stages<BM, BN, KIND, FAST, 2>(g, s);
-    } else if constexpr (FAST && BM + BN <= 384) return launch_e4m3_stages<BM, BN, KIND, FAST, 3>(g, s);     // (4096^3 64 us, with two 70; exact sums: even)
-    else return launch_e4m3_stages<BM, BN, KIND, FAST, 2>(g, s);
+    constexpr int few = e4m3_stages(BM, BN, FAST, 1), many = e4m3_stages(BM, BN, FAST, 1 << 30);
+    if constexpr (few != many)
+        if (e4m3_stages(BM, BN, FAST, g.tiles_m * (int64_t)g.tiles_n) == few) return launch_e4m3_stages<BM, BN, KIND, FAST, few>(g, s);
+    return launch_e4m3_stages<BM, BN, KIND, FAST, many>(g, s);
 }
 
 template <int BM, int BN, bool FAST>

@@ -27,13 +27,15 @@ __device__ __forceinline__ float gated_value(const E4m3GemmArgs &g, int kind, in
 //   v_mfma_f32_16x16x32_bf16 on expanded codes, W as the row operand: lane (r = lane & 15, q = lane >> 4) holds chunks q and q + 4
 //   (16 bytes each) of row r for four instructions.  Chunk c of row r stands at 128 r + 16 (c ^ (r >> 1)): no bank conflicts.
 //   The lane ends up with row m = r of A and columns 4 q .. 4 q + 3.
-template <int MT, bool GATED, int WAVES, int DEPTH>
+constexpr int kFewDepth = 2;                                // slots of a wave's ring
+template <int MT, bool GATED, int WAVES>
 __global__ __launch_bounds__(64 * WAVES) void e4m3_few_rows_kernel(const E4m3GemmArgs g, float *__restrict__ h, int kind)
 {
 #if defined(__HIP_DEVICE_COMPILE__)
     constexpr int NW = GATED ? 2 : 1, NT = NW + MT;         // tiles of 16 rows: of W, of A
     constexpr int SLOT = NT * 2048, P = 2 * NT;             // copies of a block
-    static_assert(DEPTH == 2 || DEPTH == 4, "blocks of a turn go round the ring");
+    constexpr int DEPTH = kFewDepth;
+    static_assert(4 % DEPTH == 0, "the four blocks of a turn go round the ring");
     typedef __attribute__((address_space(3))) void *lds_ptr_t;
     typedef __bf16 bf16x8v __attribute__((ext_vector_type(8)));
     extern __shared__ __attribute__((aligned(16))) uint8_t lds[];
@@ -221,23 +223,21 @@ __global__ __launch_bounds__(256) void e4m3_rows_f32_kernel(const float *__restr
 }
 
 // --------------------------------------------------------------------------
-constexpr int64_t kFewRows = 64;
+size_t e4m3_gated_workspace_bytes(int64_t M, int64_t F) { return M <= kE4m3FewRows ? (size_t)M * (size_t)F * 4 : 0; }
 
-size_t e4m3_gated_workspace_bytes(int64_t M, int64_t F) { return M <= kFewRows ? (size_t)M * (size_t)F * 4 : 0; }
-
-template <int MT, bool GATED, int WAVES, int DEPTH>
+template <int MT, bool GATED, int WAVES>
 static hipError_t launch_few(int kind, const E4m3GemmArgs &g, float *h, hipStream_t s)
 {
-    constexpr int NW = GATED ? 2 : 1, ring = WAVES * DEPTH * (NW + MT) * 2048, sums = WAVES * NW * MT * 1024, smem = ring > sums ? ring : sums;
+    constexpr int NW = GATED ? 2 : 1, ring = WAVES * kFewDepth * (NW + MT) * 2048, sums = WAVES * NW * MT * 1024, smem = ring > sums ? ring : sums;
     static_assert(smem <= 160 * 1024, "LDS");
     static uint64_t attr_set = 0;                           // the dynamic LDS limit is raised once per kernel variant and device
     int dev = 0;
     if (hipError_t e = hipGetDevice(&dev); e != hipSuccess) return e;
     if (((attr_set >> (dev & 63)) & 1u) == 0) {
-        if (hipError_t e = hipFuncSetAttribute((const void *)e4m3_few_rows_kernel<MT, GATED, WAVES, DEPTH>, hipFuncAttributeMaxDynamicSharedMemorySize, smem)) return e;
+        if (hipError_t e = hipFuncSetAttribute((const void *)e4m3_few_rows_kernel<MT, GATED, WAVES>, hipFuncAttributeMaxDynamicSharedMemorySize, smem)) return e;
         attr_set |= 1ull << (dev & 63);
     }
-    e4m3_few_rows_kernel<MT, GATED, WAVES, DEPTH><<<(unsigned)((g.N + 15) / 16), 64 * WAVES, smem, s>>>(g, h, kind);
+    e4m3_few_rows_kernel<MT, GATED, WAVES><<<(unsigned)((g.N + 15) / 16), 64 * WAVES, smem, s>>>(g, h, kind);
     return hipGetLastError();
 }
 
@@ -249,13 +249,13 @@ static hipError_t launch_few_rows(int kind, const E4m3GemmArgs &g, float *h, hip
     const bool many = (g.N + 15) / 16 > 256;
     hipError_t e;
     if (g.M <= 16) {
-        if (gated) e = many ? launch_few<1, true, 4, 2>(kind, g, h, s) : launch_few<1, true, 8, 2>(kind, g, h, s);
-        else e = many ? launch_few<1, false, 4, 2>(kind, g, h, s) : launch_few<1, false, 8, 2>(kind, g, h, s);
+        if (gated) e = many ? launch_few<1, true, 4>(kind, g, h, s) : launch_few<1, true, 8>(kind, g, h, s);
+        else e = many ? launch_few<1, false, 4>(kind, g, h, s) : launch_few<1, false, 8>(kind, g, h, s);
     } else if (g.M <= 32) {
-        if (gated) e = many ? launch_few<2, true, 4, 2>(kind, g, h, s) : launch_few<2, true, 8, 2>(kind, g, h, s);
-        else e = many ? launch_few<2, false, 4, 2>(kind, g, h, s) : launch_few<2, false, 8, 2>(kind, g, h, s);
-    } else if (gated) e = many ? launch_few<4, true, 2, 2>(kind, g, h, s) : launch_few<4, true, 4, 2>(kind, g, h, s);
-    else e = many ? launch_few<4, false, 2, 2>(kind, g, h, s) : launch_few<4, false, 4, 2>(kind, g, h, s);
+        if (gated) e = many ? launch_few<2, true, 4>(kind, g, h, s) : launch_few<2, true, 8>(kind, g, h, s);
+        else e = many ? launch_few<2, false, 4>(kind, g, h, s) : launch_few<2, false, 8>(kind, g, h, s);
+    } else if (gated) e = many ? launch_few<4, true, 2>(kind, g, h, s) : launch_few<4, true, 4>(kind, g, h, s);
+    else e = many ? launch_few<4, false, 2>(kind, g, h, s) : launch_few<4, false, 4>(kind, g, h, s);
     if (e) return e;
     if (!h) return hipSuccess;
     const int64_t nb = (g.N + 127) / 128, blocks = g.M * nb;
@@ -265,25 +265,10 @@ static hipError_t launch_few_rows(int kind, const E4m3GemmArgs &g, float *h, hip
 
 hipError_t launch_e4m3_gemm(int kind, const E4m3GemmArgs &g, void *workspace, hipStream_t s)
 {
-    if (g.M <= kFewRows) return launch_few_rows(kind, g, g.codes ? static_cast<float *>(workspace) : nullptr, s);
-    const bool gated = kind >= kE4m3Silu;
-    // The shape whose rounds of tiles over the 256 compute units take least, by the time of a step (128 k) of a full round, ns:
-    // 4096^3 takes exact 105 / 117 / 106 / 112 / 118 / 160 us with the shapes in this order, fast 56 / 65 / 64 / 69 / 76 / 110.
-    struct Shape {
-        int bm, bn, exact, fast;
-        hipError_t (*launch)(int, const E4m3GemmArgs &, hipStream_t);
-    };
-    static const Shape kShapes[] = {{256, 256, 3150, 1750, launch_e4m3_256x256}, {256, 128, 1800, 1000, launch_e4m3_256x128}, {128, 256, 1640, 980, launch_e4m3_128x256},
-                                    {128, 128, 880, 540, launch_e4m3_128x128}, {64, 256, 910, 600, launch_e4m3_64x256}, {64, 64, 300, 215, launch_e4m3_64x64}};
-    const Shape *best = nullptr;
-    int64_t least = 0;
-    for (const Shape &c : kShapes) {
-        if (gated && c.bn != 256) continue;
-        const int64_t bf = gated ? c.bn / 2 : c.bn, tiles = ((g.M + c.bm - 1) / c.bm) * ((g.N + bf - 1) / bf);
-        const int64_t cost = (tiles + 255) / 256 * (g.fast ? c.fast : c.exact);
-        if (!best || cost < least) best = &c, least = cost;
-    }
-    return best->launch(kind, g, s);
+    if (g.M <= kE4m3FewRows) return launch_few_rows(kind, g, g.codes ? static_cast<float *>(workspace) : nullptr, s);
+    static hipError_t (*const launch[kE4m3ShapeCount])(int, const E4m3GemmArgs &, hipStream_t) = {launch_e4m3_256x256, launch_e4m3_256x128, launch_e4m3_128x256,
+                                                                                             launch_e4m3_128x128, launch_e4m3_64x256, launch_e4m3_64x64};
+    return launch[e4m3_shape(g.M, g.N, kind >= kE4m3Silu, g.fast)](kind, g, s);
 }
 
 }  // namespace nvfp4
