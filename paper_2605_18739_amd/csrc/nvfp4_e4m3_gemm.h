@@ -34,9 +34,10 @@ enum { kE4m3F32 = 0, kE4m3Bf16 = 1, kE4m3Silu = 2, kE4m3Gelu = 3 };
 // With exact sums a step is four phases of two sub-steps (16 k each): a phase reads the next one's codes, a sub-step expands the
 // next one's operands between its matrix instructions, the barrier and the copies stand in front of and in the last phase.
 // (Rows of 64 bytes in four slots, with a barrier every 64 k and three half steps for a copy, took 2 to 6 % longer on large products.)
-// What bounds it is the clock that the matrix pipes hold: 3520 x 4096 x 14336 takes 181 us with fast sums (2.28 PFLOP/s, matrix
-// instructions in 52 % of the SIMDs' cycles) and 316 with exact ones (1.31); gated 3520 x 2*11008 x 4096, gate and up kept, exact, 510 (1.24);
-// 4096 x 2048 x 17600, 256 tiles of 128 x 256, 262 to 278 (1.1: the two stages do not cover a line's first way from memory in full).
+// What bounds it is the clock that the matrix pipes hold: 3520 x 4096 x 14336 takes 182 to 185 us with fast sums (2.25 PFLOP/s, matrix
+// instructions in 54 % of the SIMDs' cycles) and 316 with exact ones (1.31); gated 3520 x 2*11008 x 4096, gate and up kept, 470 to 490 with
+// exact sums (1.3), 285 with fast ones (2.2: prologue and epilogue of its five rounds of tiles are not hidden, 96 us at K = 128);
+// 4096 x 2048 x 17600, 256 tiles of 128 x 256, 280 (1.05: the two stages do not cover a line's first way from memory in full).
 template <int BM, int BN, int KIND, bool FAST, int STAGES>
 __global__ __launch_bounds__(256) void e4m3_gemm_kernel(const E4m3GemmArgs g)
 {

@@ -21,7 +21,7 @@ __device__ __forceinline__ float gated_value(const E4m3GemmArgs &g, int kind, in
 // projection that belong to them), its waves cut the blocks of 128 k between them and add their sums in LDS in a fixed order.
 // A wave's blocks go through a ring of DEPTH slots in LDS of its own, filled by copies that write LDS directly (eight rows of 128
 // bytes each, whole lines), so waves wait for their own copies only and there is no barrier on the way.  5 x 4096 x 14336 takes 12.6 us
-// (4.7 TB/s), 64 rows of it 20; 8 x 2*14336 x 4096 gated 26 with the launch behind it (20 at 5.9 TB/s, and 4.8), 64 rows 43.  (Loads
+// (4.7 TB/s), 64 rows of it 20; 8 x 2*14336 x 4096 gated 26 with the launch behind it (20 at 5.9 TB/s, and 4.8), 64 rows 33 and 4.9.  (Loads
 // straight into the instruction's operands, where neighbouring lanes hold different rows, take a cycle of the address unit for each
 // lane: 14, 43, 33 and 119 us.  Gated columns by the 128 to a workgroup, which would need no second launch: 41 to 49 us for 8 rows.)
 //   v_mfma_f32_16x16x32_bf16 on expanded codes, W as the row operand: lane (r = lane & 15, q = lane >> 4) holds chunks q and q + 4

@@ -14,7 +14,7 @@ namespace nvfp4 {
 // (LDS).  The codes along the tokens are turned in LDS: 16-byte chunks in an order that depends on the column.
 // Sixteen elements a lane leave room for the next tile's inputs, in flight while this one is computed: a workgroup goes from tile
 // to tile, and what it computes (45 to 60 vector instructions an element, about as long as the memory needs) hides behind its loads.
-// 7040 x 11008: 191 us, 4.5 TB/s; vector instructions take 57 % of the SIMDs' cycles.  (A workgroup of half the waves to each tile, which
+// 7040 x 11008: 194 us, 4.4 TB/s; vector instructions take 54 % of the SIMDs' cycles (GELU: 203 and 62 %).  (A workgroup of half the waves to each tile, which
 // ends with it: 240; half the waves that go from tile to tile spill the loads in flight: 369.)
 constexpr int kGatedWaves = 16;
 
